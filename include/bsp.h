@@ -255,6 +255,127 @@ bsp_status bsp_linear(const bsp_scheme *scheme, int32_t batch, bsp_dtype in_dt, 
 bsp_status bsp_maxpool2x2(bsp_dtype dt, int32_t n, int32_t c, int32_t h, int32_t w,
                           const void *x, void *y, void *stream);
 
+/* ---- decode: what a language model runs between and inside its FC layers, one token at a time ----
+ *
+ * FC layers with 4-bit weights and group scales.  The format: a row-major rows x cols matrix W is
+ * cut into groups of `group` (32, 64 or 128) consecutive columns of one row (the last may be short);
+ *   W[r][k] ~ scales[k / group][r] * (code(r, k) - 8),   code 0 .. 15
+ *   codes   code(r, k) is the low (k even) or high (k odd) half of byte k / 2 of row r; rows begin
+ *           every 16 * ceil(ceil(cols / 2) / 16) bytes; 16-byte aligned
+ *   scales  bf16, [ceil(cols / group)][rows rounded up to 16]; 8-byte aligned
+ * What lies between a row's last code and the next row, and scales past the last row, are not read
+ * as values.  Rows of codes and of scales may be longer than 2^31 bytes in all. */
+
+/* Bytes of `codes` and elements of `scales`.  Host-only, pure. */
+bsp_status bsp_q4_sizes(int32_t rows, int32_t cols, int32_t group, int64_t *code_bytes, int64_t *n_scales);
+
+/* Quantise: a = the largest |w| of the group, s = a * (1 / 7) (in fp32) rounded to bf16 (RNE), code =
+ * 8 + clamp(round(w / s), -7, 7) (fp32 division, ties to even); 8 where s is 0.  Weights removed by
+ * mask_or_null (rows x cols bytes, as from bsp_prune) count as 0 and so stay exactly 0: a pruned
+ * layer keeps its zeros.  w must be finite.  The padding of codes and scales is set to 0.  Async. */
+bsp_status bsp_q4_quantize(int32_t rows, int32_t cols, int32_t group, bsp_dtype wdt, const void *w,
+                           const uint8_t *mask_or_null, uint8_t *codes, void *scales, void *stream);
+
+/* The weights that codes stand for, scales[k / group][r] * (code - 8) in fp32, rounded to wdt (RNE):
+ * for checkpoints, tests, and layers that bsp_pack takes as well (large batches).  Async. */
+bsp_status bsp_q4_dequantize(int32_t rows, int32_t cols, int32_t group, bsp_dtype wdt, const uint8_t *codes,
+                             const void *scales, void *w, void *stream);
+
+/* Forward of an FC layer with such weights, on feature-major activations as bsp_linear:
+ *   y[o][b] = bias[o] + sum_g scales[g][o] * sum_{k in g} (code(o, k) - 8) * x[k][b], then ReLU if relu.
+ * Made for small batches (decoding); right for any.  Sums are in fp32 (x of BSP_F32 is multiplied in
+ * full); x must be finite, and an Inf or NaN makes every output of its batch column NaN.  No
+ * workspace.  Async. */
+bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batch, bsp_dtype in_dt, bsp_dtype out_dt,
+                         const void *x, const uint8_t *codes, const void *scales, const float *bias_or_null,
+                         int32_t relu, void *y, void *stream);
+
+/* Keys and values of the tokens seen so far lie in pages of page_size tokens.  Token t of sequence s
+ * is slot t % page_size of page table[s][t / page_size]; entries of the table that are negative (or
+ * not below `pages`) hold nothing.  Keys and values of one layer are arrays of `pages` pages each, a
+ * page being
+ *   BSP_HEAD_MAJOR  [kv_heads][page_size][head_dim]
+ *   BSP_SLOT_MAJOR  [page_size][kv_heads][head_dim]
+ * and page_stride elements after the one before (0: no gap).  16-byte aligned; head_dim is a
+ * multiple of 8 up to 256. */
+typedef enum { BSP_HEAD_MAJOR = 0, BSP_SLOT_MAJOR = 1 } bsp_page_order;
+typedef struct {
+    int32_t dtype;          /* bsp_dtype of keys, values, queries and attention outputs */
+    int32_t order;          /* bsp_page_order */
+    int32_t pages, page_size, kv_heads, head_dim;
+    int64_t page_stride;    /* a multiple of 16 bytes, at least a page, or 0 */
+} bsp_cache;
+
+/* Element strides of a [sequence or token][head][dim] array.  Feature-major activations
+ * [heads * head_dim][batch] have {1, head_dim * batch, batch}. */
+typedef struct {
+    int64_t seq, head, dim;
+} bsp_strides;
+
+/* Writes the keys k and values v of n tokens (strides ks, vs; dtype of the cache) into the cache:
+ * token i goes to position pos[i] of sequence rows[i] (rows NULL: i).  A token whose position is
+ * negative, past the table or in an entry that holds nothing, or whose sequence is not in
+ * 0 .. seqs - 1, is not written.  No two tokens may share a place.  Async. */
+bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, const bsp_strides *ks, const void *v,
+                            const bsp_strides *vs, void *keys, void *values, const int32_t *table, int32_t seqs,
+                            int32_t width, const int32_t *rows_or_null, const int32_t *pos, void *stream);
+
+/* Attention of one new token of each of `batch` sequences over its cached tokens:
+ *   y[b][h] = sum_t p[t] * value[t],  p = softmax over t of scale * <q[b][h], key[t]>
+ * with the key head h / (heads / kv_heads), over tokens t from max(0, len - window) (window 0: from
+ * 0) to len = lens[row] that lie in pages; row = rows[b] (rows NULL: b).  lse_or_null
+ * [batch][heads] receives log sum exp of the scores, with which parts of one attention are joined.
+ * No such token (len 0, no page, row not in 0 .. seqs - 1): y = 0 and lse = -Inf.  lens above width *
+ * page_size read as that.  Nothing else of the cache is used: what other slots hold, NaN too,
+ * does not reach y.  Scores, sums and the softmax are in fp32; for BSP_BF16, probabilities are
+ * rounded to bf16 before they multiply the values.
+ * workspace: bsp_attention_workspace bytes, 16-byte aligned, whose content does not matter; calls
+ * that may overlap need one each.  Async. */
+bsp_status bsp_attention_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t width, int64_t *bytes);
+bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, const void *q, const bsp_strides *qs,
+                         const void *keys, const void *values, const int32_t *table, int32_t seqs, int32_t width,
+                         const int32_t *rows_or_null, const int32_t *lens, float scale, int32_t window, void *y,
+                         const bsp_strides *ys, float *lse_or_null, void *workspace, void *stream);
+
+/* Care of the pages.  The state is on the device and the host never waits for it: table
+ * [seqs][width], lens [seqs], and refs [pages], the number of table entries that name a page (0: the
+ * page is free).  Free pages are given out lowest first, so results are unique.  `data` are the
+ * planes of a model that share one table (keys and values of every layer): `planes` arrays of pages,
+ * plane_stride elements apart.  Rows that are not in 0 .. seqs - 1 are left out; the rows that one
+ * call changes must differ.  scratch: bsp_cache_scratch bytes (n: the longest list of the calls),
+ * 16-byte aligned, whose content does not matter.  All async. */
+bsp_status bsp_cache_scratch(const bsp_cache *cache, int32_t seqs, int32_t width, int32_t n, int64_t *bytes);
+
+/* Sequence children[i] becomes sequence parents[i]: the same pages, now shared.  All parents are read
+ * before any child changes, so beams may be permuted in place; what a child held is released. */
+bsp_status bsp_cache_fork(int32_t seqs, int32_t width, int32_t pages, int32_t *table, int32_t *lens, int32_t *refs,
+                          int32_t n, const int32_t *parents, const int32_t *children, void *scratch, void *stream);
+
+/* Room for counts[i] more tokens in each sequence rows[i]: pages for the positions from pos[i] =
+ * lens[rows[i]] on, which becomes pos[i] + counts[i].  A last page that has tokens and that another
+ * entry shares is first copied (the slots in use) to a page of the sequence's own (a last entry that
+ * names no page just gets one).  Where the free
+ * pages or the width do not suffice for the whole call, nothing changes and every pos is -1; so is
+ * that of a row that is left out. */
+bsp_status bsp_cache_extend(const bsp_cache *cache, int32_t planes, int64_t plane_stride, void *data, int32_t seqs,
+                            int32_t width, int32_t *table, int32_t *lens, int32_t *refs, int32_t n,
+                            const int32_t *rows, const int32_t *counts, int32_t *pos, void *scratch, void *stream);
+
+/* Sequences rows[i] end: their entries become -1, their lengths 0. */
+bsp_status bsp_cache_release(int32_t seqs, int32_t width, int32_t pages, int32_t *table, int32_t *lens, int32_t *refs,
+                             int32_t n, const int32_t *rows, void *stream);
+
+/* With U pages in use, the k-th of those at U or above moves to the k-th free one below U, so that
+ * pages 0 .. U - 1 are the ones in use.  info (2 int32) receives U and the number of pages moved. */
+bsp_status bsp_cache_compact(const bsp_cache *cache, int32_t planes, int64_t plane_stride, void *data, int32_t seqs,
+                             int32_t width, int32_t *table, int32_t *refs, int32_t *info, void *scratch,
+                             void *stream);
+
+/* Copies page src[i] to page dst[i] in every plane; pairs with a page not in 0 .. pages - 1 are left
+ * out.  No page may be written twice, or both read and written. */
+bsp_status bsp_cache_copy(const bsp_cache *cache, int32_t planes, int64_t plane_stride, void *data, int32_t n,
+                          const int32_t *src, const int32_t *dst, void *stream);
+
 /* Static string for a status code. */
 const char *bsp_status_string(bsp_status status);
 

@@ -11,17 +11,23 @@ built, importing the functions raises - there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 __all__ = [
     "F32", "BF16", "ROW", "COL", "UNSTRUCTURED", "DENSE", "PUNCHED", "ROWCOL", "PATTERN", "BspError", "Scheme", "ConvShape",
     "lib", "lib_path", "bsp_packed_sizes", "bsp_prune", "bsp_prune_noalloc", "bsp_pack", "bsp_unpack", "bsp_conv2d",
     "bsp_linear", "bsp_maxpool2x2", "bsp_status_string", "bsp_version", "bsp_to_bcs",
+    "HEAD_MAJOR", "SLOT_MAJOR", "CacheShape", "bsp_q4_sizes", "bsp_q4_quantize", "bsp_q4_dequantize", "bsp_q4_linear",
+    "bsp_attention_workspace", "bsp_attention", "bsp_cache_append", "bsp_cache_scratch", "bsp_cache_fork",
+    "bsp_cache_extend", "bsp_cache_release", "bsp_cache_compact", "bsp_cache_copy",
 ]
 
 _I64x4 = ctypes.c_int64 * 4
 F32, BF16 = 0, 1
 ROW, COL, UNSTRUCTURED, DENSE, PUNCHED, ROWCOL, PATTERN = 0, 1, 2, 3, 4, 5, 6
+
+HEAD_MAJOR, SLOT_MAJOR = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "_build", "libbsp.so")
@@ -56,6 +62,31 @@ class ConvShape(ctypes.Structure):
                                                "stride_w", "pad_h", "pad_w")]
 
 
+class CacheShape(ctypes.Structure):
+    """bsp_cache: the pages of a cache's keys or values (one layer's)."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "order", "pages", "page_size", "kv_heads", "head_dim")] + [
+        ("page_stride", ctypes.c_int64)]
+
+    @classmethod
+    def of(cls, plane, order: int = HEAD_MAJOR) -> "CacheShape":
+        """The shape of one plane of pages, [pages, kv_heads, page_size, head_dim] (HEAD_MAJOR) or
+        [pages, page_size, kv_heads, head_dim] (SLOT_MAJOR), each page contiguous."""
+        pages, a, b, dim = plane.shape
+        heads, slots = (a, b) if order == HEAD_MAJOR else (b, a)
+        c = cls({4: F32, 2: BF16}[plane.element_size()], order, pages, slots, heads, dim,
+                plane.stride(0) if pages > 1 else 0)
+        _plane("plane", c, plane)
+        return c
+
+    def plane_shape(self):
+        inner = (self.kv_heads, self.page_size) if self.order == HEAD_MAJOR else (self.page_size, self.kv_heads)
+        return (self.pages, *inner, self.head_dim)
+
+
+class _Strides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("seq", "head", "dim")]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -82,8 +113,25 @@ def lib():
     L.bsp_status_string.argtypes = [I32]
     L.bsp_status_string.restype = ctypes.c_char_p
     L.bsp_version.argtypes = []
+    I64, ca, sd = ctypes.c_int64, P(CacheShape), P(_Strides)
+    L.bsp_q4_sizes.argtypes = [I32, I32, I32, VP, VP]
+    L.bsp_q4_quantize.argtypes = [I32, I32, I32, I32, VP, VP, VP, VP, VP]
+    L.bsp_q4_dequantize.argtypes = [I32, I32, I32, I32, VP, VP, VP, VP]
+    L.bsp_q4_linear.argtypes = [I32] * 6 + [VP, VP, VP, VP, I32, VP, VP]
+    L.bsp_cache_append.argtypes = [ca, I32, VP, sd, VP, sd, VP, VP, VP, I32, I32, VP, VP, VP]
+    L.bsp_attention_workspace.argtypes = [ca, I32, I32, I32, VP]
+    L.bsp_attention.argtypes = [ca, I32, I32, VP, sd, VP, VP, VP, I32, I32, VP, VP, ctypes.c_float, I32, VP, sd, VP, VP, VP]
+    L.bsp_cache_scratch.argtypes = [ca, I32, I32, I32, VP]
+    L.bsp_cache_fork.argtypes = [I32, I32, I32, VP, VP, VP, I32, VP, VP, VP, VP]
+    L.bsp_cache_extend.argtypes = [ca, I32, I64, VP, I32, I32, VP, VP, VP, I32, VP, VP, VP, VP, VP]
+    L.bsp_cache_release.argtypes = [I32, I32, I32, VP, VP, VP, I32, VP, VP]
+    L.bsp_cache_compact.argtypes = [ca, I32, I64, VP, I32, I32, VP, VP, VP, VP, VP]
+    L.bsp_cache_copy.argtypes = [ca, I32, I64, VP, I32, VP, VP, VP]
     for f in ("bsp_packed_sizes", "bsp_prune", "bsp_prune_noalloc", "bsp_pack", "bsp_unpack", "bsp_conv2d",
-              "bsp_linear", "bsp_maxpool2x2", "bsp_version", "bsp_to_bcs"):
+              "bsp_linear", "bsp_maxpool2x2", "bsp_version", "bsp_to_bcs", "bsp_q4_sizes", "bsp_q4_quantize",
+              "bsp_q4_dequantize", "bsp_q4_linear", "bsp_cache_append", "bsp_attention_workspace", "bsp_attention",
+              "bsp_cache_scratch", "bsp_cache_fork", "bsp_cache_extend", "bsp_cache_release", "bsp_cache_compact",
+              "bsp_cache_copy"):
         getattr(L, f).restype = I32
     _lib = L
     return L
@@ -247,3 +295,209 @@ def bsp_maxpool2x2(dt: int, n: int, c: int, h: int, w: int, x, y, stream=None):
     _need("y", y, n * c * (h // 2) * (w // 2) * _esize(dt))
     _check("bsp_maxpool2x2", lib().bsp_maxpool2x2(int(dt), int(n), int(c), int(h), int(w), _p(x),
                                                   _p(y), _stream(stream)))
+
+
+# ---- decode: 4-bit FC layers, attention over a paged cache, care of its pages ----
+
+def _dev(name: str, t, nbytes: int):
+    """A contiguous device array of at least `nbytes`."""
+    _need(name, t, nbytes)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the device")
+
+
+def _ints(name: str, t, n: int):
+    _dev(name, t, 4 * n)
+    if t.element_size() != 4 or t.is_floating_point():
+        raise ValueError(f"{name} must be int32")
+
+
+def _plane(name: str, cache: CacheShape, t):
+    """Keys or values of one layer."""
+    if tuple(t.shape) != cache.plane_shape() or t.element_size() != _esize(cache.dtype):
+        raise ValueError(f"{name} is not an array of the cache's pages")
+    d = cache.head_dim
+    page = cache.kv_heads * cache.page_size * d
+    want = (cache.page_stride or page, (cache.page_size if cache.order == HEAD_MAJOR else cache.kv_heads) * d, d, 1)
+    if any(n > 1 and have != s for n, have, s in zip(t.shape, t.stride(), want)):
+        raise ValueError(f"{name}: the pages are not contiguous, or not page_stride elements apart")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the device")
+
+
+@functools.lru_cache(maxsize=1024)
+def _strides(seq: int, head: int, dim: int) -> _Strides:
+    return _Strides(seq, head, dim)
+
+
+def _heads(name: str, t, cache: CacheShape, n: int, heads: int):
+    """Strides of an [n, heads, head_dim] array of the cache's type."""
+    if tuple(t.shape) != (n, heads, cache.head_dim) or t.element_size() != _esize(cache.dtype):
+        raise ValueError(f"{name} must be [{n}, {heads}, {cache.head_dim}] of the cache's type")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the device")
+    return _strides(*t.stride())
+
+
+def _table(table):
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences, width]")
+    _ints("table", table, 0)
+    return table.shape
+
+
+def bsp_q4_sizes(rows: int, cols: int, group: int):
+    """-> (bytes of codes, elements of scales)."""
+    out = (ctypes.c_int64 * 2)()
+    a = ctypes.addressof(out)
+    _check("bsp_q4_sizes", lib().bsp_q4_sizes(int(rows), int(cols), int(group), a, a + 8))
+    return tuple(out)
+
+
+def _q4_arrays(rows, cols, group, codes, scales):
+    nc, ns = bsp_q4_sizes(rows, cols, group)
+    _dev("codes", codes, nc)
+    _dev("scales", scales, ns * 2)
+
+
+def bsp_q4_quantize(rows: int, cols: int, group: int, wdt: int, w, mask, codes, scales, stream=None):
+    _q4_arrays(rows, cols, group, codes, scales)
+    _dev("w", w, rows * cols * _esize(wdt))
+    if mask is not None:
+        _dev("mask", mask, rows * cols)
+    _check("bsp_q4_quantize", lib().bsp_q4_quantize(int(rows), int(cols), int(group), int(wdt), _p(w), _p(mask),
+                                                    _p(codes), _p(scales), _stream(stream)))
+
+
+def bsp_q4_dequantize(rows: int, cols: int, group: int, wdt: int, codes, scales, w, stream=None):
+    _q4_arrays(rows, cols, group, codes, scales)
+    _dev("w", w, rows * cols * _esize(wdt))
+    _check("bsp_q4_dequantize", lib().bsp_q4_dequantize(int(rows), int(cols), int(group), int(wdt), _p(codes), _p(scales),
+                                                        _p(w), _stream(stream)))
+
+
+def bsp_q4_linear(rows: int, cols: int, group: int, batch: int, in_dt: int, out_dt: int, x, codes, scales, bias,
+                  relu: bool, y, stream=None):
+    _q4_arrays(rows, cols, group, codes, scales)
+    _dev("x", x, cols * batch * _esize(in_dt))
+    _dev("y", y, rows * batch * _esize(out_dt))
+    if bias is not None:
+        _dev("bias", bias, rows * 4)
+    _check("bsp_q4_linear", lib().bsp_q4_linear(int(rows), int(cols), int(group), int(batch), int(in_dt), int(out_dt),
+                                                _p(x), _p(codes), _p(scales), _p(bias), int(bool(relu)), _p(y),
+                                                _stream(stream)))
+
+
+def bsp_cache_append(cache: CacheShape, k, v, keys, values, table, pos, rows=None, stream=None):
+    """k and v: [tokens, kv_heads, head_dim] of any strides."""
+    n = k.shape[0]
+    ks, vs = _heads("k", k, cache, n, cache.kv_heads), _heads("v", v, cache, n, cache.kv_heads)
+    _plane("keys", cache, keys)
+    _plane("values", cache, values)
+    seqs, width = _table(table)
+    _ints("pos", pos, n)
+    if rows is not None:
+        _ints("rows", rows, n)
+    _check("bsp_cache_append", lib().bsp_cache_append(cache, n, _p(k), ks, _p(v), vs, _p(keys), _p(values), _p(table), seqs,
+                                                      width, _p(rows), _p(pos), _stream(stream)))
+
+
+def bsp_attention_workspace(cache: CacheShape, batch: int, heads: int, width: int) -> int:
+    """Bytes of bsp_attention's workspace."""
+    out = ctypes.c_int64()
+    _check("bsp_attention_workspace", lib().bsp_attention_workspace(cache, int(batch), int(heads), int(width),
+                                                                    ctypes.addressof(out)))
+    return out.value
+
+
+def bsp_attention(cache: CacheShape, q, keys, values, table, lens, y, scale: float, window: int = 0, rows=None, lse=None,
+                  workspace=None, stream=None):
+    """q and y: [batch, heads, head_dim] of any strides (y's elements distinct)."""
+    batch, heads = q.shape[:2]
+    qs, ys = _heads("q", q, cache, batch, heads), _heads("y", y, cache, batch, heads)
+    _plane("keys", cache, keys)
+    _plane("values", cache, values)
+    seqs, width = _table(table)
+    _ints("lens", lens, seqs)
+    if rows is not None:
+        _ints("rows", rows, batch)
+    if lse is not None:
+        _dev("lse", lse, batch * heads * 4)
+    need = bsp_attention_workspace(cache, batch, heads, width)
+    if need:
+        _dev("workspace", workspace, need)
+    _check("bsp_attention", lib().bsp_attention(cache, batch, heads, _p(q), qs, _p(keys), _p(values), _p(table), seqs, width,
+                                                _p(rows), _p(lens), float(scale), int(window), _p(y), ys, _p(lse),
+                                                _p(workspace), _stream(stream)))
+
+
+def bsp_cache_scratch(cache: CacheShape, seqs: int, width: int, n: int) -> int:
+    """Bytes of the scratch of fork, extend and compact with lists of up to n sequences."""
+    out = ctypes.c_int64()
+    _check("bsp_cache_scratch", lib().bsp_cache_scratch(cache, int(seqs), int(width), int(n), ctypes.addressof(out)))
+    return out.value
+
+
+def _state(table, lens, refs, pages=None):
+    seqs, width = _table(table)
+    _ints("lens", lens, seqs)
+    _ints("refs", refs, refs.numel() if pages is None else pages)
+    return seqs, width, refs.numel() if pages is None else pages
+
+
+def _planes(cache: CacheShape, data):
+    """Planes and plane stride of [planes, *plane_shape]."""
+    if data.dim() != 5 or data.shape[0] < 1:
+        raise ValueError("data must be [planes, pages, ., ., head_dim]")
+    _plane("data", cache, data[0])
+    return data.shape[0], data.stride(0)
+
+
+def bsp_cache_fork(table, lens, refs, parents, children, scratch, stream=None):
+    seqs, width, pages = _state(table, lens, refs)
+    n = parents.numel()
+    _ints("parents", parents, n)
+    _ints("children", children, n)
+    _dev("scratch", scratch, 4 * n * (width + 1))
+    _check("bsp_cache_fork", lib().bsp_cache_fork(seqs, width, pages, _p(table), _p(lens), _p(refs), n, _p(parents),
+                                                  _p(children), _p(scratch), _stream(stream)))
+
+
+def bsp_cache_extend(cache: CacheShape, data, table, lens, refs, rows, counts, pos, scratch, stream=None):
+    planes, plane_stride = _planes(cache, data)
+    seqs, width, _ = _state(table, lens, refs, cache.pages)
+    n = rows.numel()
+    _ints("rows", rows, n)
+    _ints("counts", counts, n)
+    _ints("pos", pos, n)
+    _dev("scratch", scratch, bsp_cache_scratch(cache, seqs, width, n))
+    _check("bsp_cache_extend", lib().bsp_cache_extend(cache, planes, plane_stride, _p(data), seqs, width, _p(table),
+                                                      _p(lens), _p(refs), n, _p(rows), _p(counts), _p(pos), _p(scratch),
+                                                      _stream(stream)))
+
+
+def bsp_cache_release(table, lens, refs, rows, stream=None):
+    seqs, width, pages = _state(table, lens, refs)
+    n = rows.numel()
+    _ints("rows", rows, n)
+    _check("bsp_cache_release", lib().bsp_cache_release(seqs, width, pages, _p(table), _p(lens), _p(refs), n, _p(rows),
+                                                        _stream(stream)))
+
+
+def bsp_cache_compact(cache: CacheShape, data, table, refs, info, scratch, stream=None):
+    planes, plane_stride = _planes(cache, data)
+    seqs, width = _table(table)
+    _ints("refs", refs, cache.pages)
+    _ints("info", info, 2)
+    _dev("scratch", scratch, bsp_cache_scratch(cache, seqs, width, 0))
+    _check("bsp_cache_compact", lib().bsp_cache_compact(cache, planes, plane_stride, _p(data), seqs, width, _p(table),
+                                                        _p(refs), _p(info), _p(scratch), _stream(stream)))
+
+
+def bsp_cache_copy(cache: CacheShape, data, src, dst, stream=None):
+    planes, plane_stride = _planes(cache, data)
+    n = src.numel()
+    _ints("src", src, n)
+    _ints("dst", dst, n)
+    _check("bsp_cache_copy", lib().bsp_cache_copy(cache, planes, plane_stride, _p(data), n, _p(src), _p(dst),
+                                                  _stream(stream)))
