@@ -292,7 +292,7 @@ bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batc
 
 /* Keys and values of the tokens seen so far lie in pages of page_size tokens.  Token t of sequence s
  * is slot t % page_size of page table[s][t / page_size]; entries of the table that are negative (or
- * not below `pages`) hold nothing.  Keys and values of one layer are arrays of `pages` pages each, a
+ * not below `pages`) hold nothing; width * page_size is at most 2^30.  Keys and values of one layer are arrays of `pages` pages each, a
  * page being
  *   BSP_HEAD_MAJOR  [kv_heads][page_size][head_dim]
  *   BSP_SLOT_MAJOR  [page_size][kv_heads][head_dim]

@@ -33,10 +33,11 @@ bsp_status check_cache(const bsp_cache *c) {
     return BSP_OK;
 }
 
-// A table of sequences, and positions in them, that 32-bit numbers count.
+constexpr int64_t kMaxTokens = 1 << 30;   // of a sequence: 32-bit numbers count positions, with room to round up
+
 bsp_status check_table(const int32_t *table, int32_t seqs, int32_t width, int32_t page_size) {
     if (seqs < 0 || width < 0 || (!table && (int64_t)seqs * width > 0)) return BSP_EINVAL;
-    return (int64_t)width * page_size > INT32_MAX ? BSP_EUNSUPPORTED : BSP_OK;
+    return (int64_t)width * page_size > kMaxTokens ? BSP_EUNSUPPORTED : BSP_OK;
 }
 
 bsp_status check_pages(const int32_t *table, const int32_t *lens, const int32_t *refs, int32_t seqs, int32_t width,
@@ -115,7 +116,7 @@ bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, co
 bsp_status bsp_attention_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t width, int64_t *bytes) {
     if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
     if (!bytes || batch < 0 || heads < 1 || heads % cache->kv_heads || width < 0) return BSP_EINVAL;
-    if ((int64_t)width * cache->page_size > INT32_MAX || (int64_t)batch * heads > INT32_MAX / 256) return BSP_EUNSUPPORTED;
+    if ((int64_t)width * cache->page_size > kMaxTokens || (int64_t)batch * heads > INT32_MAX / 256) return BSP_EUNSUPPORTED;
     *bytes = attention_workspace(cache_args(*cache), batch, heads, width);
     return BSP_OK;
 }
@@ -162,7 +163,7 @@ bsp_status bsp_cache_extend(const bsp_cache *cache, int32_t planes, int64_t plan
     if (const bsp_status st = check_planes(cache, planes, plane_stride, data); st != BSP_OK) return st;
     if (const bsp_status st = check_pages(table, lens, refs, seqs, width, cache->pages, n); st != BSP_OK) return st;
     if (n > 0 && (!rows || !counts || !pos || !scratch || !aligned(scratch, 16))) return BSP_EINVAL;
-    if ((int64_t)width * cache->page_size > INT32_MAX) return BSP_EUNSUPPORTED;
+    if ((int64_t)width * cache->page_size > kMaxTokens) return BSP_EUNSUPPORTED;
     if (n == 0) return BSP_OK;
     return status(launch_extend({seqs, width, cache->pages, table, lens, refs, n, (int32_t *)scratch},
                                 planes_args(cache, planes, plane_stride, data), rows, counts, pos, S(stream)));

@@ -66,9 +66,10 @@ struct AttnArgs {
     int batch, heads, group, seqs, width, window;
     float scale;
     void *workspace;
+    int chunk, splits, head_groups;   // set by launch_attention: tokens of a part, parts at most
 };
 int64_t attention_workspace(const CacheArgs &c, int batch, int heads, int width);
-hipError_t launch_attention(const AttnArgs &a, hipStream_t st);
+hipError_t launch_attention(AttnArgs a, hipStream_t st);
 
 // ---- pages ----
 struct PagesArgs {

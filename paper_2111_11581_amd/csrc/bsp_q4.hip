@@ -4,24 +4,11 @@
 #include <hip/hip_runtime.h>
 
 #include "bsp_decode.h"
+#include "bsp_decode_dev.h"
 
 namespace bsp {
 
 namespace {
-
-__device__ __forceinline__ float bf16_to_f32(uint32_t h) { return __uint_as_float(h << 16); }
-// Round to nearest even; NaN stays NaN.
-__device__ __forceinline__ uint16_t f32_to_bf16(float f) {
-    const uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40u);
-    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-}
-template <typename E> __device__ __forceinline__ float to_f32(E v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t v) { return bf16_to_f32(v); }
-template <typename E> __device__ __forceinline__ E from_f32(float v);
-template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) { return f32_to_bf16(v); }
 
 // Eight consecutive elements of a row, those at or past `n` read as 0.
 template <typename E, bool VEC>
