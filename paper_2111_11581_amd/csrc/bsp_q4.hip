@@ -5,6 +5,7 @@
 
 #include "bsp_decode.h"
 #include "bsp_decode_dev.h"
+#include "bsp_q4_mm.h"
 
 namespace bsp {
 
@@ -84,49 +85,6 @@ __global__ __launch_bounds__(256) void k_q4_dequantize(Q4Shape s, const uint8_t 
     }
 }
 
-// A wave computes one row for 8 vectors: lanes take 8 columns at a time.
-template <typename X, typename Y>
-__global__ __launch_bounds__(256) void k_q4_linear(Q4Shape s, int batch, const X *__restrict__ x,
-                                                   const uint8_t *__restrict__ codes, const uint16_t *__restrict__ scales,
-                                                   const float *__restrict__ bias, int relu, Y *__restrict__ y) {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    const int lane = threadIdx.x % 64;
-    if (row >= s.rows) return;
-    for (int64_t b0 = blockIdx.y * 8; b0 < batch; b0 += gridDim.y * 8) {
-    float acc[8] = {};
-    for (int64_t col = lane * 8; col < s.cols; col += 512) {
-        const uint32_t packed = *(const uint32_t *)(codes + row * s.stride + col / 2);
-        const float sf = bf16_to_f32(scales[col / s.group * s.rows16 + row]);
-        float part[8] = {};
-        for (int i = 0; i < 8; ++i) {
-            if (col + i >= s.cols) break;
-            const float q = (float)((int)(packed >> (4 * i) & 15) - 8);
-#pragma unroll
-            for (int b = 0; b < 8; ++b)
-                if (b0 + b < batch) part[b] += q * to_f32<X>(x[(col + i) * batch + b0 + b]);
-        }
-#pragma unroll
-        for (int b = 0; b < 8; ++b) acc[b] += sf * part[b];
-    }
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-        for (int d = 1; d < 64; d *= 2) acc[b] += __shfl_xor(acc[b], d);
-        if (lane == 0 && b0 + b < batch) {
-            float v = acc[b] + (bias ? bias[row] : 0.f);
-            if (relu && v < 0.f) v = 0.f;
-            y[row * batch + b0 + b] = from_f32<Y>(v);
-        }
-    }
-    }
-}
-
-template <typename X, typename Y>
-void linear(const Q4Shape &s, int batch, const void *x, const uint8_t *codes, const uint16_t *scales, const float *bias,
-            int relu, void *y, hipStream_t st) {
-    const dim3 grid((s.rows + 3) / 4, std::min((batch + 7) / 8, 65535));
-    k_q4_linear<X, Y><<<grid, 256, 0, st>>>(s, batch, (const X *)x, codes, scales, bias, relu, (Y *)y);
-}
-
 // Rows that begin at multiples of 16 bytes are read and written in vectors.
 template <typename E> bool in_vectors(const Q4Shape &s, const void *w) {
     return s.cols % (16 / (int)sizeof(E)) == 0 && (uintptr_t)w % 16 == 0;
@@ -172,15 +130,8 @@ hipError_t launch_q4_dequantize(const Q4Shape &s, int wdt, const uint8_t *codes,
 
 hipError_t launch_q4_linear(const Q4Shape &s, int batch, int in_dt, int out_dt, const void *x, const uint8_t *codes,
                             const uint16_t *scales, const float *bias, int relu, void *y, hipStream_t st) {
-    if (in_dt == BSP_F32 && out_dt == BSP_F32)
-        linear<float, float>(s, batch, x, codes, scales, bias, relu, y, st);
-    else if (in_dt == BSP_F32)
-        linear<float, uint16_t>(s, batch, x, codes, scales, bias, relu, y, st);
-    else if (out_dt == BSP_F32)
-        linear<uint16_t, float>(s, batch, x, codes, scales, bias, relu, y, st);
-    else
-        linear<uint16_t, uint16_t>(s, batch, x, codes, scales, bias, relu, y, st);
-    return hipGetLastError();
+    const Q4Args a = {s, x, codes, scales, bias, y, batch, relu, out_dt == BSP_BF16, (uintptr_t)x % 16 == 0, 0};
+    return in_dt == BSP_F32 ? q4_linear_f32(a, st) : q4_linear_bf16(a, st);
 }
 
 }  // namespace bsp
