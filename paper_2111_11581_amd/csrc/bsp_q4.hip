@@ -130,7 +130,7 @@ hipError_t launch_q4_dequantize(const Q4Shape &s, int wdt, const uint8_t *codes,
 
 hipError_t launch_q4_linear(const Q4Shape &s, int batch, int in_dt, int out_dt, const void *x, const uint8_t *codes,
                             const uint16_t *scales, const float *bias, int relu, void *y, hipStream_t st) {
-    const Q4Args a = {s, x, codes, scales, bias, y, batch, relu, out_dt == BSP_BF16, (uintptr_t)x % 16 == 0, 0};
+    const Q4Args a = {s, x, codes, scales, bias, y, batch, relu, out_dt == BSP_BF16, 0};
     return in_dt == BSP_F32 ? q4_linear_f32(a, st) : q4_linear_bf16(a, st);
 }
 

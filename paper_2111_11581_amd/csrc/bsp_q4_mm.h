@@ -10,7 +10,10 @@
 //
 // Activations pass through LDS, a wave's own part of it, so the main loop has no barrier:
 //  * one vector: 128 elements a chunk, in the order of the codes' pairs; a lane reads 16 bytes.
-//  * more: rows of the feature-major array; transposing LDS reads give a lane 4 rows of one column.
+//  * more: rows of 16 NT elements of the feature-major array, loaded 16 bytes at a time at whatever
+//    alignment; transposing LDS reads give a lane 4 rows of one column.  Rows of 64 elements are
+//    twisted (32-byte pieces exchanged by bits 2 and 3 of the row), or the 16 rows that one read
+//    touches would lie in the same banks.
 //  * fp32 activations are cut into three bf16 (8 bits each, 24 in all), whose products are added.
 // The waves of a workgroup take 128-column chunks in turn and are joined at the end.
 #pragma once
@@ -27,7 +30,6 @@ struct Q4Args {
     const float *bias;
     void *y;
     int batch, relu, out_bf16;
-    int vec;                      // x is 16-byte aligned
     int waves;
 };
 
@@ -37,19 +39,14 @@ constexpr int kQ4Waves = 8;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// How activations come into the operands.
-constexpr int kOne = 0;           // one vector
-constexpr int kTr = 1;            // rows of a multiple of 4 elements in LDS: transposing reads
-constexpr int kEach = 2;          // rows of any length: read element by element
-
 // Columns of x staged at a time, bf16 parts of an element, and a wave's LDS bytes.
 template <typename X> constexpr int q4_parts() { return sizeof(X) == 4 ? 3 : 1; }
 template <typename X, int NT> constexpr int q4_stage() {
     return sizeof(X) == 4 ? kQ4Chunk / NT : NT == 4 ? 64 : kQ4Chunk;
 }
-template <typename X, int NT, int MT, int MODE> constexpr int q4_wave_lds() {
-    constexpr int stage = MODE == kOne ? 4 * kQ4Chunk * 2 * q4_parts<X>() : q4_stage<X, NT>() * 16 * NT * 2 * q4_parts<X>();
-    constexpr int join = (MODE == kOne ? 1 : 16 * NT) * (16 * MT + 4) * 4;
+template <typename X, int NT, int MT, bool ONE> constexpr int q4_wave_lds() {
+    constexpr int stage = ONE ? 4 * kQ4Chunk * 2 * q4_parts<X>() : q4_stage<X, NT>() * 16 * NT * 2 * q4_parts<X>();
+    constexpr int join = (ONE ? 1 : 16 * NT) * (16 * MT + 4) * 4;
     return stage > join ? stage : join;
 }
 
@@ -70,8 +67,8 @@ __device__ __forceinline__ void q4_transpose(uint32_t *d) {
 // Eight codes as 1 + n / 16, in the order of pairs (0, 4), (1, 5), (2, 6), (3, 7).
 __device__ __forceinline__ bf16x8 q4_expand(uint32_t d) {
     const uint32_t mask = 0x00780078u, one = 0x3f803f80u;
-    return as_bf16x8(make_uint4(((d << 3) & mask) | one, ((d >> 1) & mask) | one, ((d >> 5) & mask) | one,
-                                ((d >> 9) & mask) | one));
+    return as_bf16x8((u32x4){((d << 3) & mask) | one, ((d >> 1) & mask) | one, ((d >> 5) & mask) | one,
+                                ((d >> 9) & mask) | one});
 }
 
 // The three bf16 whose sum an fp32 is (cut, not rounded, so that nothing overflows); Inf and NaN are
@@ -88,16 +85,15 @@ __device__ __forceinline__ void q4_cut(float x, uint16_t *p) {
 }
 __device__ __forceinline__ void q4_cut(uint16_t x, uint16_t *p) { p[0] = x; }
 
-// A workgroup: 16 MT rows, 16 NT vectors (kOne: one vector).
-template <typename X, int G, int NT, int MT, int MODE>
+// A workgroup: 16 MT rows, 16 NT vectors (ONE: one vector).
+template <typename X, int G, int NT, int MT, bool ONE>
 __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
-    constexpr bool ONE = MODE == kOne;
     constexpr int PARTS = q4_parts<X>(), GPC = kQ4Chunk / G, SPG = G / 32;   // groups of a chunk, steps of a group
     constexpr int STAGE = ONE ? kQ4Chunk : q4_stage<X, NT>();
     constexpr int PF = ONE ? 4 : 1;                                           // chunks in flight ahead
     constexpr int VE = 16 / sizeof(X);                                        // elements of a 16-byte load
     constexpr int NV = ONE ? 1 : STAGE * 16 * NT / VE / 64;                   // such loads of a lane and stage
-    constexpr int WLDS = q4_wave_lds<X, NT, MT, MODE>();
+    constexpr int WLDS = q4_wave_lds<X, NT, MT, ONE>();
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, quad = lane / 16;
     const int rows = a.s.rows, cols = a.s.cols, B = a.batch, W = a.waves;
@@ -105,12 +101,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     unsigned char *mine = lds + wave * WLDS;
     const X *x = (const X *)a.x;
 
-    // vectors of this workgroup.  With up to 16 NT in all (flat) a stage of x is one run of memory and
-    // lies in LDS as it is; otherwise in rows of 16 NT.
-    const int c0 = ONE ? 0 : blockIdx.y * (16 * NT), nc = ONE ? 1 : min(16 * NT, B - c0);
-    const bool flat = MODE == kEach || B <= 16 * NT;
-    const int RS = flat ? B : 16 * NT;
-    const bool fast = a.vec && (flat || B % VE == 0);   // whole stages are loaded 16 bytes at a time
+    const int c0 = ONE ? 0 : blockIdx.y * (16 * NT), nc = ONE ? 1 : min(16 * NT, B - c0);   // its vectors
 
     const uint8_t *wp[MT];
     const uint16_t *sp = a.scales + row0 + quad * 4;
@@ -119,18 +110,18 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     const int n_chunks = (cols + kQ4Chunk - 1) / kQ4Chunk;
 
     struct Weights {
-        uint4 w[MT];
-        uint2 s[MT][GPC];
+        u32x4 w[MT];
+        u32x2 s[MT][GPC];
     };
     auto load_w = [&](int c, Weights &w) {   // past a row's end: its last 16 bytes, whose x is 0
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int64_t at = min((int64_t)c * 64, a.s.stride - 16 - quad * 16);
-            w.w[m] = *(const uint4 *)(wp[m] + at);
+            w.w[m] = *(const u32x4 *)(wp[m] + at);
 #pragma unroll
             for (int g = 0; g < GPC; ++g) {
                 const int64_t group = min(c * GPC + g, a.s.n_groups - 1);
-                w.s[m][g] = *(const uint2 *)(sp + group * a.s.rows16 + min((int64_t)16 * m, a.s.rows16 - 16 - row0));
+                w.s[m][g] = *(const u32x2 *)(sp + group * a.s.rows16 + min((int64_t)16 * m, a.s.rows16 - 16 - row0));
             }
         }
     };
@@ -155,73 +146,85 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
             for (int t = 0; t < PARTS; ++t) at[t * kQ4Chunk + 2 * i] = p[t];
         }
     };
-    // more: a whole stage, 16 bytes at a time
-    constexpr int PLANE = STAGE * 16 * NT;
+    // more: rows of a stage, 16 bytes at a time.  What a row's last load takes past the vectors goes to
+    // columns that no output has.
+    constexpr int RS = 16 * NT, PLANE = STAGE * RS;
     struct Stage {
-        uint4 raw[NV];
+        u32x4 raw[NV];
+    };
+    auto twist = [](int row) { return NT == 4 ? (row >> 2 & 3) << 4 : 0; };   // in elements
+    const int total = cols * B;
+    auto whole = [&](int64_t k0) {   // a stage whose loads end within x
+        return k0 + STAGE <= cols && (k0 + STAGE - 1) * B + c0 + (nc + VE - 1) / VE * VE <= total;
     };
     auto load_stage = [&](int64_t k0, Stage &v) {
         const X *p = x + k0 * B + c0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = (i * 64 + lane) * VE, k = at / (16 * NT), c = at % (16 * NT);
-            const bool in = flat ? at < STAGE * B : c < nc;   // others read the first ones, and are not stored or not used
-            v.raw[i] = *(const uint4 *)(p + (!in ? 0 : flat ? at : k * (int64_t)B + c));
+            const int at = (i * 64 + lane) * VE, k = at / RS, c = at % RS;
+            __builtin_memcpy(&v.raw[i], p + (c < nc ? k * B + c : 0), 16);
+        }
+    };
+    // the last stages: rows past the last column of W are 0, and a load that would end past x begins
+    // earlier (x has at least VE elements) and is shifted
+    auto load_last = [&](int64_t k0, Stage &v) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = (i * 64 + lane) * VE, k = at / RS, c = at % RS;
+            const bool in = k0 + k < cols && c < nc;
+            const int off = in ? (int)(k0 + k) * B + c0 + c : 0, from = min(off, total - VE);
+            unsigned __int128 w;
+            __builtin_memcpy(&w, x + from, 16);
+            w = in ? w >> (8 * (int)sizeof(X) * (off - from)) : 0;
+            __builtin_memcpy(&v.raw[i], &w, 16);
         }
     };
     auto store_stage = [&](const Stage &v) {
         uint16_t *base = (uint16_t *)mine;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = (i * 64 + lane) * VE;
-            if (flat && at >= STAGE * B) continue;
+            const int at = ((i * 64 + lane) * VE) ^ twist((i * 64 + lane) * VE / RS);
             if constexpr (PARTS == 1) {
-                *(uint4 *)(base + at) = v.raw[i];
+                *(u32x4 *)(base + at) = v.raw[i];
             } else {
-                const uint32_t u[4] = {v.raw[i].x, v.raw[i].y, v.raw[i].z, v.raw[i].w};
                 uint16_t q[4][3];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q4_cut(__uint_as_float(u[j]), q[j]);
+                for (int j = 0; j < 4; ++j) q4_cut(__uint_as_float(v.raw[i][j]), q[j]);
 #pragma unroll
                 for (int t = 0; t < 3; ++t)
-                    *(uint2 *)(base + t * PLANE + at) = make_uint2(q[0][t] | (uint32_t)q[1][t] << 16, q[2][t] | (uint32_t)q[3][t] << 16);
+                    *(u32x2 *)(base + t * PLANE + at) = (u32x2){q[0][t] | (uint32_t)q[1][t] << 16, q[2][t] | (uint32_t)q[3][t] << 16};
             }
         }
     };
-    // a stage element by element: the last one of a row, and arrays that are not aligned
-    auto stage_slowly = [&](int64_t k0) {
+    auto stage_tiny = [&](int64_t k0) {   // of an x of fewer than VE elements
         uint16_t *base = (uint16_t *)mine;
-#pragma unroll 4
-        for (int e = lane; e < STAGE * nc; e += 64) {
-            const int k = e / nc, c = e - k * nc;
+        for (int e = lane; e < PLANE; e += 64) {
+            const int k = e / RS, c = e % RS;
             uint16_t q[3];
-            q4_cut(k0 + k < cols ? x[(k0 + k) * B + c0 + c] : (X)0, q);
+            q4_cut(k0 + k < cols && c < nc ? x[(k0 + k) * B + c] : (X)0, q);
 #pragma unroll
-            for (int t = 0; t < PARTS; ++t) base[t * PLANE + k * RS + c] = q[t];
+            for (int t = 0; t < PARTS; ++t) base[t * PLANE + (e ^ twist(k))] = q[t];
         }
     };
+    int col_at[NT];                   // of the lane's transposing reads
+#pragma unroll
+    for (int t = 0; t < NT; ++t) col_at[t] = (t * 16 + r % 4 * 4) ^ twist(quad * 8 + r / 4 % 2 * 4);
     // the x operand of the step that begins at column k of the stage
     auto operand = [&](int k, int t, int part, int slot) {
         if constexpr (ONE) {
-            return as_bf16x8(*(const uint4 *)(mine + ((slot * PARTS + part) * kQ4Chunk + k + quad * 8) * 2));
-        } else if constexpr (MODE == kTr) {
-            const int row = k + quad * 8 + (r / 4 % 2) * 4 + r / 8, col = t * 16 + r % 4 * 4;
-            unsigned char *p = mine + (part * PLANE + row * RS + col) * 2;
+            return as_bf16x8(*(const u32x4 *)(mine + ((slot * PARTS + part) * kQ4Chunk + k + quad * 8) * 2));
+        } else {
+            const int row = k + quad * 8 + r / 4 % 2 * 4 + r / 8;
+            unsigned char *p = mine + (part * PLANE + row * RS + col_at[t]) * 2;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p + 4 * RS));
-            const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
-            return as_bf16x8(make_uint4(l.x, l.y, h.x, h.y));
-        } else {   // past the last column: what lies there, which no output takes
-            const uint16_t *p = (const uint16_t *)mine + part * PLANE + (k + quad * 8) * RS + t * 16 + r;
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = p[i * RS] | (uint32_t)p[(i + 4) * RS] << 16;
-            return as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+            const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
+            return as_bf16x8((u32x4){l.x, l.y, h.x, h.y});
         }
     };
 
     f32x4 acc[MT][NT], sum[MT][NT], start[NT];
-    const bf16x8 minus = as_bf16x8(make_uint4(0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u));   // -1.5
+    const bf16x8 minus = as_bf16x8((u32x4){0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u});   // -1.5
     const f32x4 zero = {0, 0, 0, 0};
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -233,34 +236,26 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
 #pragma unroll
         for (int s = 0; s < STAGE / 32; ++s) {
             const int step = k / 32 + s;                  // of the chunk
-            bf16x8 xo[NT][PARTS];
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) xo[t][p] = operand(s * 32, t, p, slot);
             const bool first = step % SPG == 0;
+            bf16x8 wo[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const bf16x8 wo = q4_expand(d[m][step]);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (first) sum[m][t] = zero;
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p)
-                        sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo, xo[t][p], sum[m][t], 0, 0, 0);
-                }
-            }
+            for (int m = 0; m < MT; ++m) wo[m] = q4_expand(d[m][step]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 if (first) start[t] = zero;
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p)
-                    start[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus, xo[t][p], start[t], 0, 0, 0);
+                for (int p = 0; p < PARTS; ++p) {
+                    const bf16x8 xo = operand(s * 32, t, p, slot);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo[m], xo, first && p == 0 ? zero : sum[m][t], 0, 0, 0);
+                    start[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus, xo, start[t], 0, 0, 0);
+                }
             }
             if (step % SPG == SPG - 1)
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    const uint2 sc = w.s[m][step / SPG];
+                    const u32x2 sc = w.s[m][step / SPG];
                     const f32x4 f = {bf16_to_f32(sc.x & 0xffffu), __uint_as_float(sc.x & 0xffff0000u),
                                      bf16_to_f32(sc.y & 0xffffu), __uint_as_float(sc.y & 0xffff0000u)};
 #pragma unroll
@@ -303,9 +298,14 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     } else {
         Weights w;
         Stage v;
+        auto load_x = [&](int64_t k0) {
+            if (whole(k0))
+                load_stage(k0, v);
+            else if (k0 < (int64_t)n_chunks * kQ4Chunk && total >= VE)
+                load_last(k0, v);
+        };
         if (wave < n_chunks) load_w(wave, w);
-        auto whole = [&](int64_t k0) { return fast && k0 + STAGE <= cols; };
-        if (whole((int64_t)wave * kQ4Chunk)) load_stage((int64_t)wave * kQ4Chunk, v);
+        load_x((int64_t)wave * kQ4Chunk);
         for (int c = wave; c < n_chunks; c += W) {
             uint32_t d[MT][4];
             const Weights now = w;
@@ -313,14 +313,13 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
             load_w(min(c + W, n_chunks - 1), w);
 #pragma unroll
             for (int k = 0; k < kQ4Chunk; k += STAGE) {
-                const int64_t k0 = (int64_t)c * kQ4Chunk + k, next = k + STAGE < kQ4Chunk ? k0 + STAGE : (int64_t)(c + W) * kQ4Chunk;
                 fence();
-                if (whole(k0))
+                if (total >= VE)
                     store_stage(v);
                 else
-                    stage_slowly(k0);
+                    stage_tiny((int64_t)c * kQ4Chunk + k);
                 fence();
-                if (whole(next)) load_stage(next, v);
+                load_x(k + STAGE < kQ4Chunk ? (int64_t)c * kQ4Chunk + k + STAGE : (int64_t)(c + W) * kQ4Chunk);
                 multiply(d, now, k, 0);
             }
         }
@@ -351,32 +350,27 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     }
 }
 
-template <typename X, int G, int NT, int MT, int MODE>
+template <typename X, int G, int NT, int MT, bool ONE>
 hipError_t q4_run(const Q4Args &a, hipStream_t st) {
-    constexpr int wave = q4_wave_lds<X, NT, MT, MODE>();
+    constexpr int wave = q4_wave_lds<X, NT, MT, ONE>();
     if (kQ4Waves * wave > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT, MODE>,
+        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT, ONE>,
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kQ4Waves * wave);
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)div_up64(a.s.rows, 16 * MT), MODE == kOne ? 1 : (unsigned)((a.batch + 16 * NT - 1) / (16 * NT)));
-    k_q4<X, G, NT, MT, MODE><<<grid, 64 * a.waves, a.waves * wave, st>>>(a);
+    const dim3 grid((unsigned)div_up64(a.s.rows, 16 * MT), ONE ? 1 : (unsigned)((a.batch + 16 * NT - 1) / (16 * NT)));
+    k_q4<X, G, NT, MT, ONE><<<grid, 64 * a.waves, a.waves * wave, st>>>(a);
     return hipGetLastError();
-}
-
-template <typename X, int G, int NT, int MT>
-hipError_t q4_mode(const Q4Args &a, hipStream_t st) {
-    return a.batch % 4 == 0 || a.batch > 16 * NT ? q4_run<X, G, NT, MT, kTr>(a, st) : q4_run<X, G, NT, MT, kEach>(a, st);
 }
 
 template <typename X, int G>
 hipError_t q4_pick(Q4Args a, hipStream_t st) {
     a.waves = std::min(kQ4Waves, (a.s.cols + kQ4Chunk - 1) / kQ4Chunk);
-    if (a.batch == 1) return q4_run<X, G, 1, 1, kOne>(a, st);
-    if (a.batch <= 16) return q4_mode<X, G, 1, 1>(a, st);
-    if (a.batch <= 32) return a.s.rows >= 32 * 256 ? q4_mode<X, G, 2, 2>(a, st) : q4_mode<X, G, 2, 1>(a, st);
-    if (a.s.rows >= 32 * 192) return q4_mode<X, G, 4, 2>(a, st);
-    return q4_mode<X, G, 4, 1>(a, st);
+    if (a.batch == 1) return q4_run<X, G, 1, 1, true>(a, st);
+    if (a.batch <= 16) return q4_run<X, G, 1, 1, false>(a, st);
+    if (a.batch <= 32) return a.s.rows >= 32 * 256 ? q4_run<X, G, 2, 2, false>(a, st) : q4_run<X, G, 2, 1, false>(a, st);
+    if (a.s.rows >= 32 * 192) return q4_run<X, G, 4, 2, false>(a, st);
+    return q4_run<X, G, 4, 1, false>(a, st);
 }
 
 template <typename X>
