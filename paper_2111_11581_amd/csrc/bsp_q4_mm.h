@@ -1,4 +1,5 @@
-// k_q4: y = W x for W in 4 bits with group scales, on matrix instructions.
+// y = W x for W in 4 bits with group scales, on matrix instructions: k_q4_one for one vector, k_q4 for
+// more.
 //
 // Weights go from memory to the operand registers: a lane reads 16 bytes (32 codes) of one row, four
 // lanes 128 columns; two exchanges between the quads (permlane swaps) give every lane the 8 codes of
@@ -6,16 +7,8 @@
 // bits in the mantissa of 1.0: two instructions for two codes.  What this adds, the constant, is
 // taken out again by the sum's start value -1.5 sum(x), which a product with a constant operand gives
 // once per group for all rows: 1 + n / 16 - 1.5 = (n - 8) / 16.  All products are exact and sums fp32;
-// the group's scale multiplies its sum in fp32.
-//
-// Activations pass through LDS, a wave's own part of it, so the main loop has no barrier:
-//  * one vector: 128 elements a chunk, in the order of the codes' pairs; a lane reads 16 bytes.
-//  * more: rows of 16 NT elements of the feature-major array, loaded 16 bytes at a time at whatever
-//    alignment; transposing LDS reads give a lane 4 rows of one column.  Rows of 64 elements are
-//    twisted (32-byte pieces exchanged by bits 2 and 3 of the row), or the 16 rows that one read
-//    touches would lie in the same banks.
-//  * fp32 activations are cut into three bf16 (8 bits each, 24 in all), whose products are added.
-// The waves of a workgroup take 128-column chunks in turn and are joined at the end.
+// the group's scale multiplies its sum in fp32.  fp32 activations are cut into three bf16 (8 bits
+// each, 24 in all), whose products are added.
 #pragma once
 #include "bsp_decode.h"
 #include "bsp_decode_dev.h"
@@ -39,16 +32,7 @@ constexpr int kQ4Waves = 8;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// Columns of x staged at a time, bf16 parts of an element, and a wave's LDS bytes.
-template <typename X> constexpr int q4_parts() { return sizeof(X) == 4 ? 3 : 1; }
-template <typename X, int NT> constexpr int q4_stage() {
-    return sizeof(X) == 4 ? kQ4Chunk / NT : NT == 4 ? 64 : kQ4Chunk;
-}
-template <typename X, int NT, int MT, bool ONE> constexpr int q4_wave_lds() {
-    constexpr int stage = ONE ? 4 * kQ4Chunk * 2 * q4_parts<X>() : q4_stage<X, NT>() * 16 * NT * 2 * q4_parts<X>();
-    constexpr int join = (ONE ? 1 : 16 * NT) * (16 * MT + 4) * 4;
-    return stage > join ? stage : join;
-}
+template <typename X> constexpr int q4_parts() { return sizeof(X) == 4 ? 3 : 1; }   // bf16 parts of an element
 
 // 4 x 4 transpose over quads of lanes and registers.
 __device__ __forceinline__ void q4_transpose(uint32_t *d) {
@@ -64,313 +48,391 @@ __device__ __forceinline__ void q4_transpose(uint32_t *d) {
     }
 }
 
-// Eight codes as 1 + n / 16, in the order of pairs (0, 4), (1, 5), (2, 6), (3, 7).
-__device__ __forceinline__ bf16x8 q4_expand(uint32_t d) {
-    const uint32_t mask = 0x00780078u, one = 0x3f803f80u;
-    return as_bf16x8((u32x4){((d << 3) & mask) | one, ((d >> 1) & mask) | one, ((d >> 5) & mask) | one,
-                                ((d >> 9) & mask) | one});
+// Eight codes as 1 + n / 16, in the order of pairs (0, 4), (1, 5), (2, 6), (3, 7).  The constants are
+// kept in registers (an instruction holds one literal), so that a pair takes a shift and one and-or.
+struct Q4Expand {
+    uint32_t mask = 0x00780078u, one = 0x3f803f80u;
+    __device__ __forceinline__ Q4Expand() { asm("" : "+s"(mask), "+v"(one)); }
+    __device__ __forceinline__ bf16x8 operator()(uint32_t d) const {
+        return as_bf16x8((u32x4){((d << 3) & mask) | one, ((d >> 1) & mask) | one, ((d >> 5) & mask) | one,
+                                 ((d >> 9) & mask) | one});
+    }
+};
+
+// The upper halves of a pair, and what they leave of each.
+__device__ __forceinline__ uint32_t q4_upper(float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float q4_rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+// Pairs of elements as pairs of each of their bf16 parts.  An fp32 is the sum of three bf16, cut, not
+// rounded, so that nothing overflows; of an Inf or NaN the second is NaN.
+__device__ __forceinline__ void q4_cut(float a, float b, uint32_t *p) {
+    p[0] = q4_upper(a, b);
+    a = q4_rest(a), b = q4_rest(b);
+    p[1] = q4_upper(a, b);
+    p[2] = q4_upper(q4_rest(a), q4_rest(b));
+}
+__device__ __forceinline__ void q4_cut(uint16_t a, uint16_t b, uint32_t *p) { p[0] = a | (uint32_t)b << 16; }
+
+// Where a lane finds codes: 32-bit offsets from the workgroup's first row, so that an address is a
+// scalar base and one register.  Past the last row the last one is read again.
+template <int MT> struct Q4Lane {
+    const uint8_t *codes;
+    uint32_t at[MT], quad16, last;
+    const uint16_t *scales[MT];
+    __device__ __forceinline__ Q4Lane(const Q4Args &a, int64_t row0, int r, int quad)
+        : codes(a.codes + row0 * a.s.stride), quad16(quad * 16), last((uint32_t)a.s.stride - 16) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            at[m] = (uint32_t)min((int64_t)16 * m + r, a.s.rows - 1 - row0) * (uint32_t)a.s.stride;
+            scales[m] = a.scales + min(row0 + 16 * m, (int64_t)a.s.rows16 - 16);
+        }
+    }
+};
+
+// Codes and scales of a 128-column chunk of MT row tiles, as a lane holds them.
+template <int G, int MT> struct Q4Weights {
+    static constexpr int GPC = kQ4Chunk / G;   // groups of a chunk
+    u32x4 w[MT];
+    u32x2 s[MT][GPC];
+
+    // Past a row's end its last 16 bytes are read again, whose x is 0; past the last group the last.
+    __device__ __forceinline__ void load(const Q4Args &a, const Q4Lane<MT> &l, int chunk) {
+        const uint32_t col = min((uint32_t)chunk * 64 + l.quad16, l.last);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            w[m] = *(const u32x4 *)(l.codes + (l.at[m] + col));
+#pragma unroll
+            for (int g = 0; g < GPC; ++g)
+                s[m][g] = *(const u32x2 *)((const uint8_t *)(l.scales[m] + (int64_t)min(chunk * GPC + g, a.s.n_groups - 1) * a.s.rows16) +
+                                           (l.quad16 >> 1));
+        }
+    }
+    __device__ __forceinline__ void codes(int m, uint32_t *d) const {
+        d[0] = w[m].x, d[1] = w[m].y, d[2] = w[m].z, d[3] = w[m].w;
+        q4_transpose(d);
+    }
+    __device__ __forceinline__ f32x4 scale(int m, int g) const {
+        return (f32x4){bf16_to_f32(s[m][g].x & 0xffffu), __uint_as_float(s[m][g].x & 0xffff0000u),
+                       bf16_to_f32(s[m][g].y & 0xffffu), __uint_as_float(s[m][g].y & 0xffff0000u)};
+    }
+};
+
+// The products of `steps` 32-column steps of one group, from step `first` of a chunk: x operands xo of
+// NT vector tiles, codes d of the MT row tiles.
+template <int G, int MT, int NT, int PARTS, int US>
+__device__ __forceinline__ void q4_unit(const Q4Expand &expand, const Q4Weights<G, MT> &w, const uint32_t (*d)[4], int first,
+                                        const bf16x8 (*xo)[NT][PARTS], f32x4 (*acc)[NT]) {
+    const bf16x8 minus = as_bf16x8((u32x4){0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u});   // -1.5
+    f32x4 start[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        start[t] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < US; ++s)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+                start[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus, xo[s][t][p], start[t], 0, 0, 0);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        f32x4 sum[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[t] = start[t];
+#pragma unroll
+        for (int s = 0; s < US; ++s) {
+            const bf16x8 wo = expand(d[m][first + s]);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo, xo[s][t][p], sum[t], 0, 0, 0);
+        }
+        const f32x4 f = w.scale(m, first / (G / 32));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[m][t] += f * sum[t];
+        if (MT > 1) __builtin_amdgcn_sched_barrier(0);   // or all tiles' sums are begun at once, and spill
+    }
 }
 
-// The three bf16 whose sum an fp32 is (cut, not rounded, so that nothing overflows); Inf and NaN are
-// their first part alone.
-__device__ __forceinline__ void q4_cut(float x, uint16_t *p) {
-    const uint32_t u = __float_as_uint(x);
-    const bool finite = (u & 0x7f800000u) != 0x7f800000u;
-    const float rest = x - __uint_as_float(u & 0xffff0000u);
-    const uint32_t v = __float_as_uint(rest);
-    const float last = rest - __uint_as_float(v & 0xffff0000u);
-    p[0] = (uint16_t)((u >> 16) | ((!finite && (u & 0x007fffffu)) ? 0x40u : 0u));
-    p[1] = finite ? (uint16_t)(v >> 16) : (uint16_t)0;
-    p[2] = finite ? (uint16_t)(__float_as_uint(last) >> 16) : (uint16_t)0;
+// Sum over the waves that share rows, bias, ReLU and the store of one output.
+__device__ __forceinline__ void q4_store(const Q4Args &a, float v, int64_t row, int col) {
+    v = v * 16.f + (a.bias ? a.bias[row] : 0.f);
+    if (a.relu && v < 0.f) v = 0.f;
+    const int64_t at = row * a.batch + col;
+    if (a.out_bf16)
+        ((uint16_t *)a.y)[at] = f32_to_bf16(v);
+    else
+        ((float *)a.y)[at] = v;
 }
-__device__ __forceinline__ void q4_cut(uint16_t x, uint16_t *p) { p[0] = x; }
 
-// A workgroup: 16 MT rows, 16 NT vectors (ONE: one vector).
-template <typename X, int G, int NT, int MT, bool ONE>
+// One vector.  A workgroup computes 16 rows; its waves take chunks in turn, four at a time in flight,
+// and are joined at the end.  A wave keeps x of its chunks in its own part of LDS, in the order of the
+// codes' pairs, and a lane reads the 16 bytes of its 8 columns (all 16 columns of the operand are the
+// vector).
+template <typename X, int G>
+__global__ __launch_bounds__(64 * kQ4Waves, 4) void k_q4_one(Q4Args a) {
+    constexpr int PARTS = q4_parts<X>(), PF = 4, SPG = G / 32;
+    __shared__ __attribute__((aligned(16))) uint16_t s_x[kQ4Waves][PF][PARTS][kQ4Chunk];
+    __shared__ f32x4 s_o[kQ4Waves][4];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, quad = lane / 16;
+    const int W = a.waves, cols = a.s.cols;
+    const int64_t row0 = (int64_t)blockIdx.x * 16;
+    const Q4Lane<1> at(a, row0, r, quad);
+    const Q4Expand expand;
+    const X *x = (const X *)a.x;
+    const int n_chunks = (cols + kQ4Chunk - 1) / kQ4Chunk;
+    f32x4 acc[1][1] = {{{0, 0, 0, 0}}};
+    Q4Weights<G, 1> w[PF];
+    X v[PF][2];
+    for (int c = wave; c < n_chunks; c += PF * W) {
+#pragma unroll
+        for (int i = 0; i < PF; ++i) {
+            const uint32_t k = (uint32_t)(c + i * W) * kQ4Chunk + lane;   // elements lane and lane + 64 of the chunk
+            v[i][0] = x[min(k, (uint32_t)cols - 1)], v[i][1] = x[min(k + 64, (uint32_t)cols - 1)];
+            w[i].load(a, at, min(c + i * W, n_chunks - 1));
+        }
+        // a wave's LDS operations stay in order; the fences hold the compiler to it
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < PF; ++i) {
+            const int k = (c + i * W) * kQ4Chunk + lane;
+            uint32_t p[3];
+            q4_cut(k < cols ? v[i][0] : (X)0, k + 64 < cols ? v[i][1] : (X)0, p);
+#pragma unroll
+            for (int t = 0; t < PARTS; ++t) {   // element k of 8 goes to place 2 (k % 4) + k / 4
+                uint16_t *to = &s_x[wave][i][t][lane / 8 * 8 + lane % 4 * 2 + lane / 4 % 2];
+                to[0] = (uint16_t)p[t], to[64] = (uint16_t)(p[t] >> 16);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < PF; ++i) {
+            uint32_t d[1][4];
+            w[i].codes(0, d[0]);
+#pragma unroll
+            for (int step = 0; step < 4; step += SPG) {
+                bf16x8 xo[SPG][1][PARTS];
+#pragma unroll
+                for (int s = 0; s < SPG; ++s)
+#pragma unroll
+                    for (int t = 0; t < PARTS; ++t)
+                        xo[s][0][t] = as_bf16x8(*(const u32x4 *)&s_x[wave][i][t][(step + s) * 32 + quad * 8]);
+                q4_unit<G, 1, 1, PARTS, SPG>(expand, w[i], d, step, xo, acc);
+            }
+        }
+    }
+    if (r == 0) s_o[wave][quad] = acc[0][0];
+    __syncthreads();
+    if (threadIdx.x < 16 && row0 + threadIdx.x < a.s.rows) {
+        float v = 0.f;
+        for (int k = 0; k < W; ++k) v += ((const float *)s_o[k])[threadIdx.x];
+        q4_store(a, v, row0 + threadIdx.x, 0);
+    }
+}
+
+// More vectors.  A workgroup computes 16 MT rows for 16 NT vectors; its waves take chunks in turn and
+// are joined at the end.  A wave keeps STAGE columns of x at a time in its own part of LDS, so that
+// the main loop has no barrier; the next stage's x is asked for before weights, which come from
+// farther, so that waiting for x leaves weights of two chunks in flight.
+//  * Rows of x are loaded 16 bytes at a time at whatever alignment; what the last load of a row takes
+//    past the vectors goes to columns that no output has.
+//  * Transposing LDS reads give a lane 4 rows of one column.  Rows of 64 elements are twisted (32-byte
+//    pieces exchanged by bits 2 and 3 of the row): the rows that one read touches lay in the same banks.
+template <typename X, int NT> constexpr int q4_stage() { return sizeof(X) == 4 ? kQ4Chunk / NT : NT == 4 ? 64 : kQ4Chunk; }
+template <typename X, int NT, int MT> constexpr int q4_wave_lds() {
+    constexpr int stage = q4_stage<X, NT>() * 16 * NT * 2 * q4_parts<X>(), join = 16 * NT * (16 * MT + 4) * 4;
+    return stage > join ? stage : join;
+}
+template <typename X, int G, int NT, int MT>
 __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
-    constexpr int PARTS = q4_parts<X>(), GPC = kQ4Chunk / G, SPG = G / 32;   // groups of a chunk, steps of a group
-    constexpr int STAGE = ONE ? kQ4Chunk : q4_stage<X, NT>();
-    constexpr int PF = ONE ? 4 : 1;                                           // chunks in flight ahead
-    constexpr int VE = 16 / sizeof(X);                                        // elements of a 16-byte load
-    constexpr int NV = ONE ? 1 : STAGE * 16 * NT / VE / 64;                   // such loads of a lane and stage
-    constexpr int WLDS = q4_wave_lds<X, NT, MT, ONE>();
+    constexpr int PARTS = q4_parts<X>(), STAGE = q4_stage<X, NT>(), WLDS = q4_wave_lds<X, NT, MT>();
+    constexpr int RS = 16 * NT, PLANE = STAGE * RS, VE = 16 / sizeof(X), NV = PLANE / VE / 64;   // loads of a lane and stage
+    constexpr int US = G == 32 || STAGE == 32 || NT * PARTS > 4 ? 1 : 2; // steps of a unit: their x operands are held in registers
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, quad = lane / 16;
-    const int rows = a.s.rows, cols = a.s.cols, B = a.batch, W = a.waves;
+    const int cols = a.s.cols, B = a.batch, W = a.waves, total = cols * B;
     const int64_t row0 = (int64_t)blockIdx.x * (16 * MT);
-    unsigned char *mine = lds + wave * WLDS;
-    const X *x = (const X *)a.x;
-
-    const int c0 = ONE ? 0 : blockIdx.y * (16 * NT), nc = ONE ? 1 : min(16 * NT, B - c0);   // its vectors
-
-    const uint8_t *wp[MT];
-    const uint16_t *sp = a.scales + row0 + quad * 4;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) wp[m] = a.codes + min(row0 + 16 * m + r, (int64_t)rows - 1) * a.s.stride + quad * 16;
+    const Q4Lane<MT> at(a, row0, r, quad);
+    const Q4Expand expand;
+    const int c0 = blockIdx.y * RS, nc = min(RS, B - c0);
+    uint16_t *mine = (uint16_t *)(lds + wave * WLDS);
     const int n_chunks = (cols + kQ4Chunk - 1) / kQ4Chunk;
-
-    struct Weights {
-        u32x4 w[MT];
-        u32x2 s[MT][GPC];
-    };
-    auto load_w = [&](int c, Weights &w) {   // past a row's end: its last 16 bytes, whose x is 0
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int64_t at = min((int64_t)c * 64, a.s.stride - 16 - quad * 16);
-            w.w[m] = *(const u32x4 *)(wp[m] + at);
-#pragma unroll
-            for (int g = 0; g < GPC; ++g) {
-                const int64_t group = min(c * GPC + g, a.s.n_groups - 1);
-                w.s[m][g] = *(const u32x2 *)(sp + group * a.s.rows16 + min((int64_t)16 * m, a.s.rows16 - 16 - row0));
-            }
-        }
-    };
-    // one vector: elements 2 lane and 2 lane + 1 of a chunk, those past `cols` 0, each cut into its
-    // parts, to their places: element k of 8 goes to place 2 (k % 4) + k / 4
-    struct Pair {
-        X e[2];
-    };
-    auto load_pair = [&](int64_t k0) {
-        Pair p;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) p.e[i] = k0 + 2 * lane + i < cols ? x[k0 + 2 * lane + i] : (X)0;
-        return p;
-    };
-    auto store_pair = [&](const Pair &v, int slot) {
-        uint16_t *at = (uint16_t *)mine + slot * kQ4Chunk * PARTS + (lane / 4) * 8 + (lane % 4 / 2) + (lane % 2) * 4;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint16_t p[3];
-            q4_cut(v.e[i], p);
-#pragma unroll
-            for (int t = 0; t < PARTS; ++t) at[t * kQ4Chunk + 2 * i] = p[t];
-        }
-    };
-    // more: rows of a stage, 16 bytes at a time.  What a row's last load takes past the vectors goes to
-    // columns that no output has.
-    constexpr int RS = 16 * NT, PLANE = STAGE * RS;
-    struct Stage {
-        u32x4 raw[NV];
-    };
     auto twist = [](int row) { return NT == 4 ? (row >> 2 & 3) << 4 : 0; };   // in elements
-    const int total = cols * B;
-    auto whole = [&](int64_t k0) {   // a stage whose loads end within x
-        return k0 + STAGE <= cols && (k0 + STAGE - 1) * B + c0 + (nc + VE - 1) / VE * VE <= total;
+
+    // The lane's loads: columns my_k + i * KI of a stage, vectors from my_c on.  They are clamped to x
+    // rather than left out (a branch around them would wait for them), and what lies past the end is
+    // mended before it is stored: columns past the last are 0, a load that would end past x has begun
+    // earlier and is shifted.
+    constexpr int KI = 64 * VE / RS;
+    const int my_k = lane * VE / RS, my_c = lane * VE % RS, base = my_k * B + c0 + (my_c < nc ? my_c : 0);
+    const bool tiny = total < VE;     // not one load: read element by element when stored
+    const uint8_t *from = tiny ? a.codes : (const uint8_t *)a.x;
+    const uint32_t last = tiny ? 0 : (uint32_t)(total - VE) * (uint32_t)sizeof(X), lane_at = (uint32_t)base * (uint32_t)sizeof(X);
+    u32x4 v[NV];
+    auto load = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            __builtin_memcpy(&v[i], from + min(lane_at + (uint32_t)(k0 + i * KI) * (uint32_t)B * (uint32_t)sizeof(X), last), 16);
+        asm volatile("" ::: "memory");   // the loads stay here, a stage ahead of their use
     };
-    auto load_stage = [&](int64_t k0, Stage &v) {
-        const X *p = x + k0 * B + c0;
+    auto mend = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = (i * 64 + lane) * VE, k = at / RS, c = at % RS;
-            __builtin_memcpy(&v.raw[i], p + (c < nc ? k * B + c : 0), 16);
-        }
-    };
-    // the last stages: rows past the last column of W are 0, and a load that would end past x begins
-    // earlier (x has at least VE elements) and is shifted
-    auto load_last = [&](int64_t k0, Stage &v) {
+            const int k = k0 + my_k + i * KI;
+            const bool in = k < cols && my_c < nc;
+            if (tiny) {
+                alignas(16) X e[VE];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = (i * 64 + lane) * VE, k = at / RS, c = at % RS;
-            const bool in = k0 + k < cols && c < nc;
-            const int off = in ? (int)(k0 + k) * B + c0 + c : 0, from = min(off, total - VE);
-            unsigned __int128 w;
-            __builtin_memcpy(&w, x + from, 16);
-            w = in ? w >> (8 * (int)sizeof(X) * (off - from)) : 0;
-            __builtin_memcpy(&v.raw[i], &w, 16);
-        }
-    };
-    auto store_stage = [&](const Stage &v) {
-        uint16_t *base = (uint16_t *)mine;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = ((i * 64 + lane) * VE) ^ twist((i * 64 + lane) * VE / RS);
-            if constexpr (PARTS == 1) {
-                *(u32x4 *)(base + at) = v.raw[i];
+                for (int j = 0; j < VE; ++j) e[j] = in && my_c + j < nc ? ((const X *)a.x)[k * B + c0 + my_c + j] : (X)0;
+                __builtin_memcpy(&v[i], e, 16);
             } else {
-                uint16_t q[4][3];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) q4_cut(__uint_as_float(v.raw[i][j]), q[j]);
-#pragma unroll
-                for (int t = 0; t < 3; ++t)
-                    *(u32x2 *)(base + t * PLANE + at) = (u32x2){q[0][t] | (uint32_t)q[1][t] << 16, q[2][t] | (uint32_t)q[3][t] << 16};
+                const uint32_t off = lane_at + (uint32_t)(k0 + i * KI) * (uint32_t)B * (uint32_t)sizeof(X);
+                unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v[i]);
+                w = in ? w >> (8 * (off - min(off, last))) : 0;
+                v[i] = __builtin_bit_cast(u32x4, w);
             }
         }
     };
-    auto stage_tiny = [&](int64_t k0) {   // of an x of fewer than VE elements
-        uint16_t *base = (uint16_t *)mine;
-        for (int e = lane; e < PLANE; e += 64) {
-            const int k = e / RS, c = e % RS;
-            uint16_t q[3];
-            q4_cut(k0 + k < cols && c < nc ? x[(k0 + k) * B + c] : (X)0, q);
+    auto store = [&](int k0) __attribute__((always_inline)) {
+        if (k0 + STAGE > cols || (int64_t)(k0 + STAGE - 1) * B + c0 + (nc + VE - 1) / VE * VE > total) mend(k0);
 #pragma unroll
-            for (int t = 0; t < PARTS; ++t) base[t * PLANE + (e ^ twist(k))] = q[t];
-        }
-    };
-    int col_at[NT];                   // of the lane's transposing reads
+        for (int i = 0; i < NV; ++i) {
+            const int k = my_k + i * (64 * VE / RS);
+            uint16_t *p = mine + k * RS + (my_c ^ twist(k));
+            if constexpr (PARTS == 1) {
+                *(u32x4 *)p = v[i];
+            } else {
+                uint32_t q[2][3];
+                q4_cut(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]), q[0]);
+                q4_cut(__uint_as_float(v[i][2]), __uint_as_float(v[i][3]), q[1]);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) col_at[t] = (t * 16 + r % 4 * 4) ^ twist(quad * 8 + r / 4 % 2 * 4);
-    // the x operand of the step that begins at column k of the stage
-    auto operand = [&](int k, int t, int part, int slot) {
-        if constexpr (ONE) {
-            return as_bf16x8(*(const u32x4 *)(mine + ((slot * PARTS + part) * kQ4Chunk + k + quad * 8) * 2));
-        } else {
-            const int row = k + quad * 8 + r / 4 % 2 * 4 + r / 8;
-            unsigned char *p = mine + (part * PLANE + row * RS + col_at[t]) * 2;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p + 4 * RS));
-            const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
-            return as_bf16x8((u32x4){l.x, l.y, h.x, h.y});
-        }
-    };
-
-    f32x4 acc[MT][NT], sum[MT][NT], start[NT];
-    const bf16x8 minus = as_bf16x8((u32x4){0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u, 0xbfc0bfc0u});   // -1.5
-    const f32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[m][t] = zero;
-
-    // the steps of columns [k, k + STAGE) of a chunk, whose codes are transposed in d
-    auto multiply = [&](const uint32_t (*d)[4], const Weights &w, int k, int slot) {
-#pragma unroll
-        for (int s = 0; s < STAGE / 32; ++s) {
-            const int step = k / 32 + s;                  // of the chunk
-            const bool first = step % SPG == 0;
-            bf16x8 wo[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) wo[m] = q4_expand(d[m][step]);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (first) start[t] = zero;
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    const bf16x8 xo = operand(s * 32, t, p, slot);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-                        sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo[m], xo, first && p == 0 ? zero : sum[m][t], 0, 0, 0);
-                    start[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus, xo, start[t], 0, 0, 0);
-                }
+                for (int t = 0; t < 3; ++t) *(u32x2 *)(p + t * PLANE) = (u32x2){q[0][t], q[1][t]};
             }
-            if (step % SPG == SPG - 1)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const u32x2 sc = w.s[m][step / SPG];
-                    const f32x4 f = {bf16_to_f32(sc.x & 0xffffu), __uint_as_float(sc.x & 0xffff0000u),
-                                     bf16_to_f32(sc.y & 0xffffu), __uint_as_float(sc.y & 0xffff0000u)};
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[m][t] += f * (sum[m][t] + start[t]);
-                }
         }
     };
-    auto transpose = [&](const Weights &w, uint32_t (*d)[4]) {
+    const int lane_row = quad * 8 + r / 4 % 2 * 4 + r / 8;   // of the lane's transposing reads
+    int place[NT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            d[m][0] = w.w[m].x, d[m][1] = w.w[m].y, d[m][2] = w.w[m].z, d[m][3] = w.w[m].w;
-            q4_transpose(d[m]);
-        }
+    for (int t = 0; t < NT; ++t) place[t] = lane_row * RS + ((t * 16 + r % 4 * 4) ^ twist(lane_row));
+    auto operand = [&](int k, int t, int part) __attribute__((always_inline)) {
+        const uint16_t *p = mine + part * PLANE + k * RS + place[t];
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p + 2 * RS));
+        const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
+        return as_bf16x8((u32x4){l.x, l.y, h.x, h.y});
     };
-    auto fence = [&]() {   // a wave's LDS operations stay in order; the compiler's too
+    auto fence = [&]() __attribute__((always_inline)) {   // a wave's LDS operations stay in order; the compiler's too
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
 
-    if constexpr (ONE) {
-        Weights w[PF];
-        Pair v[PF];
-        for (int c = wave; c < n_chunks; c += PF * W) {
+    f32x4 acc[MT][NT];
 #pragma unroll
-            for (int i = 0; i < PF; ++i) {
-                load_w(c + i * W, w[i]);
-                v[i] = load_pair((int64_t)(c + i * W) * kQ4Chunk);
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[m][t] = (f32x4){0, 0, 0, 0};
+    Q4Weights<G, MT> ring[2];
+    load(wave * kQ4Chunk);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ring[i].load(a, at, min(wave + i * W, n_chunks - 1));
+    asm volatile("" ::: "memory");
+    auto chunk = [&](int c, Q4Weights<G, MT> &w) __attribute__((always_inline)) {
+        uint32_t d[MT][4];
+        const Q4Weights<G, MT> now = w;
+#pragma unroll
+        for (int k = 0; k < kQ4Chunk; k += STAGE) {
+            fence();
+            store(c * kQ4Chunk + k);
+            fence();
+            load(k + STAGE < kQ4Chunk ? c * kQ4Chunk + k + STAGE : (c + W) * kQ4Chunk);
+            if (k == 0) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) now.codes(m, d[m]);
+                w.load(a, at, min(c + 2 * W, n_chunks - 1));
+                asm volatile("" ::: "memory");
             }
-            fence();
 #pragma unroll
-            for (int i = 0; i < PF; ++i) store_pair(v[i], i);
-            fence();
+            for (int u = 0; u < STAGE / 32; u += US) {
+                bf16x8 xo[US][NT][PARTS];
 #pragma unroll
-            for (int i = 0; i < PF; ++i) {
-                uint32_t d[MT][4];
-                transpose(w[i], d);
-                multiply(d, w[i], 0, i);
+                for (int s = 0; s < US; ++s)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) xo[s][t][p] = operand((u + s) * 32, t, p);
+                q4_unit<G, MT, NT, PARTS, US>(expand, now, d, k / 32 + u, xo, acc);
             }
         }
-    } else {
-        Weights w;
-        Stage v;
-        auto load_x = [&](int64_t k0) {
-            if (whole(k0))
-                load_stage(k0, v);
-            else if (k0 < (int64_t)n_chunks * kQ4Chunk && total >= VE)
-                load_last(k0, v);
-        };
-        if (wave < n_chunks) load_w(wave, w);
-        load_x((int64_t)wave * kQ4Chunk);
-        for (int c = wave; c < n_chunks; c += W) {
-            uint32_t d[MT][4];
-            const Weights now = w;
-            transpose(now, d);
-            load_w(min(c + W, n_chunks - 1), w);
-#pragma unroll
-            for (int k = 0; k < kQ4Chunk; k += STAGE) {
-                fence();
-                if (total >= VE)
-                    store_stage(v);
-                else
-                    stage_tiny((int64_t)c * kQ4Chunk + k);
-                fence();
-                load_x(k + STAGE < kQ4Chunk ? (int64_t)c * kQ4Chunk + k + STAGE : (int64_t)(c + W) * kQ4Chunk);
-                multiply(d, now, k, 0);
-            }
-        }
+    };
+    for (int c = wave; c < n_chunks;) {
+        chunk(c, ring[0]);
+        if ((c += W) >= n_chunks) break;
+        chunk(c, ring[1]);
+        c += W;
     }
 
     // join the waves: [vector][row] of each in LDS
     constexpr int RW = 16 * MT + 4;
-    float *o = (float *)mine;
     fence();
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-        if (t * 16 + r < nc)
 #pragma unroll
-            for (int m = 0; m < MT; ++m) *(f32x4 *)(o + (t * 16 + r) * RW + m * 16 + quad * 4) = acc[m][t];
+        for (int m = 0; m < MT; ++m) *(f32x4 *)((float *)mine + (t * 16 + r) * RW + m * 16 + quad * 4) = acc[m][t];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * MT * (ONE ? 1 : 16 * NT); i += 64 * W) {
-        const int col = ONE ? 0 : i % (16 * NT), row = ONE ? i : i / (16 * NT);
-        if (col >= nc || row0 + row >= rows) continue;
-        float v = 0.f;
-        for (int k = 0; k < W; ++k) v += ((const float *)(lds + k * WLDS))[col * RW + row];
-        v = v * 16.f + (a.bias ? a.bias[row0 + row] : 0.f);
-        if (a.relu && v < 0.f) v = 0.f;
-        const int64_t at = (row0 + row) * B + c0 + col;
-        if (a.out_bf16)
-            ((uint16_t *)a.y)[at] = f32_to_bf16(v);
-        else
-            ((float *)a.y)[at] = v;
+    for (int i = threadIdx.x; i < 16 * MT * RS; i += 64 * W) {
+        const int col = i % RS, row = i / RS;
+        if (col >= nc || row0 + row >= a.s.rows) continue;
+        float sum = 0.f;
+        for (int k = 0; k < W; ++k) sum += ((const float *)(lds + k * WLDS))[col * RW + row];
+        q4_store(a, sum, row0 + row, c0 + col);
     }
 }
 
-template <typename X, int G, int NT, int MT, bool ONE>
-hipError_t q4_run(const Q4Args &a, hipStream_t st) {
-    constexpr int wave = q4_wave_lds<X, NT, MT, ONE>();
-    if (kQ4Waves * wave > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT, ONE>,
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, kQ4Waves * wave);
+template <typename X, int G, int NT, int MT>
+hipError_t q4_run(Q4Args a, hipStream_t st) {
+    constexpr int lds = q4_wave_lds<X, NT, MT>();
+    if (kQ4Waves * lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 kQ4Waves * lds);
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)div_up64(a.s.rows, 16 * MT), ONE ? 1 : (unsigned)((a.batch + 16 * NT - 1) / (16 * NT)));
-    k_q4<X, G, NT, MT, ONE><<<grid, 64 * a.waves, a.waves * wave, st>>>(a);
+    const dim3 grid((unsigned)div_up64(a.s.rows, 16 * MT), (unsigned)((a.batch + 16 * NT - 1) / (16 * NT)));
+    k_q4<X, G, NT, MT><<<grid, 64 * a.waves, a.waves * lds, st>>>(a);
     return hipGetLastError();
 }
 
+// Workgroup shapes.  One vector: a wave has four chunks in flight, so no more waves than fill them
+// (1024 x 1024 4.1 us with 8 waves, 3.1 with 2).  More: with few row tiles, as many workgroups as make
+// one for each CU (1024 x 1024, 64 vectors: 4.2 us in 16-vector tiles, 5.3 in one of 64; 4096 x 4096
+// 23 and 10.5); with many, two row tiles a wave and four waves, so that each reads x half as often and a
+// CU holds two workgroups (16384 x 4096, 64 vectors 37 -> 24 us, 16 vectors 15.7 -> 12.4).
 template <typename X, int G>
 hipError_t q4_pick(Q4Args a, hipStream_t st) {
-    a.waves = std::min(kQ4Waves, (a.s.cols + kQ4Chunk - 1) / kQ4Chunk);
-    if (a.batch == 1) return q4_run<X, G, 1, 1, true>(a, st);
-    if (a.batch <= 16) return q4_run<X, G, 1, 1, false>(a, st);
-    if (a.batch <= 32) return a.s.rows >= 32 * 256 ? q4_run<X, G, 2, 2, false>(a, st) : q4_run<X, G, 2, 1, false>(a, st);
-    if (a.s.rows >= 32 * 192) return q4_run<X, G, 4, 2, false>(a, st);
-    return q4_run<X, G, 4, 1, false>(a, st);
+    const int n_chunks = (a.s.cols + kQ4Chunk - 1) / kQ4Chunk;
+    const int64_t tiles = a.s.rows16 / 16;
+    if (a.batch == 1) {
+        a.waves = std::min(kQ4Waves, (n_chunks + 3) / 4);
+        k_q4_one<X, G><<<(unsigned)tiles, 64 * a.waves, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    a.waves = std::min(kQ4Waves, n_chunks);
+    auto groups = [&](int vectors) { return tiles * ((a.batch + vectors - 1) / vectors); };
+    if constexpr (sizeof(X) == 4) {   // three operands for each: no more than 16 vectors fit the registers
+        const int64_t n = groups(16);
+        if (n <= 256) return q4_run<X, G, 1, 1>(a, st);
+        if (n <= 512) return q4_run<X, G, 1, 2>(a, st);
+        if (n >= 4096) a.waves = std::min(2, n_chunks);   // 16384 x 4096, 61 vectors: 73 us with 8 waves, 53 with 2
+        return q4_run<X, G, 1, 4>(a, st);
+    } else {
+        const int nt = a.batch <= 16 || groups(16) <= 256 ? 1 : a.batch <= 32 || groups(32) <= 256 ? 2 : 4;
+        const bool many = groups(16 * nt) >= (nt == 1 ? 1024 : 512);
+        if (many) a.waves = std::min(4, n_chunks);
+        if (nt == 1) return many ? q4_run<X, G, 1, 2>(a, st) : q4_run<X, G, 1, 1>(a, st);
+        if (nt == 2) return many ? q4_run<X, G, 2, 2>(a, st) : q4_run<X, G, 2, 1>(a, st);
+        return many ? q4_run<X, G, 4, 2>(a, st) : q4_run<X, G, 4, 1>(a, st);
+    }
 }
 
 template <typename X>
