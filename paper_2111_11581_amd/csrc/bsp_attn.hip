@@ -25,7 +25,7 @@ namespace bsp {
 
 namespace {
 
-constexpr int kWaves = 4, kTile = 512;   // waves of a workgroup; tokens whose places it keeps in LDS
+constexpr int kWaves = 4, kTile = 1024;   // waves of a workgroup; tokens whose places it keeps in LDS
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Page of token t of a sequence, or -1 where the entry holds nothing.
@@ -55,18 +55,73 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
     }
 }
 
-// The tokens of a sequence, and how many parts of `chunk` they make (1 where there are none).
+__device__ __forceinline__ int row_of(const AttnArgs &a, int b) { return a.rows ? a.rows[b] : b; }
+__device__ __forceinline__ int len_of(const AttnArgs &a, int row) {
+    const int len = (unsigned)row < (unsigned)a.seqs ? a.lens[row] : 0;
+    return max(0, (int)min((int64_t)len, (int64_t)a.width * a.c.page_size));
+}
+// The tokens that a sequence attends to, and their number in blocks of 32.
+constexpr int kBlock = 32;
 struct Span {
-    int first, len, parts;
+    int row, first, len, blocks;
 };
-__device__ __forceinline__ Span span_of(const AttnArgs &a, int b, int *row) {
-    *row = a.rows ? a.rows[b] : b;
+__device__ __forceinline__ Span span_of(const AttnArgs &a, int row, int len) {
     Span s;
-    s.len = (unsigned)*row < (unsigned)a.seqs ? a.lens[*row] : 0;
-    s.len = max(0, (int)min((int64_t)s.len, (int64_t)a.width * a.c.page_size));
+    s.row = row, s.len = len;
     s.first = a.window && s.len > a.window ? s.len - a.window : 0;
-    s.parts = max(1, (int)(((unsigned)(s.len - s.first) + a.chunk - 1) / a.chunk));
+    s.blocks = (int)(((unsigned)(s.len - s.first) + kBlock - 1) / kBlock);
     return s;
+}
+
+// How the work is shared out, when sequences are split.  A unit is a sequence's tokens for one head
+// group.  All units in a row, each as long as its blocks and kCost more (what beginning and ending a
+// segment takes: 5 of a segment's 19 us where 17 blocks take 13; without it the workgroups that get
+// many short units take twice as long), are cut into equal shares, one for each workgroup, whatever
+// the lengths are.  Share g and unit u meet in at most one segment, number g + u (one of the two grows
+// from each segment to the next).  Every workgroup works the cuts out for itself from the lengths:
+// s_before[b] is the length of a head group's units before sequence b, s_len[b] its tokens.
+constexpr int kCost = 8, kMinShare = kCost + 8;   // 8 blocks are two steps of each wave
+constexpr int kMostSeqs = 1024, kMostShares = 512;
+__device__ __forceinline__ int length_of(const Span &s) { return s.blocks ? s.blocks + kCost : 0; }
+__device__ __forceinline__ void count_blocks(const AttnArgs &a, int32_t *s_before, int32_t *s_len) {
+    constexpr int PER = kMostSeqs / 256;
+    __shared__ int s_wave[4];
+    const int t = threadIdx.x, lane = t % 64;
+    int mine[PER], sum = 0;
+    const int per = (a.batch + 255) / 256;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        mine[i] = 0;
+        if (i < per && t * per + i < a.batch) {
+            const int len = len_of(a, row_of(a, t * per + i));
+            s_len[t * per + i] = len;
+            mine[i] = length_of(span_of(a, 0, len));
+        }
+        sum += mine[i];
+    }
+    int upto = sum;
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) s_wave[t / 64] = upto;
+    __syncthreads();
+    int before = upto - sum;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) before += w < t / 64 ? s_wave[w] : 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (i < per && t * per + i <= a.batch) {
+            s_before[t * per + i] = before;
+            before += mine[i];
+        }
+    if (t == 255) s_before[a.batch] = before;   // the last thread's own end is everyone's
+    __syncthreads();
+}
+// Length of a share.
+__device__ __forceinline__ int64_t share_of(const AttnArgs &a, const int32_t *s_before, int64_t *total) {
+    *total = (int64_t)uni(s_before[a.batch]) * (a.c.kv_heads * a.head_groups);
+    return max((int64_t)kMinShare, (*total + a.shares - 1) / a.shares);
 }
 
 // What a wave loads and multiplies in one step, for head_dim up to DP.
@@ -75,35 +130,29 @@ template <typename E, int DP> struct Step;
 template <int DP> struct Step<uint16_t, DP> {
     static constexpr int TOK = 32, NK = DP / 32, VW = DP == 64 ? 4 : 8, NV = DP / (16 * VW);
     typedef uint32_t VRaw __attribute__((ext_vector_type(VW / 2)));
-    uint4 q[NK];
-    uint4 k[2][NK];
+    u32x4 q[NK];
+    u32x4 k[2][NK];
     VRaw v[8][NV];
 
-    __device__ __forceinline__ void load_q(const uint16_t *p, int64_t stride, bool on, int quad, int D) {
+    __device__ __forceinline__ void load_q(const uint16_t *row, int quad) {
 #pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = c * 32 + quad * 8 + 2 * i;
-                w[i] = on && d < D ? p[d * stride] | (uint32_t)p[(d + 1) * stride] << 16 : 0u;
-            }
-            q[c] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int c = 0; c < NK; ++c) q[c] = *(const u32x4 *)(row + c * 32 + quad * 8);
     }
-    // ko: places of tokens l % 16 and 16 + l % 16; vo: of tokens 4 quad + i and 16 + 4 quad + i
-    template <bool FULL>
-    __device__ __forceinline__ void load(const uint16_t *keys, const uint16_t *values, const int64_t *ko, const int64_t *vo,
-                                         int quad, int r, int D) {
+    // places of tokens r and 16 + r
+    template <bool FULL> __device__ __forceinline__ void load_k(const uint16_t *keys, const int64_t *ko, int quad, int D) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
+                if (!FULL && DP < 256 && c * 32 >= D) break;
                 const int d = c * 32 + quad * 8;
                 const bool in = FULL || d < D;
-                k[t][c] = *(const uint4 *)(keys + max(ko[t], (int64_t)0) + (in ? d : 0));
-                if (!in) k[t][c] = make_uint4(0, 0, 0, 0);
+                k[t][c] = *(const u32x4 *)(keys + max(ko[t], (int64_t)0) + (in ? d : 0));
+                if (!in) k[t][c] = (u32x4){0, 0, 0, 0};
             }
+    }
+    // places of tokens 4 quad + i and 16 + 4 quad + i
+    template <bool FULL> __device__ __forceinline__ void load_v(const uint16_t *values, const int64_t *vo, int r, int D) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -112,27 +161,29 @@ template <int DP> struct Step<uint16_t, DP> {
                 v[i][h] = *(const VRaw *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0));
             }
     }
-    __device__ __forceinline__ void clear_v(const int64_t *vo) {
+    __device__ __forceinline__ void clear_v(uint32_t dead) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (vo[i] < 0)
+            if (dead >> i & 1)
 #pragma unroll
                 for (int h = 0; h < NV; ++h) v[i][h] = (VRaw)0;
     }
-    __device__ __forceinline__ void scores(float *s) const {
+    template <bool FULL> __device__ __forceinline__ void scores(float *s, int D) const {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x4 c4 = {0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < NK; ++c)
+            for (int c = 0; c < NK; ++c) {
+                if (!FULL && DP < 256 && c * 32 >= D) break;
                 c4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k[t][c]), as_bf16x8(q[c]), c4, 0, 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[4 * t + i] = c4[i];
         }
     }
     // Probabilities are rounded to bf16 here: their product runs on bf16 operands.
     __device__ __forceinline__ void outputs(const float *p, f32x4 (*acc)[VW]) const {
-        const uint4 b = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+        const u32x4 b = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
 #pragma unroll
         for (int h = 0; h < NV; ++h)
 #pragma unroll
@@ -141,7 +192,7 @@ template <int DP> struct Step<uint16_t, DP> {
                 uint32_t w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][h][j / 2], v[2 * i][h][j / 2], sel);
-                acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])),
+                acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8((u32x4){w[0], w[1], w[2], w[3]}),
                                                                     as_bf16x8(b), acc[h][j], 0, 0, 0);
             }
     }
@@ -153,25 +204,21 @@ template <int DP> struct Step<float, DP> {
     f32x4 k[NK];
     f32x4 v[4][NV];
 
-    __device__ __forceinline__ void load_q(const float *p, int64_t stride, bool on, int quad, int D) {
+    __device__ __forceinline__ void load_q(const float *row, int quad) {
 #pragma unroll
-        for (int c = 0; c < NK; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = c * 16 + quad * 4 + i;
-                q[c][i] = on && d < D ? p[d * stride] : 0.f;
-            }
+        for (int c = 0; c < NK; ++c) q[c] = *(const f32x4 *)(row + c * 16 + quad * 4);
     }
-    template <bool FULL>
-    __device__ __forceinline__ void load(const float *keys, const float *values, const int64_t *ko, const int64_t *vo,
-                                         int quad, int r, int D) {
+    template <bool FULL> __device__ __forceinline__ void load_k(const float *keys, const int64_t *ko, int quad, int D) {
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
+            if (!FULL && DP < 256 && c * 16 >= D) break;
             const int d = c * 16 + quad * 4;
             const bool in = FULL || d < D;
             k[c] = *(const f32x4 *)(keys + max(ko[0], (int64_t)0) + (in ? d : 0));
             if (!in) k[c] = (f32x4){0, 0, 0, 0};
         }
+    }
+    template <bool FULL> __device__ __forceinline__ void load_v(const float *values, const int64_t *vo, int r, int D) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -180,21 +227,23 @@ template <int DP> struct Step<float, DP> {
                 v[i][h] = *(const f32x4 *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0));
             }
     }
-    __device__ __forceinline__ void clear_v(const int64_t *vo) {
+    __device__ __forceinline__ void clear_v(uint32_t dead) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (vo[i] < 0)
+            if (dead >> i & 1)
 #pragma unroll
                 for (int h = 0; h < NV; ++h) v[i][h] = (f32x4){0, 0, 0, 0};
     }
-    __device__ __forceinline__ void scores(float *s) const {
-        f32x4 c4 = {0, 0, 0, 0};
+    template <bool FULL> __device__ __forceinline__ void scores(float *s, int D) const {
+        f32x4 c4[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};   // two chains, or each product waits for the one before
 #pragma unroll
-        for (int c = 0; c < NK; ++c)
+        for (int c = 0; c < NK; ++c) {
+            if (!FULL && DP < 256 && c * 16 >= D) break;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c4 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], q[c][i], c4, 0, 0, 0);
+            for (int i = 0; i < 4; ++i) c4[i % 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], q[c][i], c4[i % 2], 0, 0, 0);
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = c4[i];
+        for (int i = 0; i < 4; ++i) s[i] = c4[0][i] + c4[1][i];
     }
     __device__ __forceinline__ void outputs(const float *p, f32x4 (*acc)[VW]) const {
 #pragma unroll
@@ -207,27 +256,93 @@ template <int DP> struct Step<float, DP> {
     }
 };
 
-// A workgroup: one part of a sequence's tokens, for up to 16 query heads of one key head.  Its waves
-// take the steps in turn and are joined through LDS; a sequence of one part is finished here, others
-// leave (maximum, sum) and outputs of their parts in the workspace.
-template <typename E, int DP, bool FULL>
+// The workspace: maxima and sums, then outputs, of segments' heads; first share and number of segments
+// of each unit.
+struct Parts {
+    float *m, *l, *o;
+    int2 *count;
+    int heads;
+    __device__ __forceinline__ explicit Parts(const AttnArgs &a) : heads(min(16, a.group)) {
+        const int64_t units = (int64_t)a.batch * a.c.kv_heads * a.head_groups, n = (a.shares + units) * heads;
+        count = (int2 *)a.workspace;
+        m = (float *)(count + units), l = m + n, o = l + n;
+    }
+    __device__ __forceinline__ int64_t at(int64_t segment, int head) const { return segment * heads + head; }
+};
+
+// A workgroup: its share of the work, or (shares 0) a unit: a sequence's tokens for up to 16 query heads
+// of one key head.  In a segment its waves take the steps in turn and are joined through LDS; a unit
+// of one segment is finished here, others leave (maximum, sum) and outputs of their segments in the
+// workspace.
+template <typename E, int DP, bool FULL, bool SHARED>
 __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArgs a) {
     typedef Step<E, DP> St;
     constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV, ROW = DP + 4;
     __shared__ int64_t place[kTile];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16], s_o[2][16][ROW];
+    __shared__ int32_t s_before[SHARED ? kMostSeqs + 1 : 1], s_len[SHARED ? kMostSeqs : 1];
+    __shared__ __attribute__((aligned(16))) E s_q[16][DP + 16 / sizeof(E)];
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, quad = lane / 16, D = a.c.head_dim;
-    const int part = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;   // unit: (sequence, key head, head group)
-    const int hg = unit % a.head_groups, bj = unit / a.head_groups, j = bj % a.c.kv_heads, b = bj / a.c.kv_heads;
-    int row;
-    const Span sp = span_of(a, b, &row);
-    if (part >= sp.parts) return;
-    const int from = sp.first + part * a.chunk, to = min(sp.len, from + a.chunk);
+    const int wave = uni(threadIdx.x / 64), D = a.c.head_dim;
+    const int per_seq = a.c.kv_heads * a.head_groups;   // units of a sequence
+    int64_t pos = 0, end = 1, total;
+    if (SHARED) {
+        count_blocks(a, s_before, s_len);
+        const int64_t share = share_of(a, s_before, &total);
+        pos = blockIdx.x * share, end = min(pos + share, total);
+        // sequences without tokens: no workgroup's work
+        for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+            if (uni(s_before[b + 1]) != uni(s_before[b])) continue;
+            for (int i = threadIdx.x; i < per_seq; i += 64 * kWaves) Parts(a).count[b * (int64_t)per_seq + i] = make_int2(0, 1);
+            for (int i = threadIdx.x; i < a.heads * D; i += 64 * kWaves)
+                ((E *)a.y)[b * a.ys.seq + i / D * a.ys.head + i % D * a.ys.dim] = (E)0;
+            if (a.lse)
+                for (int i = threadIdx.x; i < a.heads; i += 64 * kWaves) a.lse[(int64_t)b * a.heads + i] = -INFINITY;
+        }
+    }
+    while (pos < end) {
+    int lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));   // what goes by the lane is worked out again for each segment, not held in registers
+    const int r = lane % 16, quad = lane / 16;
+    int b, u, from, to;
+    bool whole_unit = true;
+    int64_t segment = 0;
+    Span sp;
+    if (SHARED) {
+        int lo = 0, hi = a.batch;   // the last sequence that begins at or before pos, which has blocks
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((int64_t)uni(s_before[mid]) * per_seq <= pos) lo = mid; else hi = mid;
+        }
+        b = lo;
+        sp = span_of(a, uni(row_of(a, b)), uni(s_len[b]));
+        const int64_t rest = pos - (int64_t)uni(s_before[b]) * per_seq;
+        const int length = length_of(sp);
+        u = uni((int)(rest / length));
+        const int off = (int)(rest - (int64_t)u * length), n = (int)min(end - pos, (int64_t)(length - off));
+        const int first = max(0, off - kCost), last = max(0, off + n - kCost);   // blocks of the segment
+        pos += n;
+        if (first == last) continue;
+        from = sp.first + first * kBlock, to = min(sp.len, sp.first + last * kBlock);
+        whole_unit = last - first == sp.blocks;
+        if (first == 0 && threadIdx.x == 0) {   // for k_attn_join: segments of the unit
+            const int64_t start = rest - off + (int64_t)uni(s_before[b]) * per_seq;
+            Parts(a).count[b * (int64_t)per_seq + u] = make_int2(blockIdx.x, (int)((start + length - 1) / share_of(a, s_before, &total)) - blockIdx.x + 1);
+        }
+        segment = b * (int64_t)per_seq + u + blockIdx.x;
+    } else {
+        b = blockIdx.x / per_seq, u = blockIdx.x - b * per_seq;
+        const int row = uni(row_of(a, b));
+        sp = span_of(a, row, uni(len_of(a, row)));
+        from = sp.first, to = sp.len;
+        pos = end;
+    }
+    const int hg = u % a.head_groups, j = u / a.head_groups;
     const int heads = min(16, a.group - hg * 16), h0 = j * a.group + hg * 16;
 
+    const int32_t *table = a.table + (int64_t)sp.row * a.width;
+    const E *keys = (const E *)a.keys + j * a.c.head_stride, *values = (const E *)a.values + j * a.c.head_stride;
     St st;
-    st.load_q((const E *)a.q + b * a.qs.seq + (h0 + min(r, heads - 1)) * a.qs.head, a.qs.dim, r < heads, quad, D);
     f32x4 acc[NV][VW];
 #pragma unroll
     for (int h = 0; h < NV; ++h)
@@ -235,7 +350,6 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
         for (int i = 0; i < VW; ++i) acc[h][i] = (f32x4){0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
     const float scale = a.scale * kLog2e;
-    const int32_t *table = a.table + (int64_t)row * a.width;
 
     for (int base = from; base < to; base += kTile) {
         const int n = min(kTile, to - base), padded = (n + TOK - 1) / TOK * TOK;
@@ -245,30 +359,50 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
             if (t < n) {
                 uint32_t slot;
                 const int page = page_of(a.c, table, (uint32_t)(base + t), &slot);
-                if (page >= 0) at = page * a.c.page_stride + slot * a.c.slot_stride + j * a.c.head_stride;
+                if (page >= 0) at = page * a.c.page_stride + slot * a.c.slot_stride;
             }
             place[t] = at;
         }
-        __syncthreads();
-        for (int s0 = wave * TOK; s0 < padded; s0 += kWaves * TOK) {
-            int64_t ko[NT], vo[TT];
-            bool all = true;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                ko[t] = place[s0 + 16 * t + r];
-                all = all && ko[t] >= 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vo[4 * t + i] = place[s0 + 16 * t + 4 * quad + i];
+        if (base == from) {   // queries come while the places do; 0 past the heads and past head_dim
+            const E *q = (const E *)a.q + b * a.qs.seq + h0 * a.qs.head;
+            for (int i = threadIdx.x; i < 16 * DP; i += 64 * kWaves) {
+                const int h = i / DP, d = i % DP;
+                s_q[h][d] = h < heads && d < D ? q[h * a.qs.head + d * a.qs.dim] : (E)0;
             }
-            st.template load<FULL>((const E *)a.keys, (const E *)a.values, ko, vo, quad, r, D);
-            float s[TT];
-            st.scores(s);
-            const bool whole = __all(all);
+        }
+        __syncthreads();
+        if (base == from) st.load_q(s_q[r], quad);
+        // A step's keys are asked for once the step before has used its own, and likewise its values, so
+        // that one of the two is always on its way.  `dead`: the lane's tokens that hold nothing.
+        uint32_t dead;
+        auto load_k = [&](int s0) __attribute__((always_inline)) {
+            int64_t ko[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) ko[t] = place[s0 + 16 * t + r];
+            st.template load_k<FULL>(keys, ko, quad, D);
+            asm volatile("" ::: "memory");   // the loads stay ahead of their use
+        };
+        auto load_v = [&](int s0) __attribute__((always_inline)) {
+            int64_t vo[TT];
+            dead = 0;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    vo[4 * t + i] = place[s0 + 16 * t + 4 * quad + i];
+                    dead |= (vo[4 * t + i] < 0 ? 1u : 0u) << (4 * t + i);
+                }
+            st.template load_v<FULL>(values, vo, r, D);
+            asm volatile("" ::: "memory");
+        };
+        float s[TT];
+        auto softmax = [&]() __attribute__((always_inline)) {
+            const bool whole = !__any(dead != 0);
             float top = m;
 #pragma unroll
             for (int i = 0; i < TT; ++i) {
                 s[i] *= scale;
-                if (!whole && vo[i] < 0) s[i] = -INFINITY;
+                if (!whole && (dead >> i & 1)) s[i] = -INFINITY;
                 top = fmaxf(top, s[i]);
             }
             top = fmaxf(top, __shfl_xor(top, 16));
@@ -283,13 +417,28 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
             }
             l = l * keep + sum;
             m = top;
-            if (!whole) st.clear_v(vo);
+            if (!whole) st.clear_v(dead);
             if (__any(keep != 1.f))
 #pragma unroll
                 for (int h = 0; h < NV; ++h)
 #pragma unroll
                     for (int i = 0; i < VW; ++i) acc[h][i] *= keep;
             st.outputs(s, acc);
+        };
+        int s0 = wave * TOK;
+        if (s0 < padded) {
+            load_k(s0);
+            load_v(s0);
+            for (;;) {
+                st.template scores<FULL>(s, D);
+                const int next = s0 + kWaves * TOK;
+                if (next >= padded) break;
+                load_k(next);
+                softmax();
+                load_v(next);
+                s0 = next;
+            }
+            softmax();
         }
     }
 
@@ -328,83 +477,103 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
         for (int w = 0; w < kWaves; ++w) sum += s_l[w][h] * __builtin_amdgcn_exp2f(s_m[w][h] - ref);
         const float o = s_o[0][h][d] + s_o[1][h][d];
         const int64_t bh = (int64_t)b * a.heads + h0 + h;
-        if (sp.parts == 1) {
+        if (whole_unit) {
             E *y = (E *)a.y + b * a.ys.seq + (h0 + h) * a.ys.head + d * a.ys.dim;
             *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);
             if (d == 0 && a.lse) a.lse[bh] = (ref + log2f(sum)) * kLn2;
         } else {
-            float *ml = (float *)a.workspace, *out = ml + 2 * (int64_t)a.batch * a.heads * a.splits;
-            out[(bh * a.splits + part) * D + d] = o;
-            if (d == 0) ml[(bh * a.splits + part) * 2] = mm, ml[(bh * a.splits + part) * 2 + 1] = sum;
+            const Parts parts(a);
+            const int64_t at = parts.at(segment, h);
+            parts.o[at * D + d] = o;
+            if (d == 0) parts.m[at] = mm, parts.l[at] = sum;
         }
+    }
+    if (SHARED) __syncthreads();   // the next segment writes these arrays
     }
 }
 
-// Joins the parts of a sequence's query head: a workgroup each, a thread a dimension of every
-// 256 / DP-th part.
-constexpr int kMaxSplits = 256;
-template <typename E, int DP>
+// Joins the segments of a query head: 32 dimensions and 8 segments at a time.
+template <typename E>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-    __shared__ float s_w[kMaxSplits], s_red[8], s_o[256];
-    const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.heads), h = (int)(bh - (int64_t)b * a.heads), t = threadIdx.x, D = a.c.head_dim;
-    int row;
-    const Span sp = span_of(a, b, &row);
-    if (sp.parts == 1) return;
-    const float *ml = (const float *)a.workspace + bh * a.splits * 2;
-    const float *o = (const float *)a.workspace + 2 * (int64_t)a.batch * a.heads * a.splits + bh * a.splits * D;
-    const float m = t < sp.parts ? ml[2 * t] : -INFINITY, l = t < sp.parts ? ml[2 * t + 1] : 0.f;
-    float top = m;
+    __shared__ float s_w[kMostShares + 2], s_red[8], s_o[8][32];
+    const int h = blockIdx.x % a.heads, b = blockIdx.x / a.heads, t = threadIdx.x, D = a.c.head_dim;
+    const int u = h / a.group * a.head_groups + h % a.group / 16;
+    const int64_t unit = (int64_t)b * (a.c.kv_heads * a.head_groups) + u;
+    const int2 count = Parts(a).count[unit];
+    const int n = count.y;
+    if (n == 1) return;
+    const Parts parts(a);
+    const int64_t seg = unit + count.x;   // the first of n in a row
+    const int hh = h % a.group % 16;
+    float top = -INFINITY, sum = 0.f;
+    for (int p = t; p < n; p += 256) {
+        s_w[p] = parts.m[parts.at(seg + p, hh)];
+        top = fmaxf(top, s_w[p]);
+    }
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     if (t % 64 == 0) s_red[t / 64] = top;
     __syncthreads();
     top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    const float ref = top == -INFINITY ? 0.f : top, w = __builtin_amdgcn_exp2f(m - ref);
-    float sum = l * w;
+    const float ref = top == -INFINITY ? 0.f : top;
+    for (int p = t; p < n; p += 256) {
+        s_w[p] = __builtin_amdgcn_exp2f(s_w[p] - ref);
+        sum += parts.l[parts.at(seg + p, hh)] * s_w[p];
+    }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if (t % 64 == 0) s_red[4 + t / 64] = sum;
-    s_w[t] = w;
     __syncthreads();
     sum = (s_red[4] + s_red[5]) + (s_red[6] + s_red[7]);
-    constexpr int G = 256 / DP;
-    const int d = t % DP, g = t / DP;
-    float v = 0.f;
-    if (d < D)
-        for (int p = g; p < sp.parts; p += G) v += o[(int64_t)p * D + d] * s_w[p];
-    s_o[t] = v;
-    __syncthreads();
-    if (t >= D) return;
+    const int g = t / 32;
+    for (int d0 = blockIdx.y * 32; d0 < D; d0 += gridDim.y * 32) {
+        const int d = d0 + t % 32;
+        float v = 0.f;
+        if (d < D)
+#pragma unroll 8
+            for (int p = g; p < n; p += 8) v += parts.o[parts.at(seg + p, hh) * D + d] * s_w[p];
+        __syncthreads();
+        s_o[g][t % 32] = v;
+        __syncthreads();
+        if (t >= 32 || d >= D) continue;
 #pragma unroll
-    for (int i = 1; i < G; ++i) v += s_o[t + i * DP];
-    E *y = (E *)a.y + b * a.ys.seq + h * a.ys.head + t * a.ys.dim;
-    *y = from_f32<E>(sum == 0.f ? 0.f : v / sum);
-    if (t == 0 && a.lse) a.lse[bh] = (ref + log2f(sum)) * kLn2;
+        for (int i = 1; i < 8; ++i) v += s_o[i][t];
+        E *y = (E *)a.y + b * a.ys.seq + h * a.ys.head + d * a.ys.dim;
+        *y = from_f32<E>(sum == 0.f ? 0.f : v / sum);
+        if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;
+    }
 }
 
-// How the tokens are split: about `kTarget` workgroups if all sequences were as long as they may be,
-// parts of at least kMinChunk tokens (two steps a wave).
-constexpr int kTarget = 1024, kMinChunk = 256;
+// Workgroups of a call that is cut into shares: as many as the card holds.
+constexpr int shares_of(int dp) { return dp == 256 ? 256 : 512; }
 int units_of(const CacheArgs &c, int batch, int heads) {
     return batch * c.kv_heads * ((heads / c.kv_heads + 15) / 16);
 }
-int most_splits(const CacheArgs &c, int batch, int heads) {
-    return std::min(kMaxSplits, std::max(1, kTarget / std::max(1, units_of(c, batch, heads))));
+// Whether the work is cut into shares: for up to kMostSeqs sequences (more fill the card unsplit) that
+// may be longer than one share at least.
+bool shared(const CacheArgs &c, int batch, int64_t tokens) {
+    return batch <= kMostSeqs && tokens > kMinShare * kBlock;
 }
 
 template <typename E, int DP, bool FULL>
-hipError_t run(const AttnArgs &a, hipStream_t st) {
-    k_attn<E, DP, FULL><<<units_of(a.c, a.batch, a.heads) * a.splits, 64 * kWaves, 0, st>>>(a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-    k_attn_join<E, DP><<<a.batch * a.heads, 256, 0, st>>>(a);
+hipError_t run(AttnArgs a, bool split, hipStream_t st) {
+    const int units = units_of(a.c, a.batch, a.heads);
+    if (!split) {
+        k_attn<E, DP, FULL, false><<<units, 64 * kWaves, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    a.shares = shares_of(DP);
+    k_attn<E, DP, FULL, true><<<a.shares, 64 * kWaves, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const int slices = a.batch * a.heads >= 256 ? 1 : (a.c.head_dim + 31) / 32;   // few heads: more workgroups for each
+    k_attn_join<E><<<dim3(a.batch * a.heads, slices), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <typename E>
-hipError_t run(const AttnArgs &a, hipStream_t st) {
+hipError_t run(const AttnArgs &a, bool split, hipStream_t st) {
     const int D = a.c.head_dim;
-    if (D <= 64) return D == 64 ? run<E, 64, true>(a, st) : run<E, 64, false>(a, st);
-    if (D <= 128) return D == 128 ? run<E, 128, true>(a, st) : run<E, 128, false>(a, st);
-    return D == 256 ? run<E, 256, true>(a, st) : run<E, 256, false>(a, st);
+    if (D <= 64) return D == 64 ? run<E, 64, true>(a, split, st) : run<E, 64, false>(a, split, st);
+    if (D <= 128) return D == 128 ? run<E, 128, true>(a, split, st) : run<E, 128, false>(a, split, st);
+    return D == 256 ? run<E, 256, true>(a, split, st) : run<E, 256, false>(a, split, st);
 }
 
 }  // namespace
@@ -418,20 +587,21 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// (maximum, sum) and head_dim outputs of every part of every query head
+// First share and number of segments of every unit; maximum, sum and head_dim outputs of every
+// segment, at most shares + units, for each head of a group
 int64_t attention_workspace(const CacheArgs &c, int batch, int heads, int width) {
-    const int64_t most = std::min<int64_t>(most_splits(c, batch, heads), div_up64((int64_t)width * c.page_size, kMinChunk));
-    return most <= 1 ? 0 : (int64_t)batch * heads * most * (c.head_dim + 2) * 4;
+    if (!shared(c, batch, (int64_t)width * c.page_size)) return 0;
+    const int64_t units = units_of(c, batch, heads), segments = kMostShares + units;
+    return units * 8 + segments * std::min(16, heads / c.kv_heads) * (c.head_dim + 2) * 4;
 }
 
 hipError_t launch_attention(AttnArgs a, hipStream_t st) {
     int64_t tokens = (int64_t)a.width * a.c.page_size;
     if (a.window) tokens = std::min<int64_t>(tokens, a.window);
-    const int64_t most = most_splits(a.c, a.batch, a.heads);
-    a.chunk = (int)std::max<int64_t>(kMinChunk, div_up64(div_up64(tokens, most), 128) * 128);
-    a.splits = (int)std::max<int64_t>(1, div_up64(tokens, a.chunk));
     a.head_groups = (a.group + 15) / 16;
-    return a.c.dtype == BSP_F32 ? run<float>(a, st) : run<uint16_t>(a, st);
+    a.shares = 0;
+    const bool split = shared(a.c, a.batch, tokens);
+    return a.c.dtype == BSP_F32 ? run<float>(a, split, st) : run<uint16_t>(a, split, st);
 }
 
 }  // namespace bsp

@@ -66,7 +66,8 @@ struct AttnArgs {
     int batch, heads, group, seqs, width, window;
     float scale;
     void *workspace;
-    int chunk, splits, head_groups;   // set by launch_attention: tokens of a part, parts at most
+    int shares;                   // set by launch_attention: workgroups that the work is cut for, 0: one a unit
+    int head_groups;              // set by launch_attention: of up to 16 query heads of a key head
 };
 int64_t attention_workspace(const CacheArgs &c, int batch, int heads, int width);
 hipError_t launch_attention(AttnArgs a, hipStream_t st);
