@@ -264,7 +264,8 @@ bsp_status bsp_maxpool2x2(bsp_dtype dt, int32_t n, int32_t c, int32_t h, int32_t
  *           every 16 * ceil(ceil(cols / 2) / 16) bytes; 16-byte aligned
  *   scales  bf16, [ceil(cols / group)][rows rounded up to 16]; 8-byte aligned
  * What lies between a row's last code and the next row, and scales past the last row, are not read
- * as values.  Rows of codes and of scales may be longer than 2^31 bytes in all. */
+ * as values.  Codes and scales may be longer than 2^31 bytes in all; a matrix of more than 2^24 tiles
+ * of 16 x 128 is BSP_EUNSUPPORTED. */
 
 /* Bytes of `codes` and elements of `scales`.  Host-only, pure. */
 bsp_status bsp_q4_sizes(int32_t rows, int32_t cols, int32_t group, int64_t *code_bytes, int64_t *n_scales);
@@ -285,15 +286,16 @@ bsp_status bsp_q4_dequantize(int32_t rows, int32_t cols, int32_t group, bsp_dtyp
  *   y[o][b] = bias[o] + sum_g scales[g][o] * sum_{k in g} (code(o, k) - 8) * x[k][b], then ReLU if relu.
  * Made for small batches (decoding); right for any.  Sums are in fp32 (x of BSP_F32 is multiplied in
  * full); x must be finite, and an Inf or NaN makes every output of its batch column NaN.  No
- * workspace.  Async. */
+ * workspace.  rows and cols up to 2^26, rows * batch and cols * batch below 2^31 and x below 2^32 bytes;
+ * else BSP_EUNSUPPORTED.  Async. */
 bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batch, bsp_dtype in_dt, bsp_dtype out_dt,
                          const void *x, const uint8_t *codes, const void *scales, const float *bias_or_null,
                          int32_t relu, void *y, void *stream);
 
 /* Keys and values of the tokens seen so far lie in pages of page_size tokens.  Token t of sequence s
  * is slot t % page_size of page table[s][t / page_size]; entries of the table that are negative (or
- * not below `pages`) hold nothing; width * page_size is at most 2^30.  Keys and values of one layer are arrays of `pages` pages each, a
- * page being
+ * not below `pages`) hold nothing; width * page_size is at most 2^30.  Keys and values of one layer are
+ * arrays of `pages` pages each, a page being
  *   BSP_HEAD_MAJOR  [kv_heads][page_size][head_dim]
  *   BSP_SLOT_MAJOR  [page_size][kv_heads][head_dim]
  * and page_stride elements after the one before (0: no gap).  16-byte aligned; head_dim is a
@@ -354,9 +356,8 @@ bsp_status bsp_cache_fork(int32_t seqs, int32_t width, int32_t pages, int32_t *t
 /* Room for counts[i] more tokens in each sequence rows[i]: pages for the positions from pos[i] =
  * lens[rows[i]] on, which becomes pos[i] + counts[i].  A last page that has tokens and that another
  * entry shares is first copied (the slots in use) to a page of the sequence's own (a last entry that
- * names no page just gets one).  Where the free
- * pages or the width do not suffice for the whole call, nothing changes and every pos is -1; so is
- * that of a row that is left out. */
+ * names no page just gets one).  Where the free pages or the width do not suffice for the whole call,
+ * nothing changes and every pos is -1; so is that of a row that is left out. */
 bsp_status bsp_cache_extend(const bsp_cache *cache, int32_t planes, int64_t plane_stride, void *data, int32_t seqs,
                             int32_t width, int32_t *table, int32_t *lens, int32_t *refs, int32_t n,
                             const int32_t *rows, const int32_t *counts, int32_t *pos, void *scratch, void *stream);

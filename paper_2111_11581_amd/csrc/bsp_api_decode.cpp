@@ -17,8 +17,11 @@ inline int esize(int dt) { return dt == BSP_F32 ? 4 : 2; }
 inline bool aligned(const void *p, int bytes) { return (uintptr_t)p % bytes == 0; }
 
 bool q4_ok(int32_t rows, int32_t cols, int32_t group) {
-    return rows >= 1 && cols >= 1 && (group == 32 || group == 64 || group == 128);
+    return rows >= 1 && rows <= INT32_MAX - 15 && cols >= 1 && (group == 32 || group == 64 || group == 128);
 }
+
+// One launch covers the matrix in tiles of 16 x 128.
+bool q4_fits(const Q4Shape &s) { return (int64_t)s.rows16 / 16 * ((s.stride + 63) / 64) < 1 << 24; }
 
 bsp_status check_cache(const bsp_cache *c) {
     if (!c || !dtype_ok(c->dtype) || (c->order != BSP_HEAD_MAJOR && c->order != BSP_SLOT_MAJOR)) return BSP_EINVAL;
@@ -76,14 +79,18 @@ bsp_status bsp_q4_quantize(int32_t rows, int32_t cols, int32_t group, bsp_dtype 
                            uint8_t *codes, void *scales, void *stream) {
     if (!q4_ok(rows, cols, group) || !dtype_ok(wdt) || !w || !codes || !scales) return BSP_EINVAL;
     if (!aligned(codes, 16) || !aligned(scales, 8) || !aligned(w, esize(wdt))) return BSP_EINVAL;
-    return status(launch_q4_quantize(q4_shape(rows, cols, group), wdt, w, mask, codes, (uint16_t *)scales, S(stream)));
+    const Q4Shape s = q4_shape(rows, cols, group);
+    if (!q4_fits(s)) return BSP_EUNSUPPORTED;
+    return status(launch_q4_quantize(s, wdt, w, mask, codes, (uint16_t *)scales, S(stream)));
 }
 
 bsp_status bsp_q4_dequantize(int32_t rows, int32_t cols, int32_t group, bsp_dtype wdt, const uint8_t *codes,
                              const void *scales, void *w, void *stream) {
     if (!q4_ok(rows, cols, group) || !dtype_ok(wdt) || !w || !codes || !scales) return BSP_EINVAL;
     if (!aligned(codes, 16) || !aligned(scales, 8) || !aligned(w, esize(wdt))) return BSP_EINVAL;
-    return status(launch_q4_dequantize(q4_shape(rows, cols, group), wdt, codes, (const uint16_t *)scales, w, S(stream)));
+    const Q4Shape s = q4_shape(rows, cols, group);
+    if (!q4_fits(s)) return BSP_EUNSUPPORTED;
+    return status(launch_q4_dequantize(s, wdt, codes, (const uint16_t *)scales, w, S(stream)));
 }
 
 bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batch, bsp_dtype in_dt, bsp_dtype out_dt,
@@ -94,7 +101,7 @@ bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batc
     if (!aligned(x, esize(in_dt)) || !aligned(y, esize(out_dt)) || !aligned(bias, 4)) return BSP_EINVAL;
     // offsets in x, and in the codes of 64 rows, are 32-bit numbers of bytes
     if ((int64_t)cols * batch > (int64_t)UINT32_MAX / esize(in_dt) || (int64_t)cols * batch > INT32_MAX) return BSP_EUNSUPPORTED;
-    if ((int64_t)rows * batch > INT32_MAX || cols > 1 << 26) return BSP_EUNSUPPORTED;
+    if ((int64_t)rows * batch > INT32_MAX || cols > 1 << 26 || rows > 1 << 26) return BSP_EUNSUPPORTED;
     if (batch == 0) return BSP_OK;
     return status(launch_q4_linear(q4_shape(rows, cols, group), batch, in_dt, out_dt, x, codes, (const uint16_t *)scales,
                                    bias, relu ? 1 : 0, y, S(stream)));

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include "bsp_decode.h"
+#include "bsp_decode_dev.h"
 
 namespace bsp {
 
@@ -11,35 +12,45 @@ namespace {
 
 __device__ __forceinline__ bool in(int i, int n) { return (unsigned)i < (unsigned)n; }
 
-// A pair's column of the table, or (column `width`) its length, is read into scratch, and counted,
-// before any child's is changed: a workgroup owns 64 columns of all pairs.  A thread reads and
-// writes the same places, so scratch needs no more than the barrier.
-__global__ __launch_bounds__(256) void k_fork(PagesArgs a, const int32_t *__restrict__ parents,
-                                              const int32_t *__restrict__ children) {
-    const int col = blockIdx.x * 64 + threadIdx.x % 64, first = threadIdx.x / 64;
+// A pair's column of the table, or (column `width`) its length, is read, and counted, before any child's
+// is changed: a workgroup owns 16 columns of all pairs, 64 pairs at a time.  A thread keeps what it
+// read of its first pairs in registers and of more in scratch, which nobody else touches.  Bound by
+// the latency of pair, entry and count one after the other: 32 pairs of 54 entries 3.2 us, an empty
+// kernel 3 (64 columns and 4 pairs at a time, all through scratch: 14 us).
+constexpr int kForkCols = 16, kForkRows = 64, kForkKept = 4;
+__global__ __launch_bounds__(kForkCols *kForkRows) void k_fork(PagesArgs a, const int32_t *__restrict__ parents,
+                                                               const int32_t *__restrict__ children) {
+    const int col = blockIdx.x * kForkCols + threadIdx.x % kForkCols, first = threadIdx.x / kForkCols;
     const int64_t line = (int64_t)a.width + 1;
     const bool on = col <= a.width;
-    if (on)
-        for (int i = first; i < a.n; i += 4) {
-            const int p = parents[i];
-            if (!in(p, a.seqs) || !in(children[i], a.seqs)) continue;
-            const int v = col < a.width ? a.table[(int64_t)p * a.width + col] : a.lens[p];
-            a.scratch[i * line + col] = v;
-            if (col < a.width && in(v, a.pages)) atomicAdd(&a.refs[v], 1);
+    int kept[kForkKept], child[kForkKept];
+    auto read = [&](int i, int *to) {   // the child, or -1
+        const int p = parents[i], c = children[i];
+        if (!on || !in(p, a.seqs) || !in(c, a.seqs)) return -1;
+        *to = col < a.width ? a.table[(int64_t)p * a.width + col] : a.lens[p];
+        if (col < a.width && in(*to, a.pages)) atomicAdd(&a.refs[*to], 1);
+        return c;
+    };
+    auto write = [&](int c, int v) {
+        if (c < 0) return;
+        if (col == a.width) {
+            a.lens[c] = v;
+            return;
         }
+        const int old = atomicExch(&a.table[(int64_t)c * a.width + col], v);
+        if (in(old, a.pages)) atomicSub(&a.refs[old], 1);
+    };
+#pragma unroll
+    for (int k = 0; k < kForkKept; ++k) child[k] = first + k * kForkRows < a.n ? read(first + k * kForkRows, &kept[k]) : -1;
+    for (int i = first + kForkKept * kForkRows; i < a.n; i += kForkRows) {
+        int v;
+        if (read(i, &v) >= 0) a.scratch[i * line + col] = v;
+    }
     __syncthreads();
-    if (on)
-        for (int i = first; i < a.n; i += 4) {
-            const int c = children[i];
-            if (!in(parents[i], a.seqs) || !in(c, a.seqs)) continue;
-            const int v = a.scratch[i * line + col];
-            if (col == a.width) {
-                a.lens[c] = v;
-                continue;
-            }
-            const int old = atomicExch(&a.table[(int64_t)c * a.width + col], v);
-            if (in(old, a.pages)) atomicSub(&a.refs[old], 1);
-        }
+#pragma unroll
+    for (int k = 0; k < kForkKept; ++k) write(child[k], kept[k]);
+    for (int i = first + kForkKept * kForkRows; i < a.n; i += kForkRows)
+        if (on && in(parents[i], a.seqs) && in(children[i], a.seqs)) write(children[i], a.scratch[i * line + col]);
 }
 
 __global__ __launch_bounds__(256) void k_release(PagesArgs a, const int32_t *__restrict__ rows) {
@@ -109,7 +120,7 @@ __device__ __forceinline__ Need need_of(const PagesArgs &a, int page_size, int r
     n.have = max(a.lens[row], 0), n.more = max(more, 0);
     n.last = n.have / page_size;
     n.start = (int)(((int64_t)n.have + page_size - 1) / page_size);
-    n.end = (int)(((int64_t)n.have + n.more + page_size - 1) / page_size);
+    n.end = (int)min(((int64_t)n.have + n.more + page_size - 1) / page_size, (int64_t)INT32_MAX);   // past any width
     if (n.more == 0) return n;
     if (n.have % page_size && n.last < a.width) {
         n.old = a.table[(int64_t)row * a.width + n.last];
@@ -120,11 +131,14 @@ __device__ __forceinline__ Need need_of(const PagesArgs &a, int page_size, int r
     return n;
 }
 
-// One workgroup: what every sequence needs and its rank among all, the lowest free pages, then the
-// new entries.  scratch: first rank [n], copies {src, dst} [n], free pages [pages].
+// One workgroup, since a sequence's pages depend on what all before it take and the whole call on all:
+// what every sequence needs and its rank among all, the lowest free pages, then the
+// new entries.  Bound by the latency of about ten dependent accesses and barriers: 32 sequences, 612
+// pages 7 us.  scratch: first rank [n], copies {src, dst} [n], free pages [pages].
 __global__ __launch_bounds__(kScan) void k_extend(PagesArgs a, int page_size, const int32_t *__restrict__ rows,
                                                   const int32_t *__restrict__ counts, int32_t *__restrict__ pos) {
     __shared__ int bad;
+    __shared__ Need s_need[kScan];    // of the first sequences; of more they are worked out again
     int32_t *first = a.scratch, *copy = first + a.n, *list = copy + 2 * (int64_t)a.n;
     if (threadIdx.x == 0) bad = 0;
     __syncthreads();
@@ -134,6 +148,7 @@ __global__ __launch_bounds__(kScan) void k_extend(PagesArgs a, int page_size, co
         int64_t need = 0, total;
         if (i < a.n) {
             const Need n = need_of(a, page_size, rows[i], counts[i]);
+            if (base == 0) s_need[i] = n;
             if (n.more && n.end > a.width) bad = 1;
             need = n.need;
         }
@@ -148,7 +163,7 @@ __global__ __launch_bounds__(kScan) void k_extend(PagesArgs a, int page_size, co
     // a wave per sequence
     for (int i = threadIdx.x / 64; i < a.n; i += kScan / 64) {
         const int row = rows[i], lane = threadIdx.x % 64;
-        const Need n = need_of(a, page_size, row, counts[i]);
+        const Need n = i < kScan ? s_need[i] : need_of(a, page_size, row, counts[i]);
         if (lane == 0) {
             pos[i] = ok && in(row, a.seqs) ? n.have : -1;
             copy[2 * i] = ok && n.fresh_last ? n.old : -1;
@@ -177,31 +192,43 @@ __global__ __launch_bounds__(kScan) void k_extend(PagesArgs a, int page_size, co
         }
 }
 
-// Copies `n` elements of 16 bytes.
-__device__ __forceinline__ void copy16(uint4 *dst, const uint4 *src, int64_t n) {
-    for (int64_t i = threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
+// A page is copied in chunks of 2048 pieces of 16 bytes, a workgroup per chunk: all of a thread's eight
+// loads are on their way before its first store (one at a time: 12 layers' shared last pages 12 us
+// instead of 6, 8 layers' compaction 136 instead of 101).  where(i) is piece i's place on both sides.
+constexpr int kChunk = 8 * 256;
+template <typename F> __device__ __forceinline__ void copy_chunk(u32x4 *dst, const u32x4 *src, int from, int n, F where) {
+    u32x4 v[8];
+    int64_t at[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) at[k] = where(min(from + k * 256 + (int)threadIdx.x, n - 1));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = src[at[k]];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (from + k * 256 + (int)threadIdx.x < n) dst[at[k]] = v[k];
 }
 
-// The slots in use of the pages that k_extend has replaced, a workgroup per sequence and plane.
+// The slots in use of the pages that k_extend has replaced: x the sequence, y planes, z chunks.
 __global__ __launch_bounds__(256) void k_extend_copy(PagesArgs a, PlanesArgs d, int esize, const int32_t *__restrict__ pos) {
     const int i = blockIdx.x, src = a.scratch[a.n + 2 * i], dst = a.scratch[a.n + 2 * i + 1];
     if (src < 0) return;
-    const int used = pos[i] % d.c.page_size;
     const int64_t unit = 16 / esize;
+    // pieces of a head's slots in use, and of a head (slots first: one run of all heads)
+    const int run = pos[i] % d.c.page_size * (int)(d.c.slot_stride / unit);
+    const int n = run * (d.c.order == BSP_SLOT_MAJOR ? 1 : d.c.kv_heads), head = (int)(d.c.head_stride / unit);
     for (int plane = blockIdx.y; plane < d.planes; plane += gridDim.y) {
-        uint4 *base = (uint4 *)d.data + plane * (d.plane_stride / unit);
-        const uint4 *from = base + src * (d.c.page_stride / unit);
-        uint4 *to = base + dst * (d.c.page_stride / unit);
-        if (d.c.order == BSP_SLOT_MAJOR)
-            copy16(to, from, used * (d.c.slot_stride / unit));
-        else
-            for (int h = 0; h < d.c.kv_heads; ++h)
-                copy16(to + h * (d.c.head_stride / unit), from + h * (d.c.head_stride / unit), used * (d.c.slot_stride / unit));
+        u32x4 *base = (u32x4 *)d.data + plane * (d.plane_stride / unit);
+        for (int from = blockIdx.z * kChunk; from < n; from += gridDim.z * kChunk)
+            copy_chunk(base + dst * (d.c.page_stride / unit), base + src * (d.c.page_stride / unit), from, n, [&](int k) {
+                const int h = k / run;
+                return (int64_t)h * head + (k - h * run);
+            });
     }
 }
 
-// One workgroup: pages in use, the moves, counts and the page that each becomes.  scratch: moves, src
-// [pages], dst [pages], map [pages].
+// One workgroup: pages in use, the moves, counts and the page that each becomes; three passes over the
+// counts, 4096 pages at a time, 6.6 us for the smallest caches.  scratch: moves, src [pages], dst
+// [pages], map [pages].
 __global__ __launch_bounds__(kScan) void k_compact_plan(PagesArgs a, int32_t *__restrict__ info) {
     int32_t *src = a.scratch + 4, *dst = src + a.pages, *map = dst + a.pages;
     const int used = list_pages(a.refs, 0, a.pages, true, nullptr, INT32_MAX);
@@ -220,26 +247,34 @@ __global__ __launch_bounds__(kScan) void k_compact_plan(PagesArgs a, int32_t *__
     }
 }
 
-__global__ __launch_bounds__(256) void k_remap(PagesArgs a) {
-    const int32_t *map = a.scratch + 4 + 2 * (int64_t)a.pages;
-    const int64_t n = (int64_t)a.seqs * a.width;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const int p = a.table[i];
-        if (in(p, a.pages)) a.table[i] = map[p];
-    }
+// Pieces of 16 bytes in a page.
+__host__ __device__ __forceinline__ int pieces(const PlanesArgs &d, int esize) {
+    return (int)((int64_t)d.c.page_size * d.c.kv_heads * d.c.head_dim * esize / 16);
 }
 
-// Whole pages: `n` pairs, or as many as *count says.
-__global__ __launch_bounds__(256) void k_page_copy(PlanesArgs d, int esize, int n, const int32_t *__restrict__ count,
-                                                   const int32_t *__restrict__ src, const int32_t *__restrict__ dst) {
-    if (count) n = *count;
-    const int64_t unit = 16 / esize, size = (int64_t)d.c.page_size * d.c.kv_heads * d.c.head_dim / unit;
-    for (int64_t i = blockIdx.x; i < (int64_t)n * d.planes; i += gridDim.x) {
-        const int pair = (int)(i / d.planes), plane = (int)(i - (int64_t)pair * d.planes);
+// Whole pages: `n` pairs, or (compact) as many as scratch says, whose table entries follow them.  Bound
+// by memory: 224 MB read and as much written in 93 us, 4.8 TB/s, as a large copy.
+__global__ __launch_bounds__(256) void k_page_copy(PagesArgs a, PlanesArgs d, int esize, const int32_t *__restrict__ src,
+                                                   const int32_t *__restrict__ dst) {
+    int n = a.n;
+    if (a.scratch) {
+        n = a.scratch[0];
+        const int32_t *map = a.scratch + 4 + 2 * (int64_t)a.pages;
+        for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)a.seqs * a.width; i += gridDim.x * 256ll) {
+            const int p = a.table[i];
+            if (in(p, a.pages)) a.table[i] = map[p];
+        }
+    }
+    const int64_t unit = 16 / esize;
+    const int size = pieces(d, esize), chunks = (size + kChunk - 1) / kChunk;
+    const int64_t per = (int64_t)d.planes * chunks;
+    for (int64_t i = blockIdx.x; i < n * per; i += gridDim.x) {
+        const int pair = (int)(i / per), rest = (int)(i - pair * per), plane = rest / chunks;
         const int s = src[pair], t = dst[pair];
         if (!in(s, d.c.pages) || !in(t, d.c.pages)) continue;
-        uint4 *base = (uint4 *)d.data + plane * (d.plane_stride / unit);
-        copy16(base + t * (d.c.page_stride / unit), base + s * (d.c.page_stride / unit), size);
+        u32x4 *base = (u32x4 *)d.data + plane * (d.plane_stride / unit);
+        copy_chunk(base + t * (d.c.page_stride / unit), base + s * (d.c.page_stride / unit), (rest - plane * chunks) * kChunk,
+                   size, [](int k) { return k; });
     }
 }
 
@@ -254,7 +289,7 @@ int64_t pages_scratch(int pages, int width, int n) {
 }
 
 hipError_t launch_fork(const PagesArgs &a, const int32_t *parents, const int32_t *children, hipStream_t st) {
-    k_fork<<<(unsigned)(a.width / 64 + 1), 256, 0, st>>>(a, parents, children);
+    k_fork<<<(unsigned)(a.width / kForkCols + 1), kForkCols * kForkRows, 0, st>>>(a, parents, children);
     return hipGetLastError();
 }
 
@@ -267,22 +302,24 @@ hipError_t launch_extend(const PagesArgs &a, const PlanesArgs &d, const int32_t 
                          hipStream_t st) {
     k_extend<<<1, kScan, 0, st>>>(a, d.c.page_size, rows, counts, pos);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || d.planes == 0) return e;
-    k_extend_copy<<<dim3(a.n, std::min(d.planes, 65535)), 256, 0, st>>>(a, d, esize(d), pos);
+    const int chunks = std::min(div_up(pieces(d, esize(d)), kChunk), 64);
+    k_extend_copy<<<dim3(a.n, std::min(d.planes, 65535), chunks), 256, 0, st>>>(a, d, esize(d), pos);
     return hipGetLastError();
 }
 
 hipError_t launch_compact(const PagesArgs &a, const PlanesArgs &d, int32_t *info, hipStream_t st) {
     k_compact_plan<<<1, kScan, 0, st>>>(a, info);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    k_remap<<<copy_grid(div_up64((int64_t)a.seqs * a.width, 256)), 256, 0, st>>>(a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const int32_t *src = a.scratch + 4;
-    k_page_copy<<<copy_grid((int64_t)a.pages * d.planes), 256, 0, st>>>(d, esize(d), 0, a.scratch, src, src + a.pages);
+    const int64_t items = std::max((int64_t)a.pages / 2 * d.planes * div_up(pieces(d, esize(d)), kChunk), div_up64((int64_t)a.seqs * a.width, 256));
+    k_page_copy<<<copy_grid(items), 256, 0, st>>>(a, d, esize(d), src, src + a.pages);
     return hipGetLastError();
 }
 
 hipError_t launch_page_copy(const PlanesArgs &d, int n, const int32_t *src, const int32_t *dst, hipStream_t st) {
-    k_page_copy<<<copy_grid((int64_t)n * d.planes), 256, 0, st>>>(d, esize(d), n, nullptr, src, dst);
+    PagesArgs a = {};
+    a.n = n;
+    k_page_copy<<<copy_grid((int64_t)n * d.planes * div_up(pieces(d, esize(d)), kChunk)), 256, 0, st>>>(a, d, esize(d), src, dst);
     return hipGetLastError();
 }
 

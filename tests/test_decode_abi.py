@@ -159,3 +159,12 @@ def test_the_binding_refuses_host_arrays_and_wrong_shapes(B):
     t = torch.zeros(2, 4, dtype=torch.int32)
     with pytest.raises(ValueError):
         B.bsp_cache_release(t, t[0], t[0], t[0])
+
+
+def test_q4_of_more_than_one_launch_is_refused(L):
+    big = (1 << 26) + 1
+    assert L.bsp_q4_quantize(big, 2048, 64, 1, P16, None, P16, P16, None) == EUNSUPPORTED
+    assert L.bsp_q4_dequantize(2048, big, 64, 1, P16, P16, P16, None) == EUNSUPPORTED
+    assert L.bsp_q4_linear(big, 64, 64, 1, 1, 1, P16, P16, P16, None, 0, P16, None) == EUNSUPPORTED
+    assert L.bsp_q4_linear(64, big, 64, 1, 1, 1, P16, P16, P16, None, 0, P16, None) == EUNSUPPORTED
+    assert L.bsp_q4_quantize(2**31 - 1, 1, 64, 1, P16, None, P16, P16, None) == EINVAL

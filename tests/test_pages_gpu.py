@@ -249,3 +249,25 @@ def test_a_step_of_a_beam_search_in_a_graph(B):
         torch.cuda.synchronize()
         for t, e in zip((d.table, d.lens, d.refs, d.data, pos), eager):
             assert torch.equal(t, e)
+
+
+@pytest.mark.parametrize("page", [1, 4])
+def test_more_tokens_than_numbers(B, page):
+    """Counts whose sum with the length passes 32 bits."""
+    d = Device(B, 3, 4, 20, page)
+    d.extend([0], [3], 1)
+    assert d.extend([1, 0], [1, 2**31 - 1]) == [-1, -1]
+    assert d.extend([1, 2], [2**31 - 1] * 2) == [-1, -1]
+    d.check()
+
+
+@pytest.mark.parametrize("dt,order", [("f32", "slots"), ("bf16", "heads")])
+def test_pages_of_several_chunks(B, dt, order):
+    """Pages of more than 32 KB, whose copies are cut."""
+    d = Device(B, 6, 2, 9, 150, planes=3, kv=3, dim=104, dt=dt, order=order, gap=8)
+    d.extend([3, 0], [50, 201], 1)   # numbers up to 253 are exact in bf16 too
+    d.fork([0, 0], [1, 2])
+    d.extend([1, 2, 0], [0, 2, 1])
+    d.release([3])
+    d.compact()
+    d.check()
