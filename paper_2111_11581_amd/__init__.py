@@ -331,7 +331,6 @@ def _on_device(**arrays):
             raise ValueError(f"{name} must be on the device")
 
 
-@functools.lru_cache(maxsize=1024)
 def _plane_layout(key: bytes, name: str, shape, strides, dtype):
     """Keys or values of one layer: pages of the cache."""
     cache = CacheShape.from_buffer_copy(key)
@@ -345,12 +344,18 @@ def _plane_layout(key: bytes, name: str, shape, strides, dtype):
 
 
 @functools.lru_cache(maxsize=4096)
-def _heads_layout(key: bytes, name: str, shape, strides, dtype, n: int, heads: int) -> _Strides:
-    """Strides of an [n, heads, head_dim] array of the cache's type."""
+def _layouts(key: bytes, names, n: int, heads: int, *arrays):
+    """Strides of two [n, heads, head_dim] arrays of the cache's type; `arrays` are their, the keys'
+    and the values' shape, strides and type."""
     cache = CacheShape.from_buffer_copy(key)
-    if tuple(shape) != (n, heads, cache.head_dim) or dtype.itemsize != _esize(cache.dtype):
-        raise ValueError(f"{name} must be [{n}, {heads}, {cache.head_dim}] of the cache's type")
-    return _Strides(*strides)
+    out = []
+    for name, shape, strides, dtype in zip(names, arrays[0::3], arrays[1::3], arrays[2::3]):
+        if tuple(shape) != (n, heads, cache.head_dim) or dtype.itemsize != _esize(cache.dtype):
+            raise ValueError(f"{name} must be [{n}, {heads}, {cache.head_dim}] of the cache's type")
+        out.append(_Strides(*strides))
+    _plane_layout(key, "keys", *arrays[6:9])
+    _plane_layout(key, "values", *arrays[9:])
+    return out
 
 
 def _table(table):
@@ -409,10 +414,8 @@ def bsp_q4_linear(rows: int, cols: int, group: int, batch: int, in_dt: int, out_
 def bsp_cache_append(cache: CacheShape, k, v, keys, values, table, pos, rows=None, stream=None):
     """k and v: [tokens, kv_heads, head_dim] of any strides."""
     n, key = k.shape[0], bytes(cache)
-    ks = _heads_layout(key, "k", k.shape, k.stride(), k.dtype, n, cache.kv_heads)
-    vs = _heads_layout(key, "v", v.shape, v.stride(), v.dtype, n, cache.kv_heads)
-    _plane_layout(key, "keys", keys.shape, keys.stride(), keys.dtype)
-    _plane_layout(key, "values", values.shape, values.stride(), values.dtype)
+    ks, vs = _layouts(key, ("k", "v"), n, cache.kv_heads, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
     if not (k.is_cuda and v.is_cuda and keys.is_cuda and values.is_cuda):
         _on_device(k=k, v=v, keys=keys, values=values)
     seqs, width = _table(table)
@@ -442,10 +445,8 @@ def bsp_attention(cache: CacheShape, q, keys, values, table, lens, y, scale: flo
                   workspace=None, stream=None):
     """q and y: [batch, heads, head_dim] of any strides (y's elements distinct)."""
     (batch, heads, _), key = q.shape, bytes(cache)
-    qs = _heads_layout(key, "q", q.shape, q.stride(), q.dtype, batch, heads)
-    ys = _heads_layout(key, "y", y.shape, y.stride(), y.dtype, batch, heads)
-    _plane_layout(key, "keys", keys.shape, keys.stride(), keys.dtype)
-    _plane_layout(key, "values", values.shape, values.stride(), values.dtype)
+    qs, ys = _layouts(key, ("q", "y"), batch, heads, q.shape, q.stride(), q.dtype, y.shape, y.stride(), y.dtype,
+                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
     if not (q.is_cuda and y.is_cuda and keys.is_cuda and values.is_cuda):
         _on_device(q=q, y=y, keys=keys, values=values)
     seqs, width = _table(table)
