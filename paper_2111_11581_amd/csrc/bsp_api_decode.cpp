@@ -102,6 +102,7 @@ bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batc
     // offsets in x, and in the codes of 64 rows, are 32-bit numbers of bytes
     if ((int64_t)cols * batch > (int64_t)UINT32_MAX / esize(in_dt) || (int64_t)cols * batch > INT32_MAX) return BSP_EUNSUPPORTED;
     if ((int64_t)rows * batch > INT32_MAX || cols > 1 << 26 || rows > 1 << 26) return BSP_EUNSUPPORTED;
+    if (batch > 1 << 19) return BSP_EUNSUPPORTED;   // tiles of 16 vectors are a grid's y
     if (batch == 0) return BSP_OK;
     return status(launch_q4_linear(q4_shape(rows, cols, group), batch, in_dt, out_dt, x, codes, (const uint16_t *)scales,
                                    bias, relu ? 1 : 0, y, S(stream)));

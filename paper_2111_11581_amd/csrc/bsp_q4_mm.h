@@ -266,10 +266,11 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     // mended before it is stored: columns past the last are 0, a load that would end past x has begun
     // earlier and is shifted.
     constexpr int KI = 64 * VE / RS;
-    const int my_k = lane * VE / RS, my_c = lane * VE % RS, base = my_k * B + c0 + (my_c < nc ? my_c : 0);
+    const int my_k = lane * VE / RS, my_c = lane * VE % RS;
     const bool tiny = total < VE;     // not one load: read element by element when stored
     const uint8_t *from = tiny ? a.codes : (const uint8_t *)a.x;
-    const uint32_t last = tiny ? 0 : (uint32_t)(total - VE) * (uint32_t)sizeof(X), lane_at = (uint32_t)base * (uint32_t)sizeof(X);
+    const uint32_t last = tiny ? 0 : (uint32_t)(total - VE) * (uint32_t)sizeof(X), 
+                   lane_at = ((uint32_t)my_k * (uint32_t)B + (uint32_t)(c0 + (my_c < nc ? my_c : 0))) * (uint32_t)sizeof(X);
     u32x4 v[NV];
     auto load = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll

@@ -167,4 +167,5 @@ def test_q4_of_more_than_one_launch_is_refused(L):
     assert L.bsp_q4_dequantize(2048, big, 64, 1, P16, P16, P16, None) == EUNSUPPORTED
     assert L.bsp_q4_linear(big, 64, 64, 1, 1, 1, P16, P16, P16, None, 0, P16, None) == EUNSUPPORTED
     assert L.bsp_q4_linear(64, big, 64, 1, 1, 1, P16, P16, P16, None, 0, P16, None) == EUNSUPPORTED
+    assert L.bsp_q4_linear(1, 1, 64, (1 << 19) + 1, 1, 1, P16, P16, P16, None, 0, P16, None) == EUNSUPPORTED
     assert L.bsp_q4_quantize(2**31 - 1, 1, 64, 1, P16, None, P16, P16, None) == EINVAL

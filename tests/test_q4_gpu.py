@@ -251,3 +251,34 @@ def test_a_pruned_layer_in_4_bits(B):
     B.bsp_q4_linear(rows, cols, 64, batch, B.F32, B.F32, x, codes, sc, None, False, y4)
     PackedLayer(scheme, B.F32, back, mask=mask).linear(x, y, batch, B.F32)
     assert torch.allclose(y4, y, rtol=1e-4, atol=1e-4 * float(y.abs().max()))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [1, 13, 64])
+def test_in_a_graph(B, batch, dt):
+    """Captured once, replayed with other activations and the program's own work in between."""
+    import torch
+    rows, cols, group = 600, 1003, 64
+    nc, ns = B.bsp_q4_sizes(rows, cols, group)
+    gen = torch.Generator(device="cuda").manual_seed(batch)
+    codes = torch.randint(0, 256, (nc,), dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.rand(ns, device="cuda", generator=gen).bfloat16()
+    code, tdt = (B.BF16, torch.bfloat16) if dt == "bf16" else (B.F32, torch.float32)
+    x = torch.zeros(cols, batch, dtype=tdt, device="cuda")
+    y, eager = torch.empty(rows, batch, device="cuda"), torch.empty(rows, batch, device="cuda")
+
+    def call(to):
+        B.bsp_q4_linear(rows, cols, group, batch, code, B.F32, x, codes, scales, None, True, to)
+
+    call(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y)
+    for _ in range(4):
+        x.copy_(torch.randn(cols, batch, device="cuda", generator=gen))
+        y.fill_(float("nan"))
+        call(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager) and eager.abs().sum() > 0
