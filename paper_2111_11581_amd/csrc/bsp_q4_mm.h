@@ -407,8 +407,11 @@ hipError_t q4_run(Q4Args a, hipStream_t st) {
 // Workgroup shapes.  One vector: a wave has four chunks in flight, so no more waves than fill them
 // (1024 x 1024 4.1 us with 8 waves, 3.1 with 2).  More: with few row tiles, as many workgroups as make
 // one for each CU (1024 x 1024, 64 vectors: 4.2 us in 16-vector tiles, 5.3 in one of 64; 4096 x 4096
-// 23 and 10.5); with many, two row tiles a wave and four waves, so that each reads x half as often and a
-// CU holds two workgroups (16384 x 4096, 64 vectors 37 -> 24 us, 16 vectors 15.7 -> 12.4).
+// 23 and 10.5).  Beyond one for each CU, the next would be as long again: two row tiles a wave, which
+// also reads x half as often (4200 x 4096, 7 vectors 13.8 -> 10.8 us; 8000 x 8000, 50 vectors 34 -> 25),
+// or, where 16 vectors have few chunks, four waves (4099 x 1003, 13 vectors 7.6 -> 6.2, with two row
+// tiles 6.8).  With many, both, and a CU holds two workgroups (16384 x 4096, 64 vectors 37 -> 24 us, 16
+// vectors 15.7 -> 12.4).
 template <typename X, int G>
 hipError_t q4_pick(Q4Args a, hipStream_t st) {
     const int n_chunks = (a.s.cols + kQ4Chunk - 1) / kQ4Chunk;
@@ -428,8 +431,10 @@ hipError_t q4_pick(Q4Args a, hipStream_t st) {
         return q4_run<X, G, 1, 4>(a, st);
     } else {
         const int nt = a.batch <= 16 || groups(16) <= 256 ? 1 : a.batch <= 32 || groups(32) <= 256 ? 2 : 4;
-        const bool many = groups(16 * nt) >= (nt == 1 ? 1024 : 512);
-        if (many) a.waves = std::min(4, n_chunks);
+        const int64_t n = groups(16 * nt);
+        const bool most = n >= (nt == 1 ? 1024 : 512), few = nt == 1 && n_chunks < 16;
+        const bool many = most || (n > 256 && !few);
+        if (most || (n > 256 && few)) a.waves = std::min(4, n_chunks);
         if (nt == 1) return many ? q4_run<X, G, 1, 2>(a, st) : q4_run<X, G, 1, 1>(a, st);
         if (nt == 2) return many ? q4_run<X, G, 2, 2>(a, st) : q4_run<X, G, 2, 1>(a, st);
         return many ? q4_run<X, G, 4, 2>(a, st) : q4_run<X, G, 4, 1>(a, st);
