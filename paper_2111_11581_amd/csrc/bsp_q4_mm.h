@@ -245,7 +245,11 @@ template <typename X, int NT, int MT> constexpr int q4_wave_lds() {
     constexpr int stage = q4_stage<X, NT>() * 16 * NT * 2 * q4_parts<X>(), join = 16 * NT * (16 * MT + 4) * 4;
     return stage > join ? stage : join;
 }
-template <typename X, int G, int NT, int MT>
+//  * ODD: an odd number of bf16 vectors, all in one tile.  Every other row then begins in the middle of
+//    a 32-bit word, where loads are slow (4096 x 4096, 7 vectors 8.6 us, 8 vectors 5.6).  They are made
+//    from the word's beginning, one element early, and shifted when stored; what a lane lacks at its
+//    end is in the first word of the next lane (6.2 us; 8000 x 8000, 3 vectors 16.6 -> 12.0).
+template <typename X, int G, int NT, int MT, bool ODD>
 __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     constexpr int PARTS = q4_parts<X>(), STAGE = q4_stage<X, NT>(), WLDS = q4_wave_lds<X, NT, MT>();
     constexpr int RS = 16 * NT, PLANE = STAGE * RS, VE = 16 / sizeof(X), NV = PLANE / VE / 64;   // loads of a lane and stage
@@ -270,7 +274,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     const bool tiny = total < VE;     // not one load: read element by element when stored
     const uint8_t *from = tiny ? a.codes : (const uint8_t *)a.x;
     const uint32_t last = tiny ? 0 : (uint32_t)(total - VE) * (uint32_t)sizeof(X), 
-                   lane_at = ((uint32_t)my_k * (uint32_t)B + (uint32_t)(c0 + (my_c < nc ? my_c : 0))) * (uint32_t)sizeof(X);
+                   lane_at = ((uint32_t)my_k * (uint32_t)B + (uint32_t)(c0 + (my_c < nc ? my_c : 0))) * (uint32_t)sizeof(X) &
+                             (ODD ? ~3u : ~0u);
     u32x4 v[NV];
     auto load = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
@@ -278,18 +283,28 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
             __builtin_memcpy(&v[i], from + min(lane_at + (uint32_t)(k0 + i * KI) * (uint32_t)B * (uint32_t)sizeof(X), last), 16);
         asm volatile("" ::: "memory");   // the loads stay here, a stage ahead of their use
     };
+    auto straighten = [&](u32x4 &w) __attribute__((always_inline)) {   // KI is even: a lane's rows are all odd or all even
+        const uint32_t next = __builtin_amdgcn_update_dpp(0, w[0], 0x101, 0xf, 0xf, true);   // the next lane's first word
+        const int shift = my_k % 2 * 16;
+        w = (u32x4){__builtin_amdgcn_alignbit(w[1], w[0], shift), __builtin_amdgcn_alignbit(w[2], w[1], shift),
+                    __builtin_amdgcn_alignbit(w[3], w[2], shift), __builtin_amdgcn_alignbit(next, w[3], shift)};
+    };
     auto mend = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int k = k0 + my_k + i * KI;
             const bool in = k < cols && my_c < nc;
-            if (tiny) {
-                alignas(16) X e[VE];
+            const uint32_t off = lane_at + (uint32_t)(k0 + i * KI) * (uint32_t)B * (uint32_t)sizeof(X);
+            if (ODD || tiny) {
+                if (ODD) straighten(v[i]);
+                if (!in) v[i] = (u32x4){0, 0, 0, 0};
+                if (in && (!ODD || off + 16 > last)) {   // ODD: this load or the next lane's has begun earlier
+                    alignas(16) X e[VE];
 #pragma unroll
-                for (int j = 0; j < VE; ++j) e[j] = in && my_c + j < nc ? ((const X *)a.x)[k * B + c0 + my_c + j] : (X)0;
-                __builtin_memcpy(&v[i], e, 16);
+                    for (int j = 0; j < VE; ++j) e[j] = my_c + j < nc ? ((const X *)a.x)[k * B + c0 + my_c + j] : (X)0;
+                    __builtin_memcpy(&v[i], e, 16);
+                }
             } else {
-                const uint32_t off = lane_at + (uint32_t)(k0 + i * KI) * (uint32_t)B * (uint32_t)sizeof(X);
                 unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v[i]);
                 w = in ? w >> (8 * (off - min(off, last))) : 0;
                 v[i] = __builtin_bit_cast(u32x4, w);
@@ -297,7 +312,11 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
         }
     };
     auto store = [&](int k0) __attribute__((always_inline)) {
-        if (k0 + STAGE > cols || (int64_t)(k0 + STAGE - 1) * B + c0 + (nc + VE - 1) / VE * VE > total) mend(k0);
+        if (k0 + STAGE > cols || (int64_t)(k0 + STAGE - 1) * B + c0 + (nc + VE - 1) / VE * VE > total)
+            mend(k0);
+        else if constexpr (ODD)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) straighten(v[i]);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int k = my_k + i * (64 * VE / RS);
@@ -391,16 +410,18 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     }
 }
 
-template <typename X, int G, int NT, int MT>
+template <typename X, int G, int NT, int MT, bool ODD = false>
 hipError_t q4_run(Q4Args a, hipStream_t st) {
+    if constexpr (sizeof(X) == 2 && !ODD)
+        if (a.batch % 2 && a.batch < 16 * NT && (uintptr_t)a.x % 4 == 0) return q4_run<X, G, NT, MT, true>(a, st);
     constexpr int lds = q4_wave_lds<X, NT, MT>();
     if (kQ4Waves * lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+        const hipError_t e = hipFuncSetAttribute((const void *)k_q4<X, G, NT, MT, ODD>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  kQ4Waves * lds);
         if (e != hipSuccess) return e;
     }
     const dim3 grid((unsigned)div_up64(a.s.rows, 16 * MT), (unsigned)((a.batch + 16 * NT - 1) / (16 * NT)));
-    k_q4<X, G, NT, MT><<<grid, 64 * a.waves, a.waves * lds, st>>>(a);
+    k_q4<X, G, NT, MT, ODD><<<grid, 64 * a.waves, a.waves * lds, st>>>(a);
     return hipGetLastError();
 }
 

@@ -282,3 +282,34 @@ def test_in_a_graph(B, batch, dt):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, eager) and eager.abs().sum() > 0
+
+
+def between_nan(B, x, dt, before):
+    """x on the device, `before` elements after the start of an array of NaN that goes on after it."""
+    import torch
+    room = torch.full((before + x.size + 64,), float("nan"), dtype=torch.bfloat16 if dt == "bf16" else torch.float32, device="cuda")
+    out = room[before:before + x.size].view(x.shape)
+    out.copy_(tens(x, dt))
+    return out
+
+
+@pytest.mark.parametrize("before", [0, 2, 3])
+@pytest.mark.parametrize("cols", [1, 2, 3, 5, 31, 127, 128, 129, 131, 255, 257])
+@pytest.mark.parametrize("batch", [3, 5, 7, 9, 15, 17, 25, 31, 33, 41, 63, 65])
+def test_odd_batches(B, batch, cols, before):
+    """Rows of bf16 vectors that begin in the middle of a word, up to the last of x."""
+    rows, group = 20, [32, 64, 128][cols % 3]
+    n, scales = weights(rows, cols, group, cols)
+    x, _ = inputs(rows, cols, batch, "bf16", batch)
+    y = run_linear(B, n, scales, group, between_nan(B, x, "bf16", before), "bf16", "f32", None, False)
+    check_linear(y.double().cpu().numpy(), n, scales, group, x.astype(np.float64), "f32", None, False)
+
+
+@pytest.mark.parametrize("rows,cols", [(4100, 300), (4112, 2050), (8200, 1003), (16400, 140)])
+@pytest.mark.parametrize("batch", [3, 13, 16, 30, 31, 33, 61, 64])
+def test_more_tiles_than_workgroups_at_once(B, rows, cols, batch):
+    group = [32, 64, 128][batch % 3]
+    n, scales = weights(rows, cols, group, rows)
+    x, bias = inputs(rows, cols, batch, "bf16", batch)
+    y = run_linear(B, n, scales, group, between_nan(B, x, "bf16", 0), "bf16", "f32", tens(bias, "f32"), False)
+    check_linear(y.double().cpu().numpy(), n, scales, group, x.astype(np.float64), "f32", bias, False)
