@@ -1,5 +1,6 @@
-// FC layers with 4-bit weights and group scales: quantise, read back, launches.  Format (bsp.h): code n stands for scale * (n - 8); codes two to a byte in rows of
-// `stride` bytes, scales bf16 [group][row].
+// FC layers with 4-bit weights and group scales: quantise, read back, launches.  Format (bsp.h): code
+// n stands for scale * (n - 8); codes two to a byte in rows of `stride` bytes, scales bf16
+// [group][row].
 #include <hip/hip_runtime.h>
 
 #include "bsp_decode.h"
@@ -22,57 +23,53 @@ struct Place {
     }
 };
 
-// Eight elements from column `col` of a row, as they are in memory.  VEC: rows begin at multiples of
-// 16 bytes, so a vector of 16 bytes is inside or outside as a whole.
-template <typename E, bool VEC> struct Eight {
-    static constexpr int V = sizeof(E) / 2, N = 16 / sizeof(E);
-    u32x4 v[V];
-    __device__ __forceinline__ void load(const E *row, int64_t col, int64_t cols) {
-        if constexpr (VEC) {
+// Eight elements of a row (of w, or of the mask) from column `col` on, as they are in memory.  VEC: rows
+// of w begin at multiples of 16 bytes, so that a vector is inside or outside as a whole; what is
+// outside is read at the row's start.  Else all eight at once at whatever alignment, and one by one
+// only at a row's end (3000 x 4001 bf16 there and back 37 us one by one, 29.5 so; 4096 x 4096 fp32 without
+// VEC 40, with it 35).
+template <typename T, bool VEC, int BYTES> struct Eight {
+    typedef uint32_t Raw __attribute__((ext_vector_type(BYTES / 4)));
+    static constexpr int V = 8 * sizeof(T) / BYTES, N = 8 / V;   // vectors, elements of each
+    Raw v[V];
+    __device__ __forceinline__ void load(const T *row, int64_t col, int64_t cols) {
+        if (VEC) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = *(const u32x4 *)(row + (col + i * N < cols ? col + i * N : 0));
+            for (int i = 0; i < V; ++i) v[i] = *(const Raw *)(row + (col + i * N < cols ? col + i * N : 0));
+        } else if (col + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) __builtin_memcpy(&v[i], row + col + i * N, BYTES);
         } else {
-            E e[8];
+            T e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = row[col + i < cols ? col + i : 0];
             __builtin_memcpy(v, e, sizeof e);
         }
     }
-    __device__ __forceinline__ void store(E *row, int64_t col, int64_t cols) const {
-        if constexpr (VEC) {
+    __device__ __forceinline__ void store(T *row, int64_t col, int64_t cols) const {
+        if (VEC) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (col + i * N < cols) *(u32x4 *)(row + col + i * N) = v[i];
+                if (col + i * N < cols) *(Raw *)(row + col + i * N) = v[i];
+        } else if (col + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) __builtin_memcpy(row + col + i * N, &v[i], BYTES);
         } else {
-            E e[8];
+            T e[8];
             __builtin_memcpy(e, v, sizeof e);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (col + i < cols) row[col + i] = e[i];
         }
     }
-    __device__ __forceinline__ float get(int i) const {
-        if constexpr (sizeof(E) == 4) return __uint_as_float(v[i / 4][i % 4]);
-        else return bf16_to_f32((uint16_t)(v[0][i / 2] >> (i % 2 * 16)));
-    }
+    __device__ __forceinline__ uint32_t word(int i) const { return v[i / N][i % N * sizeof(T) / 4]; }
 };
-
-// The mask of eight elements, a byte each.
-template <bool VEC> struct Eight8 {
-    uint32_t v[2];
-    __device__ __forceinline__ void load(const uint8_t *row, int64_t col, int64_t cols) {
-        if constexpr (VEC) {   // rows begin at multiples of 4 bytes
-#pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] = *(const uint32_t *)(row + (col + 4 * i < cols ? col + 4 * i : 0));
-        } else {
-            uint8_t e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = row[col + i < cols ? col + i : 0];
-            __builtin_memcpy(v, e, 8);
-        }
-    }
-    __device__ __forceinline__ bool get(int i) const { return v[i / 4] >> (i % 4 * 8) & 255; }
-};
+template <bool VEC> __device__ __forceinline__ float element(const Eight<float, VEC, 16> &e, int i) {
+    return __uint_as_float(e.word(i));
+}
+template <bool VEC> __device__ __forceinline__ float element(const Eight<uint16_t, VEC, 16> &e, int i) {
+    return bf16_to_f32((uint16_t)(e.word(i) >> (i % 2 * 16)));
+}
 
 // The largest |w| of a group goes over its 4, 8 or 16 threads by lane exchanges, so w is read once and
 // codes and scales are written once: bound by that traffic (4096 x 4096 fp32: 76 MB in 18.2 us, 4.2 TB/s;
@@ -82,16 +79,16 @@ __global__ __launch_bounds__(256) void k_q4_quantize(Q4Shape s, const E *__restr
                                                      uint8_t *__restrict__ codes, uint16_t *__restrict__ scales) {
     const Place at(s);
     const int64_t row = at.row, col = at.col, from = min(row, s.rows - 1ll) * s.cols;
-    Eight<E, VEC> x;
+    Eight<E, VEC, 16> x;
     x.load(w + from, col, s.cols);
-    Eight8<VEC> m;
+    Eight<uint8_t, VEC, 4> m;   // with VEC, cols is a multiple of 4
     if constexpr (MASK) m.load(mask + from, col, s.cols);
     const int n = row < s.rows ? (int)min((int64_t)8, s.cols - col) : 0;
     float v[8], top = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        v[i] = i < n ? x.get(i) : 0.f;
-        if constexpr (MASK) v[i] = m.get(i) ? v[i] : 0.f;
+        v[i] = i < n ? element(x, i) : 0.f;
+        if constexpr (MASK) v[i] = m.word(i) >> (i % 4 * 8) & 255 ? v[i] : 0.f;
         top = fmaxf(top, fabsf(v[i]));
     }
     for (int d = 1; d < s.group / 8; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -132,7 +129,7 @@ __global__ __launch_bounds__(256) void k_q4_dequantize(Q4Shape s, const uint8_t 
     E e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = from_f32<E>((float)((int)(packed >> (4 * i) & 15) - 8) * sf);
-    Eight<E, VEC> y;
+    Eight<E, VEC, 16> y;
     __builtin_memcpy(y.v, e, sizeof e);
     y.store(w + at.row * s.cols, at.col, s.cols);
 }
