@@ -25,9 +25,10 @@ struct Place {
 
 // Eight elements of a row (of w, or of the mask) from column `col` on, as they are in memory.  VEC: rows
 // of w begin at multiples of 16 bytes, so that a vector is inside or outside as a whole; what is
-// outside is read at the row's start.  Else all eight at once at whatever alignment, and one by one
-// only at a row's end (3000 x 4001 bf16 there and back 37 us one by one, 29.5 so; 4096 x 4096 fp32 without
-// VEC 40, with it 35).
+// outside is read at the row's start, and since nothing is read again, past the caches (4096 x 4096
+// fp32 there and back 31 us, through them 33.5).  Else all eight at once at whatever alignment, and
+// one by one only at a row's end (3000 x 4001 bf16 37 us one by one, 29.5 so; without VEC the first
+// takes 40).
 template <typename T, bool VEC, int BYTES> struct Eight {
     typedef uint32_t Raw __attribute__((ext_vector_type(BYTES / 4)));
     static constexpr int V = 8 * sizeof(T) / BYTES, N = 8 / V;   // vectors, elements of each
@@ -35,7 +36,7 @@ template <typename T, bool VEC, int BYTES> struct Eight {
     __device__ __forceinline__ void load(const T *row, int64_t col, int64_t cols) {
         if (VEC) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = *(const Raw *)(row + (col + i * N < cols ? col + i * N : 0));
+            for (int i = 0; i < V; ++i) v[i] = __builtin_nontemporal_load((const Raw *)(row + (col + i * N < cols ? col + i * N : 0)));
         } else if (col + 8 <= cols) {
 #pragma unroll
             for (int i = 0; i < V; ++i) __builtin_memcpy(&v[i], row + col + i * N, BYTES);
@@ -72,7 +73,7 @@ template <bool VEC> __device__ __forceinline__ float element(const Eight<uint16_
 }
 
 // The largest |w| of a group goes over its 4, 8 or 16 threads by lane exchanges, so w is read once and
-// codes and scales are written once: bound by that traffic (4096 x 4096 fp32: 76 MB in 18.2 us, 4.2 TB/s;
+// codes and scales are written once: bound by that traffic (4096 x 4096 fp32: 76 MB in 16 us, 4.7 TB/s;
 // 512 x 4608 bf16 with a mask 4.7 us).
 template <typename E, bool VEC, bool MASK>
 __global__ __launch_bounds__(256) void k_q4_quantize(Q4Shape s, const E *__restrict__ w, const uint8_t *__restrict__ mask,
