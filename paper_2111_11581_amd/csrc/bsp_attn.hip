@@ -14,7 +14,7 @@
 // The running maximum and sum of the softmax are kept per head (per lane); the sum of a lane's own
 // tokens is added over lanes at the end.  It is bound by reading keys and values: of a CU's cycles,
 // at 9 bytes each, a step of 32 tokens of 128 dimensions needs 1820, and its 16 products 256 (131072
-// tokens of 8 key heads, 537 MB: 97 to 100 us; 32 sequences of up to 2048 tokens, 134 MB: 36; a few short
+// tokens of 8 key heads, 537 MB: 88 us; 32 sequences of up to 2048 tokens, 134 MB: 36; a few short
 // sequences: the latency of length, entry, key, value and join, 4.4 for 77 tokens).
 #include <hip/hip_runtime.h>
 
@@ -161,6 +161,12 @@ __device__ __forceinline__ Cut cut_up(const AttnArgs &a, int32_t *s_before, int3
     return c;
 }
 
+// ONCE: past the caches.
+template <bool ONCE, typename T> __device__ __forceinline__ T fetch(const T *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
 // What a wave loads and multiplies in one step, for head_dim up to DP.
 template <typename E, int DP> struct Step;
 
@@ -176,7 +182,7 @@ template <int DP> struct Step<uint16_t, DP> {
         for (int c = 0; c < NK; ++c) q[c] = *(const u32x4 *)(row + c * 32 + quad * 8);
     }
     // places of tokens r and 16 + r
-    template <bool FULL> __device__ __forceinline__ void load_k(const uint16_t *keys, const int64_t *ko, int quad, int D) {
+    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_k(const uint16_t *keys, const int64_t *ko, int quad, int D) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -184,18 +190,18 @@ template <int DP> struct Step<uint16_t, DP> {
                 if (!FULL && DP < 256 && c * 32 >= D) break;
                 const int d = c * 32 + quad * 8;
                 const bool in = FULL || d < D;
-                k[t][c] = *(const u32x4 *)(keys + max(ko[t], (int64_t)0) + (in ? d : 0));
+                k[t][c] = fetch<ONCE>((const u32x4 *)(keys + max(ko[t], (int64_t)0) + (in ? d : 0)));
                 if (!in) k[t][c] = (u32x4){0, 0, 0, 0};
             }
     }
     // places of tokens 4 quad + i and 16 + 4 quad + i
-    template <bool FULL> __device__ __forceinline__ void load_v(const uint16_t *values, const int64_t *vo, int r, int D) {
+    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_v(const uint16_t *values, const int64_t *vo, int r, int D) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int h = 0; h < NV; ++h) {
                 const int d = h * 16 * VW + r * VW;
-                v[i][h] = *(const VRaw *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0));
+                v[i][h] = fetch<ONCE>((const VRaw *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0)));
             }
     }
     __device__ __forceinline__ void clear_v(uint32_t dead) {
@@ -245,23 +251,23 @@ template <int DP> struct Step<float, DP> {
 #pragma unroll
         for (int c = 0; c < NK; ++c) q[c] = *(const f32x4 *)(row + c * 16 + quad * 4);
     }
-    template <bool FULL> __device__ __forceinline__ void load_k(const float *keys, const int64_t *ko, int quad, int D) {
+    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_k(const float *keys, const int64_t *ko, int quad, int D) {
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
             if (!FULL && DP < 256 && c * 16 >= D) break;
             const int d = c * 16 + quad * 4;
             const bool in = FULL || d < D;
-            k[c] = *(const f32x4 *)(keys + max(ko[0], (int64_t)0) + (in ? d : 0));
+            k[c] = fetch<ONCE>((const f32x4 *)(keys + max(ko[0], (int64_t)0) + (in ? d : 0)));
             if (!in) k[c] = (f32x4){0, 0, 0, 0};
         }
     }
-    template <bool FULL> __device__ __forceinline__ void load_v(const float *values, const int64_t *vo, int r, int D) {
+    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_v(const float *values, const int64_t *vo, int r, int D) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int h = 0; h < NV; ++h) {
                 const int d = h * 64 + r * 4;
-                v[i][h] = *(const f32x4 *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0));
+                v[i][h] = fetch<ONCE>((const f32x4 *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0)));
             }
     }
     __device__ __forceinline__ void clear_v(uint32_t dead) {
@@ -311,7 +317,7 @@ struct Parts {
 // of one key head.  In a segment its waves take the steps in turn and are joined through LDS; a unit
 // of one segment is finished here, others leave (maximum, sum) and outputs of their segments in the
 // workspace.
-template <typename E, int DP, bool FULL, bool SHARED>
+template <typename E, int DP, bool FULL, bool SHARED, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArgs a) {
     typedef Step<E, DP> St;
     constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV, ROW = DP + 4;
@@ -417,7 +423,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
             int64_t ko[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) ko[t] = place[s0 + 16 * t + r];
-            st.template load_k<FULL>(keys, ko, quad, D);
+            st.template load_k<FULL, ONCE>(keys, ko, quad, D);
             asm volatile("" ::: "memory");   // the loads stay ahead of their use
         };
         auto load_v = [&](int s0) __attribute__((always_inline)) {
@@ -430,7 +436,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
                     vo[4 * t + i] = place[s0 + 16 * t + 4 * quad + i];
                     dead |= (vo[4 * t + i] < 0 ? 1u : 0u) << (4 * t + i);
                 }
-            st.template load_v<FULL>(values, vo, r, D);
+            st.template load_v<FULL, ONCE>(values, vo, r, D);
             asm volatile("" ::: "memory");
         };
         float s[TT];
@@ -607,15 +613,15 @@ bool shared(const CacheArgs &c, int batch, int heads, int64_t tokens) {
            batch * (tokens / kBlock + 1 + kCost) <= INT32_MAX;
 }
 
-template <typename E, int DP, bool FULL>
+template <typename E, int DP, bool FULL, bool ONCE>
 hipError_t run(AttnArgs a, bool split, hipStream_t st) {
     const int units = units_of(a.c, a.batch, a.heads);
     if (!split) {
-        k_attn<E, DP, FULL, false><<<units, 64 * kWaves, 0, st>>>(a);
+        k_attn<E, DP, FULL, false, ONCE><<<units, 64 * kWaves, 0, st>>>(a);
         return hipGetLastError();
     }
     a.shares = shares_of(DP);
-    k_attn<E, DP, FULL, true><<<a.shares, 64 * kWaves, 0, st>>>(a);
+    k_attn<E, DP, FULL, true, ONCE><<<a.shares, 64 * kWaves, 0, st>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const int heads = a.batch * a.heads;
     if (heads < 256)   // few heads: more workgroups for each
@@ -623,6 +629,17 @@ hipError_t run(AttnArgs a, bool split, hipStream_t st) {
     else
         k_attn_join<E, 32><<<dim3(heads, (a.c.head_dim + 127) / 128), 256, 0, st>>>(a);
     return hipGetLastError();
+}
+
+// Keys and values that are read once (one head group) go past the caches where they could not stay in
+// them from one call to the next, half of the last-level one being the bound: 131072 tokens of 8 key
+// heads, 537 MB, take 94.6 us past them and 107 through them, 64 sequences of up to 6000 tokens 94 and
+// 104; 64 sequences of up to 600 tokens, 41 MB that are still there, 27.4 and 23.5.
+constexpr int64_t kLarge = 128 << 20;   // bytes
+template <typename E, int DP, bool FULL>
+hipError_t run(const AttnArgs &a, bool split, hipStream_t st) {
+    const bool once = a.head_groups == 1 && 2 * a.c.pages * a.c.page_stride * (int64_t)sizeof(E) > kLarge;
+    return once ? run<E, DP, FULL, true>(a, split, st) : run<E, DP, FULL, false>(a, split, st);
 }
 
 template <typename E>

@@ -63,3 +63,12 @@ def test_a_long_sequence_whose_scores_are_all_nan_at_one_end(B, dt):
     bad = torch.isnan(y).any(2)
     assert bad.tolist() == [[False, False, True, True], [False] * 4]
     assert torch.isnan(lse).tolist() == bad.tolist()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("tokens", [0, 3000])
+def test_caches_too_large_to_stay(B, dim, tokens, dt):
+    """Few tokens far apart, in the whole and cut."""
+    s = Wide(B, [1, 17, 0, 300, 130], 2, 6, dim, 16, dt, "heads", tokens, seed=dim, page_gap=1 << 20)
+    s.check(*s.run(dim ** -0.5), dim ** -0.5)
