@@ -72,3 +72,10 @@ def test_caches_too_large_to_stay(B, dim, tokens, dt):
     """Few tokens far apart, in the whole and cut."""
     s = Wide(B, [1, 17, 0, 300, 130], 2, 6, dim, 16, dt, "heads", tokens, seed=dim, page_gap=1 << 20)
     s.check(*s.run(dim ** -0.5), dim ** -0.5)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [8 * 64, 9 * 64 - 1, 9 * 64, 9 * 64 + 1, 8 * 128, 9 * 128 - 1, 9 * 128, 9 * 128 + 1])
+def test_lengths_about_a_few_steps(B, tokens, dt):
+    s = Wide(B, [tokens, 0, 1, tokens - 1, tokens // 2], 1, 3, 24, 1, dt, "heads", tokens, seed=tokens)
+    s.check(*s.run(0.2), 0.2)
