@@ -13,7 +13,7 @@
 //    values), dimension j of every lane makes one operand.
 // The running maximum and sum of the softmax are kept per head (per lane); the sum of a lane's own
 // tokens is added over lanes at the end.  It is bound by reading keys and values: of a CU's cycles,
-// at 9 bytes each, a step of 32 tokens of 128 dimensions needs 1820, and its 16 products 256 (131072
+// at 9 bytes each, a step of 32 tokens of 128 dimensions needs 1820, and its 24 products 384 (131072
 // tokens of 8 key heads, 537 MB: 88 us; 32 sequences of up to 2048 tokens, 134 MB: 36; a few short
 // sequences: the latency of length, entry, key, value and join, 4.4 for 77 tokens).
 #include <hip/hip_runtime.h>
@@ -224,19 +224,27 @@ template <int DP> struct Step<uint16_t, DP> {
             for (int i = 0; i < 4; ++i) s[4 * t + i] = c4[i];
         }
     }
-    // Probabilities are rounded to bf16 here: their product runs on bf16 operands.
+    // A probability is the sum of two bf16, of which it keeps 16 bits (to 2^-16 of it): the second product
+    // costs nothing that shows beneath the reads, and one rounded to a single bf16 would add as much
+    // error as the output's own rounding.
     __device__ __forceinline__ void outputs(const float *p, f32x4 (*acc)[VW]) const {
-        const u32x4 b = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+        u32x4 b[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            b[0][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+            b[1][i] = pack_bf16(p[2 * i] - bf16_to_f32(b[0][i]), p[2 * i + 1] - __uint_as_float(b[0][i] & 0xffff0000u));
+        }
 #pragma unroll
         for (int h = 0; h < NV; ++h)
 #pragma unroll
             for (int j = 0; j < VW; ++j) {
                 const uint32_t sel = j % 2 ? 0x07060302u : 0x05040100u;
-                uint32_t w[4];
+                u32x4 w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][h][j / 2], v[2 * i][h][j / 2], sel);
-                acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8((u32x4){w[0], w[1], w[2], w[3]}),
-                                                                    as_bf16x8(b), acc[h][j], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(b[i]), acc[h][j], 0, 0, 0);
             }
     }
 };
