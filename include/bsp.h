@@ -284,9 +284,9 @@ bsp_status bsp_q4_dequantize(int32_t rows, int32_t cols, int32_t group, bsp_dtyp
 
 /* Forward of an FC layer with such weights, on feature-major activations as bsp_linear:
  *   y[o][b] = bias[o] + sum_g scales[g][o] * sum_{k in g} (code(o, k) - 8) * x[k][b], then ReLU if relu.
- * Made for small batches (decoding), right for larger ones.  Sums are in fp32 (x of BSP_F32 is
- * multiplied in full), codes count as 0 .. 15 in a group's partial sums, so |x| has to stay below
- * 2^119; an Inf or NaN makes every output of its batch column NaN.  No workspace.  rows and cols up to
+ * Made for small batches (decoding), right for larger ones.  Sums are in fp32 of exact products
+ * (x of BSP_F32 counts in full, in three parts, of which an Inf makes NaN): a weight of 0 adds exactly
+ * 0, however large its x.  A group's sum must not pass 2^128: |x| below 2^125.  No workspace.  rows and cols up to
  * 2^26, batch up to 2^19, rows * batch and cols * batch below 2^31 and x below 2^32 bytes; else
  * BSP_EUNSUPPORTED.  Async. */
 bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batch, bsp_dtype in_dt, bsp_dtype out_dt,

@@ -32,3 +32,43 @@ def test_bf16_probabilities_keep_16_bits(B, lens, kv, heads, dim):
             ref, _, size, _, qk = M.attention(s.q[b, h], s.keys[:, :, j], s.values[:, :, j], s.table[b], 16, n, 0, scale)
             small = 2 * 2 * (dim + 4) * M.U24 * qk + (2 * n + 64) * M.U24
             assert (np.abs(y[b, h] - ref) <= 2.0 ** -8 * np.abs(ref) + 1.01 * (2.0 ** -16 + small) * size).all(), (b, h)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,group", [(40, 300, 32), (64, 1003, 64), (100, 4096, 128)])
+@pytest.mark.parametrize("batch", [1, 2, 5, 16, 33, 64])
+def test_weights_of_0_take_no_part(B, rows, cols, group, batch, dt):
+    """Pruned columns whose activations are 2^60 times the rest.  fp32 sums of exact products, in any
+    order: (cols + 4) 2^-24 of the sum of |w x|, which those columns are not in, with a factor of 2."""
+    import torch
+    rng = np.random.default_rng(rows + batch)
+    mask = (rng.random((rows, cols)) < 0.5).astype(np.uint8)
+    large = rng.permutation(cols)[:7]
+    mask[:, large] = 0
+    n, scales = M.q4_quantize(rng.standard_normal((rows, cols)).astype(np.float32) * 0.05, mask, group)
+    x = rng.standard_normal((cols, batch)).astype(np.float32)
+    x[large] *= 2.0 ** 60
+    x = M.bf16(x) if dt == "bf16" else x
+    y = torch.empty(rows, batch, device="cuda")
+    B.bsp_q4_linear(rows, cols, group, batch, B.BF16 if dt == "bf16" else B.F32, B.F32,
+                    torch.from_numpy(x).to(torch.bfloat16 if dt == "bf16" else torch.float32).cuda(),
+                    torch.from_numpy(M.q4_bytes(n)).cuda(), torch.from_numpy(M.q4_scales(scales)).bfloat16().cuda(), None, False, y)
+    w = M.q4_weights(n, scales, group)
+    ref, size = w @ x.astype(np.float64), np.abs(w) @ np.abs(x.astype(np.float64))
+    assert (np.abs(y.double().cpu().numpy() - ref) <= 2 * (cols + 4) * M.U24 * size).all()
+
+
+@pytest.mark.parametrize("batch", [1, 6, 40])
+def test_an_infinite_bf16_activation_counts_by_its_weight(B, batch):
+    import torch
+    rows, cols, group = 48, 260, 64
+    rng = np.random.default_rng(batch)
+    n, scales = rng.integers(0, 16, (rows, cols)), np.full((M.ceil(cols, group), rows), 0.5, np.float32)
+    x = M.bf16(rng.standard_normal((cols, batch)).astype(np.float32))
+    x[200, batch // 2] = -np.inf
+    y = torch.empty(rows, batch, device="cuda")
+    B.bsp_q4_linear(rows, cols, group, batch, B.BF16, B.F32, torch.from_numpy(x).bfloat16().cuda(),
+                    torch.from_numpy(M.q4_bytes(n)).cuda(), torch.from_numpy(M.q4_scales(scales)).bfloat16().cuda(), None, False, y)
+    with np.errstate(invalid="ignore"):
+        want = (M.q4_weights(n, scales, group)[:, 200] * -np.inf).astype(np.float32)
+    assert np.array_equal(y.cpu().numpy()[:, batch // 2], want, equal_nan=True)
