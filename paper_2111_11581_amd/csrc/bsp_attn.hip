@@ -616,10 +616,15 @@ int units_of(const CacheArgs &c, int batch, int heads) {
 // dimensions 48.4 and 46.9.  A few: 8 units of 8 steps 16.8 uncut and 14.5 cut, but in calls by
 // themselves 17.3 and 18.9 (64 units of up to 7 steps 17.8 and 19.2); 8 units of 12 steps 22 and 14.5.
 constexpr int kFew = 8, kMany = 16;
-bool shared(const CacheArgs &c, int batch, int heads, int64_t tokens) {
+// What pays, of sequences of up to `tokens` tokens: never for fewer tokens where not for more.
+bool worth_cutting(const CacheArgs &c, int batch, int heads, int64_t tokens) {
     const int64_t steps = tokens / (c.dtype == BSP_F32 ? 64 : 128);
-    return batch <= kMostSeqs && steps > (units_of(c, batch, heads) < 256 ? kFew : kMany) &&
-           batch * (tokens / kBlock + 1 + kCost) <= INT32_MAX;
+    return batch <= kMostSeqs && steps > (units_of(c, batch, heads) < 256 ? kFew : kMany);
+}
+// And 32-bit numbers count the blocks of all sequences.  A window may bring them within these again: the
+// workspace goes by what may be worth cutting alone.
+bool shared(const CacheArgs &c, int batch, int heads, int64_t tokens) {
+    return worth_cutting(c, batch, heads, tokens) && batch * (tokens / kBlock + 1 + kCost) <= INT32_MAX;
 }
 
 template <typename E, int DP, bool FULL, bool ONCE>
@@ -671,9 +676,9 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
 }
 
 // First share and number of segments of every unit; maximum, sum and head_dim outputs of every
-// segment, at most shares + units, for each head of a group
+// segment, at most shares + units, for each head of a group.  Enough for every window.
 int64_t attention_workspace(const CacheArgs &c, int batch, int heads, int width) {
-    if (!shared(c, batch, heads, (int64_t)width * c.page_size)) return 0;
+    if (!worth_cutting(c, batch, heads, (int64_t)width * c.page_size)) return 0;
     const int64_t units = units_of(c, batch, heads), segments = kMostShares + units;
     return units * 8 + segments * std::min(16, heads / c.kv_heads) * (c.head_dim + 2) * 4;
 }

@@ -1,0 +1,43 @@
+"""Windows of attention where the work is cut up: their first tokens lie inside pages, pieces and shares."""
+
+import numpy as np
+import pytest
+
+from tests import decode_model as M
+from tests.test_attention_shares_gpu import Wide
+from tests.test_paged_attention_gpu import B, Setup   # noqa: F401 (B is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+class Far(Setup):
+    """Sequences whose last tokens lie in two pages each, after a long part of the table that is gone."""
+
+    def __init__(self, B, lens, width, page, dt, window, seed):
+        import torch
+        rng = np.random.default_rng(seed)
+        self.B, self.lens, self.kv, self.heads, self.dim, self.page, self.dt, self.order = B, lens, 1, 2, 8, page, dt, "heads"
+        self.width, self.window = width, window
+        rnd = M.bf16 if dt == "bf16" else (lambda a: a)
+        self.keys, self.values = (rnd(rng.standard_normal((2, page, 1, 8)).astype(np.float32)) for _ in range(2))
+        self.q = rnd(rng.standard_normal((len(lens), 2, 8)).astype(np.float32))
+        self.table = np.full((len(lens), width), -1, np.int64)
+        for b, n in enumerate(lens):
+            last = (n - 1) // page
+            self.table[b, last] = b % 2
+            if last:
+                self.table[b, last - 1] = 1 - b % 2
+        self.tdt = torch.bfloat16 if dt == "bf16" else torch.float32
+        self.dkeys, self.dvalues = self.plane(self.keys, 0), self.plane(self.values, 0)
+        self.cache = B.CacheShape.of(self.dkeys)
+        self.dtable, self.dlens = self.ints(self.table), self.ints(lens)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_over_very_long_tables(B, dt):
+    """64 sequences in tables for 2^30 tokens each."""
+    rng = np.random.default_rng(5)
+    lens = rng.integers(1, 1 << 30, 64)
+    lens[:4] = [1, 4095, 4097, 1 << 30]
+    s = Far(B, lens.tolist(), 1 << 14, 1 << 16, dt, 4096, 5)
+    s.check(*s.run(0.35, 4096), 0.35, 4096)
