@@ -105,6 +105,7 @@ class PagedCache:
         n = seqs if longest is None else longest
         self.scratch = torch.empty(bsp_cache_scratch(self.shape, seqs, width, n), dtype=torch.uint8, device=device)
         self.workspace = torch.empty(0, dtype=torch.uint8, device=device)
+        self._outgrown = []
 
     def extend(self, rows, counts, pos, stream=None):
         """Room for counts[i] more tokens in sequence rows[i]; pos receives where they begin, or -1."""
@@ -115,10 +116,13 @@ class PagedCache:
         bsp_cache_append(self.shape, k, v, keys, values, self.table, pos, rows, stream)
 
     def reserve(self, batch: int, heads: int):
-        """A workspace for attend with `batch` sequences; attend makes one where this was not called
-        (which a graph capture cannot)."""
+        """A workspace for attend with `batch` sequences; attend makes one where this was not called.
+        Captured graphs and calls under way hold the one they were given, so that it lives as long as
+        the cache does; each is at least twice the one before, and all before take no more than it."""
         need = bsp_attention_workspace(self.shape, batch, heads, self.table.shape[1])
         if self.workspace.numel() < need:
+            self._outgrown.append(self.workspace)
+            need = max(need, 2 * self.workspace.numel())
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
 
     def attend(self, layer: int, q, y, scale: float, rows=None, window: int = 0, lse=None, stream=None):
