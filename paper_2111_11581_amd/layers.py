@@ -6,6 +6,8 @@ HIP kernels behind the C ABI.
 
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import (BF16, F32, HEAD_MAJOR, CacheShape, ConvShape, Scheme, bsp_attention, bsp_attention_workspace,
@@ -14,6 +16,16 @@ from . import (BF16, F32, HEAD_MAJOR, CacheShape, ConvShape, Scheme, bsp_attenti
                bsp_q4_linear, bsp_q4_quantize, bsp_q4_sizes, bsp_unpack)
 
 TORCH_DT = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _made_on(stream, device):
+    """Arrays that a call on ``stream`` writes are made on it: torch gives out memory that earlier work
+    of its current stream may still be using, which only that stream's own later work waits for."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
+    return torch.cuda.stream(stream)
 
 
 class PackedLayer:
@@ -34,21 +46,24 @@ class PackedLayer:
         dev = w.device
         R, C = self.scheme.rows, self.scheme.cols
         if mask is None:
-            mask = torch.empty(R * C, dtype=torch.uint8, device=dev)
+            with _made_on(stream, dev):
+                mask = torch.empty(R * C, dtype=torch.uint8, device=dev)
             bsp_prune(self.scheme, wdt, w, mask, stream)
         self.mask = mask
         nv, ni, nr, nb = bsp_packed_sizes(self.scheme, self.conv, wdt)
-        self.values = torch.empty(max(nv, 1), dtype=TORCH_DT[wdt], device=dev)
-        self.indices = torch.empty(max(ni, 1), dtype=torch.int32, device=dev)
-        self.rowptr = torch.empty(max(nr, 1), dtype=torch.int32, device=dev)
-        self.tiles = torch.empty(nb, dtype=torch.uint8, device=dev)
+        with _made_on(stream, dev):
+            self.values = torch.empty(max(nv, 1), dtype=TORCH_DT[wdt], device=dev)
+            self.indices = torch.empty(max(ni, 1), dtype=torch.int32, device=dev)
+            self.rowptr = torch.empty(max(nr, 1), dtype=torch.int32, device=dev)
+            self.tiles = torch.empty(nb, dtype=torch.uint8, device=dev)
         self.n_values, self.n_indices, self.n_rowptr = nv, ni, nr
         bsp_pack(self.scheme, wdt, w, mask, self.values, self.indices, self.rowptr, self.tiles,
                  self.conv, stream)
 
     def unpack(self, stream=None) -> torch.Tensor:
         R, C = self.scheme.rows, self.scheme.cols
-        out = torch.empty(R * C, dtype=TORCH_DT[self.wdt], device=self.tiles.device)
+        with _made_on(stream, self.tiles.device):
+            out = torch.empty(R * C, dtype=TORCH_DT[self.wdt], device=self.tiles.device)
         bsp_unpack(self.scheme, self.wdt, self.values, self.indices, self.rowptr, out, stream)
         return out
 
@@ -69,12 +84,14 @@ class QuantLayer:
                  stream=None):
         self.rows, self.cols, self.group = rows, cols, group
         nc, ns = bsp_q4_sizes(rows, cols, group)
-        self.codes = torch.empty(nc, dtype=torch.uint8, device=w.device)
-        self.scales = torch.empty(ns, dtype=torch.bfloat16, device=w.device)
+        with _made_on(stream, w.device):
+            self.codes = torch.empty(nc, dtype=torch.uint8, device=w.device)
+            self.scales = torch.empty(ns, dtype=torch.bfloat16, device=w.device)
         bsp_q4_quantize(rows, cols, group, wdt, w, mask, self.codes, self.scales, stream)
 
     def dequantize(self, wdt: int = F32, stream=None) -> torch.Tensor:
-        out = torch.empty(self.rows, self.cols, dtype=TORCH_DT[wdt], device=self.codes.device)
+        with _made_on(stream, self.codes.device):
+            out = torch.empty(self.rows, self.cols, dtype=TORCH_DT[wdt], device=self.codes.device)
         bsp_q4_dequantize(self.rows, self.cols, self.group, wdt, self.codes, self.scales, out, stream)
         return out
 
@@ -89,7 +106,7 @@ class PagedCache:
 
     Tables, lengths and counts are on the device and are never read by the host; lists are int32
     tensors on the device.  The scratch is the cache's own, so its calls belong on one stream (or on
-    streams that wait for each other).
+    streams that wait for each other); it is made on torch's current stream.
     """
 
     def __init__(self, layers: int, seqs: int, width: int, pages: int, page_size: int, kv_heads: int, head_dim: int,
@@ -115,7 +132,7 @@ class PagedCache:
         keys, values = self.planes[layer]
         bsp_cache_append(self.shape, k, v, keys, values, self.table, pos, rows, stream)
 
-    def reserve(self, batch: int, heads: int):
+    def reserve(self, batch: int, heads: int, stream=None):
         """A workspace for attend with `batch` sequences; attend makes one where this was not called.
         Captured graphs and calls under way hold the one they were given, so that it lives as long as
         the cache does; each is at least twice the one before, and all before take no more than it."""
@@ -123,11 +140,12 @@ class PagedCache:
         if self.workspace.numel() < need:
             self._outgrown.append(self.workspace)
             need = max(need, 2 * self.workspace.numel())
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
+            with _made_on(stream, self.table.device):
+                self.workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
 
     def attend(self, layer: int, q, y, scale: float, rows=None, window: int = 0, lse=None, stream=None):
         """Attention of one token of each sequence rows[i] over what its pages hold."""
-        self.reserve(q.shape[0], q.shape[1])
+        self.reserve(q.shape[0], q.shape[1], stream)
         keys, values = self.planes[layer]
         bsp_attention(self.shape, q, keys, values, self.table, self.lens, y, scale, window, rows, lse, self.workspace, stream)
 

@@ -67,3 +67,33 @@ def test_a_graph_after_a_larger_batch():
         torch.cuda.synchronize()
         assert torch.allclose(y.float(), want.float(), atol=2e-2) and torch.allclose(lse, want_lse, atol=1e-4)
         assert all(bool((o == 7).all()) for o in others)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("handle", [False, True])
+def test_what_a_call_on_another_stream_makes(handle):
+    """Memory that the current stream gave back while its own work there is still to come is not what a
+    call on another stream writes its results to."""
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2111_11581_amd as B
+    from paper_2111_11581_amd.layers import PackedLayer, QuantLayer
+    rows, cols = 256, 512
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    w = torch.randn(rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    scheme = B.Scheme(rows, cols, 16, 32, B.COL, 4)
+    quant, packed = QuantLayer(rows, cols, 64, B.F32, w), PackedLayer(scheme, B.F32, w)
+    want = [quant.codes, quant.scales, quant.dequantize(), packed.mask, packed.tiles, packed.unpack()]
+    torch.cuda.synchronize()
+    left = [torch.empty(t.nbytes, dtype=torch.uint8, device="cuda") for t in want for _ in range(4)]
+    torch.cuda._sleep(100_000_000)   # some 50 ms
+    for t in left:
+        t.fill_(0xA5)
+    del left, t
+    q, p = QuantLayer(rows, cols, 64, B.F32, w, stream=stream), PackedLayer(scheme, B.F32, w, stream=stream)
+    got = [q.codes, q.scales, q.dequantize(stream=stream), p.mask, p.tiles, p.unpack(stream=stream)]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
