@@ -73,7 +73,10 @@ class CacheShape(ctypes.Structure):
         [pages, page_size, kv_heads, head_dim] (SLOT_MAJOR), each page contiguous."""
         pages, a, b, dim = plane.shape
         heads, slots = (a, b) if order == HEAD_MAJOR else (b, a)
-        c = cls({4: F32, 2: BF16}[plane.element_size()], order, pages, slots, heads, dim,
+        code = next((c for c, t in _float_types().items() if t is plane.dtype), None)
+        if code is None:
+            raise ValueError(f"plane must be of fp32 or bf16, not {plane.dtype}")
+        c = cls(code, order, pages, slots, heads, dim,
                 plane.stride(0) if pages > 1 else 0)
         _plane_layout(bytes(c), "plane", plane.shape, plane.stride(), plane.dtype)
         _on_device(plane=plane)
@@ -306,12 +309,25 @@ def bsp_maxpool2x2(dt: int, n: int, c: int, h: int, w: int, x, y, stream=None):
 _int32 = None
 
 
-def _dev(name: str, t, nbytes: int):
-    """A contiguous device array of at least `nbytes`."""
+_types = {}   # torch's types by their codes
+
+
+def _float_types():
+    if not _types:
+        import torch
+        _types.update({F32: torch.float32, BF16: torch.bfloat16})
+    return _types
+
+
+def _dev(name: str, t, nbytes: int, dt=None):
+    """A contiguous device array of at least `nbytes`; not of another floating-point type than dt
+    (bits in arrays of integers are taken as they are)."""
     if t is None or t.nbytes < nbytes or not t.is_contiguous():
         _need(name, t, nbytes)
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the device")
+    if dt is not None and t.dtype is not _types.get(dt) and t.dtype is not _float_types().get(dt) and t.is_floating_point():
+        raise ValueError(f"{name} must be of the type that the call names, not {t.dtype}")
 
 
 def _ints(name: str, t, n: int):
@@ -334,7 +350,7 @@ def _on_device(**arrays):
 def _plane_layout(key: bytes, name: str, shape, strides, dtype):
     """Keys or values of one layer: pages of the cache."""
     cache = CacheShape.from_buffer_copy(key)
-    if tuple(shape) != cache.plane_shape() or dtype.itemsize != _esize(cache.dtype):
+    if tuple(shape) != cache.plane_shape() or dtype is not _float_types().get(cache.dtype):
         raise ValueError(f"{name} is not an array of the cache's pages")
     d = cache.head_dim
     page = cache.kv_heads * cache.page_size * d
@@ -350,7 +366,7 @@ def _layouts(key: bytes, names, n: int, heads: int, *arrays):
     cache = CacheShape.from_buffer_copy(key)
     out = []
     for name, shape, strides, dtype in zip(names, arrays[0::3], arrays[1::3], arrays[2::3]):
-        if tuple(shape) != (n, heads, cache.head_dim) or dtype.itemsize != _esize(cache.dtype):
+        if tuple(shape) != (n, heads, cache.head_dim) or dtype is not _float_types().get(cache.dtype):
             raise ValueError(f"{name} must be [{n}, {heads}, {cache.head_dim}] of the cache's type")
         out.append(_Strides(*strides))
     _plane_layout(key, "keys", *arrays[6:9])
@@ -379,12 +395,12 @@ _q4_sizes = functools.lru_cache(maxsize=4096)(bsp_q4_sizes)
 def _q4_arrays(rows, cols, group, codes, scales):
     nc, ns = _q4_sizes(rows, cols, group)
     _dev("codes", codes, nc)
-    _dev("scales", scales, ns * 2)
+    _dev("scales", scales, ns * 2, BF16)
 
 
 def bsp_q4_quantize(rows: int, cols: int, group: int, wdt: int, w, mask, codes, scales, stream=None):
     _q4_arrays(rows, cols, group, codes, scales)
-    _dev("w", w, rows * cols * _esize(wdt))
+    _dev("w", w, rows * cols * _esize(wdt), wdt)
     if mask is not None:
         _dev("mask", mask, rows * cols)
     _check("bsp_q4_quantize", lib().bsp_q4_quantize(rows, cols, group, wdt, _p(w), _p(mask), _p(codes), _p(scales),
@@ -393,7 +409,7 @@ def bsp_q4_quantize(rows: int, cols: int, group: int, wdt: int, w, mask, codes, 
 
 def bsp_q4_dequantize(rows: int, cols: int, group: int, wdt: int, codes, scales, w, stream=None):
     _q4_arrays(rows, cols, group, codes, scales)
-    _dev("w", w, rows * cols * _esize(wdt))
+    _dev("w", w, rows * cols * _esize(wdt), wdt)
     _check("bsp_q4_dequantize", lib().bsp_q4_dequantize(rows, cols, group, wdt, _p(codes), _p(scales), _p(w),
                                                         _stream(stream)))
 
@@ -401,10 +417,10 @@ def bsp_q4_dequantize(rows: int, cols: int, group: int, wdt: int, codes, scales,
 def bsp_q4_linear(rows: int, cols: int, group: int, batch: int, in_dt: int, out_dt: int, x, codes, scales, bias,
                   relu: bool, y, stream=None):
     _q4_arrays(rows, cols, group, codes, scales)
-    _dev("x", x, cols * batch * _esize(in_dt))
-    _dev("y", y, rows * batch * _esize(out_dt))
+    _dev("x", x, cols * batch * _esize(in_dt), in_dt)
+    _dev("y", y, rows * batch * _esize(out_dt), out_dt)
     if bias is not None:
-        _dev("bias", bias, rows * 4)
+        _dev("bias", bias, rows * 4, F32)
     st = lib().bsp_q4_linear(rows, cols, group, batch, in_dt, out_dt, x.data_ptr(), codes.data_ptr(), scales.data_ptr(),
                              _p(bias), 1 if relu else 0, y.data_ptr(), _stream(stream))
     if st:
@@ -454,7 +470,7 @@ def bsp_attention(cache: CacheShape, q, keys, values, table, lens, y, scale: flo
     if rows is not None:
         _ints("rows", rows, batch)
     if lse is not None:
-        _dev("lse", lse, batch * heads * 4)
+        _dev("lse", lse, batch * heads * 4, F32)
     need = _workspace(key, batch, heads, width)
     if need:
         _dev("workspace", workspace, need)

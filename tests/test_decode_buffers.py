@@ -1,4 +1,5 @@
-"""Buffers that QuantLayer and PagedCache make: how long they live, and on whose stream they are."""
+"""Buffers of the decode operators: their types, and how long those live that QuantLayer and PagedCache
+make, and on whose stream."""
 
 import weakref
 
@@ -97,3 +98,63 @@ def test_what_a_call_on_another_stream_makes(handle):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.gpu
+def test_the_default_stream_by_its_handle():
+    """Handle 0, while another stream is torch's current one."""
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2111_11581_amd as B
+    from paper_2111_11581_amd.layers import QuantLayer
+    w = torch.randn(64, 96, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    want = QuantLayer(64, 96, 32, B.F32, w)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = QuantLayer(64, 96, 32, B.F32, w, stream=torch.cuda.default_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
+
+
+@pytest.mark.gpu
+def test_arrays_of_another_type_than_the_call_names():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2111_11581_amd as B
+
+    def zeros(*shape, t=torch.bfloat16):
+        return torch.zeros(*shape, dtype=t, device="cuda")
+    nc, ns = B.bsp_q4_sizes(16, 32, 32)
+    good = dict(x=zeros(32, 4), codes=zeros(nc, t=torch.uint8), scales=zeros(ns), bias=zeros(16, t=torch.float32), y=zeros(16, 4))
+
+    def linear(**kw):
+        a = {**good, **kw}
+        B.bsp_q4_linear(16, 32, 32, 4, B.BF16, B.BF16, a["x"], a["codes"], a["scales"], a["bias"], False, a["y"])
+    linear()
+    linear(x=good["x"].view(torch.int16), y=good["y"].view(torch.uint8))   # bits as they are
+    for name, t in (("x", torch.float16), ("x", torch.float32), ("scales", torch.float16), ("scales", torch.float32),
+                    ("bias", torch.float64), ("y", torch.float16), ("y", torch.float32)):
+        with pytest.raises(ValueError, match="type"):
+            linear(**{name: good[name].to(t)})
+    w = zeros(16, 32)
+    for t in (torch.float16, torch.float32):
+        for f in (lambda w: B.bsp_q4_quantize(16, 32, 32, B.BF16, w, None, good["codes"], good["scales"]),
+                  lambda w: B.bsp_q4_dequantize(16, 32, 32, B.BF16, good["codes"], good["scales"], w)):
+            f(w)
+            with pytest.raises(ValueError, match="type"):
+                f(w.to(t))
+    plane, table, lens = zeros(4, 2, 16, 64), zeros(1, 1, t=torch.int32), zeros(1, t=torch.int32)
+    cache = B.CacheShape.of(plane)
+
+    def attention(q=zeros(1, 4, 64), keys=plane, lse=zeros(1, 4, t=torch.float32)):
+        B.bsp_attention(cache, q, keys, plane, table, lens, zeros(1, 4, 64), 1.0, lse=lse)
+    attention()
+    for kw in (dict(q=zeros(1, 4, 64, t=torch.float16)), dict(keys=plane.half()), dict(lse=zeros(1, 4, t=torch.float64))):
+        with pytest.raises(ValueError):
+            attention(**kw)
+    with pytest.raises(ValueError):
+        B.bsp_cache_append(cache, zeros(1, 2, 64), zeros(1, 2, 64, t=torch.float16), plane, plane, table, lens)
+    with pytest.raises(ValueError):
+        B.bsp_cache_copy(cache, zeros(2, 4, 2, 16, 64, t=torch.float16), lens, lens)

@@ -32,3 +32,28 @@ def test_the_workspace_grows_with_the_table(B, L, batch, kv, heads, dtype):
     c = cache(B, dtype=dtype, kv_heads=kv, page_size=64)
     sizes = [workspace(L, c, batch, heads, 1 << k) for k in range(25)]
     assert sizes == sorted(sizes)
+
+
+def test_types_of_the_same_size_are_told_apart(B):
+    import torch
+    plane = torch.zeros(4, 2, 16, 64)
+    for dtype in (torch.float16, torch.int16, torch.int32, torch.float64, torch.uint8):
+        with pytest.raises(ValueError, match="fp32 or bf16"):
+            B.CacheShape.of(plane.to(dtype))
+    for code, right, wrong in ((B.BF16, torch.bfloat16, (torch.float16, torch.int16, torch.uint16, torch.float32)),
+                               (B.F32, torch.float32, (torch.int32, torch.bfloat16, torch.uint32))):
+        key = bytes(B.CacheShape(code, B.HEAD_MAJOR, 4, 16, 2, 64, 0))
+        page = (tuple(plane.shape), plane.stride())
+        B._plane_layout(key, "keys", *page, right)
+        B._planes_layout(key, (3, *plane.shape), (plane.numel(), *plane.stride()), right)
+        q = ((5, 2, 64), (128, 64, 1))
+        B._layouts(key, ("q", "y"), 5, 2, *q, right, *q, right, *page, right, *page, right)
+        for dtype in wrong:
+            with pytest.raises(ValueError, match="pages"):
+                B._plane_layout(key, "keys", *page, dtype)
+            with pytest.raises(ValueError, match="pages"):
+                B._planes_layout(key, (3, *plane.shape), (plane.numel(), *plane.stride()), dtype)
+            for i in range(4):
+                types = [dtype if j == i else right for j in range(4)]
+                with pytest.raises(ValueError):
+                    B._layouts(key, ("q", "y"), 5, 2, *q, types[0], *q, types[1], *page, types[2], *page, types[3])
