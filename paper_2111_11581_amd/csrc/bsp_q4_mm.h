@@ -290,7 +290,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
             if (ODD || tiny) {
                 if (ODD) straighten(v[i]);
                 if (!in) v[i] = (u32x4){0, 0, 0, 0};
-                if (in && (!ODD || off + 16 > last)) {   // ODD: this load or the next lane's has begun earlier
+                // ODD: this load or the next lane's has begun earlier (off + 16 may pass 2^32)
+                if (in && (!ODD || off > last || last - off < 16)) {
                     alignas(16) X e[VE];
 #pragma unroll
                     for (int j = 0; j < VE; ++j) e[j] = my_c + j < nc ? ((const X *)a.x)[k * B + c0 + my_c + j] : (X)0;

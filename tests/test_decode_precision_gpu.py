@@ -72,3 +72,27 @@ def test_an_infinite_bf16_activation_counts_by_its_weight(B, batch):
     with np.errstate(invalid="ignore"):
         want = (M.q4_weights(n, scales, group)[:, 200] * -np.inf).astype(np.float32)
     assert np.array_equal(y.cpu().numpy()[:, batch // 2], want, equal_nan=True)
+
+
+def test_odd_batches_up_to_the_last_byte_of_4_gb(B):
+    """x of 2^32 - 4 bytes: 32-bit offsets of bytes reach within 16 of their end.  As many rows as it
+    takes for 33 vectors to be one tile: 67 GB of codes."""
+    import torch
+    rows, batch, cols, group = 2049, 33, 65075262, 128
+    assert batch * cols == 2 ** 31 - 2
+    nc, ns = B.bsp_q4_sizes(rows, cols, group)
+    if torch.cuda.mem_get_info()[0] < nc + (16 << 30):
+        pytest.skip("not enough memory left")
+    x = torch.zeros(cols, batch, dtype=torch.bfloat16, device="cuda")
+    near = torch.arange(1, 8 * batch + 1, device="cuda").view(8, batch)
+    x[-8:] = (near % 251 - 125).bfloat16()
+    codes = torch.full((nc,), 0x88, dtype=torch.uint8, device="cuda")
+    at = (cols - 8) // 2
+    codes.view(rows, -1)[:, at:at + 4] = torch.tensor([0xA9, 0xCB, 0xED, 0x7F], dtype=torch.uint8, device="cuda")
+    scales, y = torch.ones(ns, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, batch, device="cuda")
+    B.bsp_q4_linear(rows, cols, group, batch, B.BF16, B.F32, x, codes, scales, None, False, y)
+    w = torch.tensor([9, 10, 11, 12, 13, 14, 15, 7], dtype=torch.float64) - 8
+    want = w @ x[-8:].double().cpu()
+    assert torch.equal(y.double().cpu(), want.expand(rows, -1))
+    del x, codes, scales
+    torch.cuda.empty_cache()
