@@ -318,7 +318,8 @@ typedef struct {
 /* Writes the keys k and values v of n tokens (strides ks, vs; dtype of the cache) into the cache:
  * token i goes to position pos[i] of sequence rows[i] (rows NULL: i).  A token whose position is
  * negative, past the table or in an entry that holds nothing, or whose sequence is not in
- * 0 .. seqs - 1, is not written.  No two tokens may share a place.  Async. */
+ * 0 .. seqs - 1, is not written.  No two tokens may share a place.  k and v (and below, q and y) are
+ * aligned to their elements.  Async. */
 bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, const bsp_strides *ks, const void *v,
                             const bsp_strides *vs, void *keys, void *values, const int32_t *table, int32_t seqs,
                             int32_t width, const int32_t *rows_or_null, const int32_t *pos, void *stream);

@@ -114,6 +114,7 @@ bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, co
     if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
     if (n < 0 || !ks || !vs || !keys || !values || !aligned(keys, 16) || !aligned(values, 16)) return BSP_EINVAL;
     if (n > 0 && (!k || !v || !pos)) return BSP_EINVAL;
+    if (!aligned(k, esize(cache->dtype)) || !aligned(v, esize(cache->dtype))) return BSP_EINVAL;
     if (const bsp_status st = check_table(table, seqs, width, cache->page_size); st != BSP_OK) return st;
     if (n == 0 || (int64_t)seqs * width == 0) return BSP_OK;
     AppendArgs a;
@@ -139,6 +140,7 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
     if (batch < 0 || heads < 1 || heads % cache->kv_heads || window < 0 || !qs || !ys) return BSP_EINVAL;
     if (!keys || !values || !aligned(keys, 16) || !aligned(values, 16)) return BSP_EINVAL;
     if (batch > 0 && (!q || !y || (!lens && seqs > 0))) return BSP_EINVAL;
+    if (!aligned(q, esize(cache->dtype)) || !aligned(y, esize(cache->dtype)) || !aligned(lse, 4)) return BSP_EINVAL;
     if (const bsp_status st = check_table(table, seqs, width, cache->page_size); st != BSP_OK) return st;
     if ((int64_t)batch * heads > INT32_MAX / 256) return BSP_EUNSUPPORTED;
     if (batch == 0) return BSP_OK;

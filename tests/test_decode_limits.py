@@ -57,3 +57,12 @@ def test_types_of_the_same_size_are_told_apart(B):
                 types = [dtype if j == i else right for j in range(4)]
                 with pytest.raises(ValueError):
                     B._layouts(key, ("q", "y"), 5, 2, *q, types[0], *q, types[1], *page, types[2], *page, types[3])
+
+
+@pytest.mark.parametrize("dtype,off", [(0, 1), (0, 2), (0, 3), (1, 1)])
+def test_arrays_are_aligned_to_their_elements(B, L, dtype, off):
+    c, s, odd = cache(B, dtype=dtype), B._Strides(128, 64, 1), ctypes.c_void_p(4096 + off)
+    for k, v in ((odd, P16), (P16, odd)):
+        assert L.bsp_cache_append(c, 1, k, s, v, s, P16, P16, P16, 1, 4, None, P16, None) == EINVAL
+    for q, y, lse in ((odd, P16, None), (P16, odd, None), (P16, P16, ctypes.c_void_p(4098))):
+        assert L.bsp_attention(c, 1, 2, q, s, P16, P16, P16, 1, 4, None, P16, 1.0, 0, y, s, lse, P16, None) == EINVAL
