@@ -345,7 +345,7 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
  * [seqs][width], lens [seqs], and refs [pages], the number of table entries that name a page (0: the
  * page is free).  Free pages are given out lowest first, so results are unique.  `data` are the
  * planes of a model that share one table (keys and values of every layer): `planes` arrays of pages,
- * plane_stride elements apart.  Rows that are not in 0 .. seqs - 1 are left out; the rows that one
+ * plane_stride elements apart, one after the other or page by page beside each other.  Rows that are not in 0 .. seqs - 1 are left out; the rows that one
  * call changes must differ.  scratch: bsp_cache_scratch bytes (n: the longest list of the calls),
  * 16-byte aligned, whose content does not matter.  All async. */
 bsp_status bsp_cache_scratch(const bsp_cache *cache, int32_t seqs, int32_t width, int32_t n, int64_t *bytes);

@@ -54,7 +54,12 @@ bsp_status check_planes(const bsp_cache *c, int32_t planes, int64_t plane_stride
     if (const bsp_status st = check_cache(c); st != BSP_OK) return st;
     if (!data || planes < 0 || plane_stride < 0 || !aligned(data, 16)) return BSP_EINVAL;
     if (plane_stride % (16 / esize(c->dtype)) || plane_stride > INT64_MAX / 8 / std::max(planes, 1)) return BSP_EINVAL;
-    return BSP_OK;
+    if (planes < 2) return BSP_OK;
+    // no overlap: plane after plane, or the planes' pages side by side within a page's stride
+    const int64_t page = (int64_t)c->page_size * c->kv_heads * c->head_dim, stride = c->page_stride ? c->page_stride : page;
+    const bool after = plane_stride >= (c->pages - 1) * stride + page;
+    const bool beside = plane_stride >= page && (planes - 1) * plane_stride + page <= stride;
+    return after || beside ? BSP_OK : BSP_EINVAL;
 }
 
 PlanesArgs planes_args(const bsp_cache *c, int32_t planes, int64_t plane_stride, void *data) {

@@ -66,3 +66,17 @@ def test_arrays_are_aligned_to_their_elements(B, L, dtype, off):
         assert L.bsp_cache_append(c, 1, k, s, v, s, P16, P16, P16, 1, 4, None, P16, None) == EINVAL
     for q, y, lse in ((odd, P16, None), (P16, odd, None), (P16, P16, ctypes.c_void_p(4098))):
         assert L.bsp_attention(c, 1, 2, q, s, P16, P16, P16, 1, 4, None, P16, 1.0, 0, y, s, lse, P16, None) == EINVAL
+
+
+@pytest.mark.parametrize("planes,stride,page_stride,ok", [
+    (1, 0, 0, True), (0, 0, 0, True), (2, 10 * 2048, 0, True), (2, 10 * 2048 - 8, 0, False), (2, 0, 0, False), (2, 2048, 0, False),
+    (3, 9 * 2560 + 2048, 2560, True), (3, 9 * 2560 + 2040, 2560, False),
+    (4, 2048, 4 * 2048, True), (4, 2048, 4 * 2048 - 8, False), (4, 2040, 4 * 2048, False), (4, 2056, 4 * 2056, True)])
+def test_planes_do_not_overlap(B, L, planes, stride, page_stride, ok):
+    """Ten pages of 2048 elements: plane after plane, or pages of all planes beside each other."""
+    c = cache(B, page_stride=page_stride)
+    want = 0 if ok else EINVAL
+    assert L.bsp_cache_copy(c, planes, stride, P16, 0, None, None, None) == want
+    assert L.bsp_cache_extend(c, planes, stride, P16, 2, 4, P16, P16, P16, 0, None, None, None, None, None) == want
+    if not ok:
+        assert L.bsp_cache_compact(c, planes, stride, P16, 2, 4, P16, P16, P16, P16, None) == EINVAL
