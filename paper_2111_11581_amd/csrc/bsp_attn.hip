@@ -648,11 +648,12 @@ hipError_t run(AttnArgs a, bool split, hipStream_t st) {
 // Keys and values that are read once (one head group) go past the caches where they could not stay in
 // them from one call to the next, half of the last-level one being the bound: 131072 tokens of 8 key
 // heads, 537 MB, take 94.6 us past them and 107 through them, 64 sequences of up to 6000 tokens 94 and
-// 104; 64 sequences of up to 600 tokens, 41 MB that are still there, 27.4 and 23.5.
-constexpr int64_t kLarge = 128 << 20;   // bytes
+// 104; 64 sequences of up to 600 tokens, 41 MB that are still there, 27.4 and 23.5.  How much of a cache
+// is in use only the device knows: the rule goes by its pages, and a large one with few tokens in it
+// takes the slower side (those 27.4).
 template <typename E, int DP, bool FULL>
 hipError_t run(const AttnArgs &a, bool split, hipStream_t st) {
-    const bool once = a.head_groups == 1 && 2 * a.c.pages * a.c.page_stride * (int64_t)sizeof(E) > kLarge;
+    const bool once = a.head_groups == 1 && past_caches(a.c);
     return once ? run<E, DP, FULL, true>(a, split, st) : run<E, DP, FULL, false>(a, split, st);
 }
 

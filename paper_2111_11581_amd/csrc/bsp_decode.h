@@ -46,6 +46,12 @@ inline CacheArgs cache_args(const bsp_cache &c) {
     return a;
 }
 
+// Whether keys and values of a layer span more than half of the last-level cache.
+constexpr int64_t kLarge = 128 << 20;   // bytes
+inline bool past_caches(const CacheArgs &c) {
+    return c.page_stride * c.pages > kLarge / (c.dtype == BSP_F32 ? 8 : 4);
+}
+
 struct AppendArgs {
     CacheArgs c;
     const void *k, *v;
