@@ -41,3 +41,26 @@ def test_over_very_long_tables(B, dt):
     lens[:4] = [1, 4095, 4097, 1 << 30]
     s = Far(B, lens.tolist(), 1 << 14, 1 << 16, dt, 4096, 5)
     s.check(*s.run(0.35, 4096), 0.35, 4096)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("holes", [0.0, 0.3])
+@pytest.mark.parametrize("window", [1000, 1153, 2000])
+@pytest.mark.parametrize("page", [7, 16])
+def test_in_pieces(B, page, window, holes, dt):
+    """Few sequences: a piece of four blocks for each workgroup."""
+    lens = [1, 5000, 999, 1000, 1001, 1153, 1154, 0, 2000, 2001, 3777]
+    s = Wide(B, lens, 2, 6, 64, page, dt, "heads", 5000, seed=window + page, holes=holes)
+    s.check(*s.run(0.125, window), 0.125, window)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("holes", [0.0, 0.3])
+@pytest.mark.parametrize("n,kv,window", [(40, 4, 1153), (40, 4, 2000), (36, 8, 1100), (36, 8, 2200)])
+def test_in_equal_shares(B, n, kv, window, holes, dt):
+    """More pieces than workgroups; with fewer than 256 sequences times key heads, and with more."""
+    rng = np.random.default_rng(n + window)
+    lens = rng.integers(1, 3000, n)
+    lens[:6] = [0, 1, window - 1, window, window + 1, 5000]
+    s = Wide(B, lens.tolist(), kv, kv, 16, 16, dt, "slots", 5000, seed=window, holes=holes)
+    s.check(*s.run(0.25, window), 0.25, window)

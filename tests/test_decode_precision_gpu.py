@@ -96,3 +96,22 @@ def test_odd_batches_up_to_the_last_byte_of_4_gb(B):
     assert torch.equal(y.double().cpu(), want.expand(rows, -1))
     del x, codes, scales
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,cols,batch", [(4112, 300, 16), (8200, 203, 13), (16400, 140, 61), (16400, 140, 64), (16400, 600, 64)])
+def test_fp32_layers_of_many_tiles(B, rows, cols, batch, group):
+    """More tiles than workgroups run at once, and so many that a workgroup has two waves."""
+    import torch
+    rng = np.random.default_rng(rows + cols)
+    n, scales = M.q4_quantize(rng.standard_normal((rows, cols)).astype(np.float32) * 0.05, None, group)
+    x, bias = rng.standard_normal((cols, batch)).astype(np.float32), rng.standard_normal(rows).astype(np.float32) * 0.1
+    room = torch.full((cols * batch + 64,), float("nan"), device="cuda")
+    room[:cols * batch] = torch.from_numpy(x).cuda().view(-1)
+    y = torch.empty(rows, batch, device="cuda")
+    B.bsp_q4_linear(rows, cols, group, batch, B.F32, B.F32, room[:cols * batch], torch.from_numpy(M.q4_bytes(n)).cuda(),
+                    torch.from_numpy(M.q4_scales(scales)).bfloat16().cuda(), torch.from_numpy(bias).cuda(), False, y)
+    w = M.q4_weights(n, scales, group)
+    ref = w @ x.astype(np.float64) + bias[:, None]
+    size = np.abs(w) @ np.abs(x.astype(np.float64)) + np.abs(bias)[:, None]
+    assert (np.abs(y.double().cpu().numpy() - ref) <= 2 * (cols + 4) * M.U24 * size).all()
