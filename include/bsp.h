@@ -293,7 +293,8 @@ bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batc
                          const void *x, const uint8_t *codes, const void *scales, const float *bias_or_null,
                          int32_t relu, void *y, void *stream);
 
-/* Keys and values of the tokens seen so far lie in pages of page_size tokens.  Token t of sequence s
+/* Keys and values of the tokens seen so far lie in pages of page_size tokens.  Lists of sequences or
+ * tokens have fewer than 2^24 entries (a longer one is BSP_EUNSUPPORTED).  Token t of sequence s
  * is slot t % page_size of page table[s][t / page_size]; entries of the table that are negative (or
  * not below `pages`) hold nothing; width * page_size is at most 2^30.  Keys and values of one layer are
  * arrays of `pages` pages each, a page being
@@ -343,7 +344,7 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
 
 /* Care of the pages.  The state is on the device and the host never waits for it: table
  * [seqs][width], lens [seqs], and refs [pages], the number of table entries that name a page (0: the
- * page is free).  Free pages are given out lowest first, so results are unique.  `data` are the
+ * page is free); these calls alone change it, and an entry past a sequence's length names no page.  Free pages are given out lowest first, so results are unique.  `data` are the
  * planes of a model that share one table (keys and values of every layer): `planes` arrays of pages,
  * plane_stride elements apart, one after the other or page by page beside each other.  Rows that are not in 0 .. seqs - 1 are left out; the rows that one
  * call changes must differ.  scratch: bsp_cache_scratch bytes (n: the longest list of the calls),

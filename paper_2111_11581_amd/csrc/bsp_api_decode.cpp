@@ -43,11 +43,13 @@ bsp_status check_table(const int32_t *table, int32_t seqs, int32_t width, int32_
     return (int64_t)width * page_size > kMaxTokens ? BSP_EUNSUPPORTED : BSP_OK;
 }
 
+constexpr int32_t kMostListed = (1 << 24) - 1;   // a workgroup of 256 for each: a launch has fewer than 2^32 threads
+
 bsp_status check_pages(const int32_t *table, const int32_t *lens, const int32_t *refs, int32_t seqs, int32_t width,
                        int32_t pages, int32_t n) {
     if (seqs < 0 || width < 0 || pages < 1 || n < 0 || !refs) return BSP_EINVAL;
     if ((!table && (int64_t)seqs * width > 0) || (!lens && seqs > 0)) return BSP_EINVAL;
-    return BSP_OK;
+    return n > kMostListed ? BSP_EUNSUPPORTED : BSP_OK;
 }
 
 bsp_status check_planes(const bsp_cache *c, int32_t planes, int64_t plane_stride, const void *data) {
@@ -121,6 +123,7 @@ bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, co
     if (n > 0 && (!k || !v || !pos)) return BSP_EINVAL;
     if (!aligned(k, esize(cache->dtype)) || !aligned(v, esize(cache->dtype))) return BSP_EINVAL;
     if (const bsp_status st = check_table(table, seqs, width, cache->page_size); st != BSP_OK) return st;
+    if (n > kMostListed) return BSP_EUNSUPPORTED;
     if (n == 0 || (int64_t)seqs * width == 0) return BSP_OK;
     AppendArgs a;
     a.c = cache_args(*cache);
@@ -162,6 +165,7 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
 bsp_status bsp_cache_scratch(const bsp_cache *cache, int32_t seqs, int32_t width, int32_t n, int64_t *bytes) {
     if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
     if (!bytes || seqs < 0 || width < 0 || n < 0) return BSP_EINVAL;
+    if (n > kMostListed) return BSP_EUNSUPPORTED;
     *bytes = pages_scratch(cache->pages, width, n);
     return BSP_OK;
 }

@@ -5,7 +5,7 @@ import ctypes
 
 import pytest
 
-from tests.test_decode_abi import EINVAL, P16, B, L, cache   # noqa: F401 (B and L are fixtures)
+from tests.test_decode_abi import EINVAL, EUNSUPPORTED, P16, B, L, cache   # noqa: F401 (B and L are fixtures)
 
 
 def workspace(L, c, batch, heads, width):
@@ -80,3 +80,15 @@ def test_planes_do_not_overlap(B, L, planes, stride, page_stride, ok):
     assert L.bsp_cache_extend(c, planes, stride, P16, 2, 4, P16, P16, P16, 0, None, None, None, None, None) == want
     if not ok:
         assert L.bsp_cache_compact(c, planes, stride, P16, 2, 4, P16, P16, P16, P16, None) == EINVAL
+
+
+def test_lists_of_more_than_a_launch_are_refused(B, L):
+    """Before anything is changed: extend has two kernels, the second with a workgroup for each entry."""
+    c, s, n, out, want = cache(B), B._Strides(128, 64, 1), 1 << 24, ctypes.c_int64(), EUNSUPPORTED
+    for m in (n, 2 ** 31 - 1):
+        assert L.bsp_cache_append(c, m, P16, s, P16, s, P16, P16, P16, 1, 4, None, P16, None) == want
+        assert L.bsp_cache_fork(2, 4, 10, P16, P16, P16, m, P16, P16, P16, None) == want
+        assert L.bsp_cache_extend(c, 1, 0, P16, 2, 4, P16, P16, P16, m, P16, P16, P16, P16, None) == want
+        assert L.bsp_cache_release(2, 4, 10, P16, P16, P16, m, P16, None) == want
+        assert L.bsp_cache_scratch(c, 2, 4, m, ctypes.addressof(out)) == want
+    assert L.bsp_cache_scratch(c, 2, 2 ** 31 - 1, n - 1, ctypes.addressof(out)) == 0 and out.value == 4 * (n - 1) << 31
