@@ -610,11 +610,13 @@ int units_of(const CacheArgs &c, int batch, int heads) {
     return batch * c.kv_heads * ((heads / c.kv_heads + 15) / 16);
 }
 // Whether the work is cut into shares: for up to kMostSeqs sequences (more fill the card uncut) that may
-// be of many steps of a workgroup.  Cutting costs a scan of the lengths and a second kernel, some 7 us,
+// be of many steps of a workgroup.  Cutting costs a scan of the lengths and a second kernel, 4 to 10 us,
 // and the host 3 us more for a call.  Units that fill the card are worth more steps: 256 of up to 16
-// steps take 42 us uncut and 46 cut, 64 sequences of up to 600 tokens 24 and 34; up to 20 steps of 64
-// dimensions 48.4 and 46.9.  A few: 8 units of 8 steps 16.8 uncut and 14.5 cut, but in calls by
-// themselves 17.3 and 18.9 (64 units of up to 7 steps 17.8 and 19.2); 8 units of 12 steps 22 and 14.5.
+// steps take 42 us uncut and 41 cut, 64 sequences of up to 600 tokens 24 and 34; up to 20 steps of 64
+// dimensions 48.4 and 46.9.  A few: 8 units of 8 steps 17.1 uncut and 14.3 cut, but in calls by
+// themselves 17.3 and 19.5 (64 units of up to 7 steps 17.8 and 19.2); 8 units of 12 steps 22 and 14.5.
+// Lengths are on the device, so that the rule goes by the table's width: short sequences in wide tables
+// are cut too (1 of 77 tokens 6.9 us in a table as long, 10.6 in one for 8192).
 constexpr int kFew = 8, kMany = 16;
 // What pays, of sequences of up to `tokens` tokens: never for fewer tokens where not for more.
 bool worth_cutting(const CacheArgs &c, int batch, int heads, int64_t tokens) {

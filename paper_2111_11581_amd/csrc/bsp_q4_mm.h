@@ -239,9 +239,9 @@ template <typename X, int NT, int MT> constexpr int q4_wave_lds() {
     return stage > join ? stage : join;
 }
 //  * ODD: an odd number of bf16 vectors, all in one tile.  Every other row then begins in the middle of
-//    a 32-bit word, where loads are slow (4096 x 4096, 7 vectors 8.6 us, 8 vectors 5.6).  They are made
+//    a 32-bit word, where loads are slow (4096 x 4096, 7 vectors 8.6 us, 8 vectors 5.5).  They are made
 //    from the word's beginning, one element early, and shifted when stored; what a lane lacks at its
-//    end is in the first word of the next lane (6.2 us; 8000 x 8000, 3 vectors 16.6 -> 12.0).
+//    end is in the first word of the next lane (6.1 us; 8000 x 8000, 3 vectors 16.6 -> 13.0).
 template <typename X, int G, int NT, int MT, bool ODD>
 __global__ __launch_bounds__(64 * kQ4Waves, 2) void k_q4(Q4Args a) {
     constexpr int PARTS = q4_parts<X>(), STAGE = q4_stage<X, NT>(), WLDS = q4_wave_lds<X, NT, MT>();
@@ -419,13 +419,13 @@ hipError_t q4_run(Q4Args a, hipStream_t st) {
 }
 
 // Workgroup shapes.  One vector: a wave has four chunks in flight, so no more waves than fill them
-// (1024 x 1024 4.1 us with 8 waves, 3.1 with 2).  More: with few row tiles, as many workgroups as make
-// one for each CU (1024 x 1024, 64 vectors: 4.2 us in 16-vector tiles, 5.3 in one of 64; 4096 x 4096
-// 23 and 10.5).  Beyond one for each CU, the next would be as long again: two row tiles a wave, which
-// also reads x half as often (4200 x 4096, 7 vectors 13.8 -> 10.8 us; 8000 x 8000, 50 vectors 34 -> 25),
-// or, where 16 vectors have few chunks, four waves (4099 x 1003, 13 vectors 7.6 -> 6.2, with two row
-// tiles 6.8).  With many, both, and a CU holds two workgroups (16384 x 4096, 64 vectors 37 -> 24 us, 16
-// vectors 15.7 -> 12.4).
+// (1024 x 1024 4.3 us with 8 waves, 3.2 with 2).  More: with few row tiles, as many workgroups as make
+// one for each CU (1024 x 1024, 64 vectors: 4.2 us in 16-vector tiles, 5.1 in one of 64; 4096 x 4096
+// 22 and 10.5).  Beyond one for each CU, the next would be as long again: two row tiles a wave, which
+// also reads x half as often (4200 x 4096, 7 vectors 9.1 -> 8.2 us; 8000 x 8000, 50 vectors 33 -> 23),
+// or, where 16 vectors have few chunks, four waves (4099 x 1003, 13 vectors 6.4 -> 5.0, with two row
+// tiles 6.4).  With many, both, and a CU holds two workgroups (16384 x 4096, 64 vectors 36 -> 24 us, 16
+// vectors 15.7 -> 13.0).
 template <typename X, int G>
 hipError_t q4_pick(Q4Args a, hipStream_t st) {
     const int n_chunks = (a.s.cols + kQ4Chunk - 1) / kQ4Chunk;
@@ -441,7 +441,7 @@ hipError_t q4_pick(Q4Args a, hipStream_t st) {
         const int64_t n = groups(16);
         if (n <= 256) return q4_run<X, G, 1, 1>(a, st);
         if (n <= 512) return q4_run<X, G, 1, 2>(a, st);
-        if (n >= 4096) a.waves = std::min(2, n_chunks);   // 16384 x 4096, 61 vectors: 73 us with 8 waves, 53 with 2
+        if (n >= 4096) a.waves = std::min(2, n_chunks);   // 16384 x 4096, 61 vectors: 76 us with 8 waves, 57 with 2
         return q4_run<X, G, 1, 4>(a, st);
     } else {
         const int nt = a.batch <= 16 || groups(16) <= 256 ? 1 : a.batch <= 32 || groups(32) <= 256 ? 2 : 4;
