@@ -284,11 +284,11 @@ bsp_status bsp_q4_dequantize(int32_t rows, int32_t cols, int32_t group, bsp_dtyp
 
 /* Forward of an FC layer with such weights, on feature-major activations as bsp_linear:
  *   y[o][b] = bias[o] + sum_g scales[g][o] * sum_{k in g} (code(o, k) - 8) * x[k][b], then ReLU if relu.
- * Made for small batches (decoding), right for larger ones.  Sums are in fp32 of exact products
- * (x of BSP_F32 counts in full, in three parts, of which an Inf makes NaN): a weight of 0 adds exactly
- * 0, however large its x.  A group's sum must not pass 2^128: |x| below 2^125.  No workspace.  rows and cols up to
- * 2^26, batch up to 2^19, rows * batch and cols * batch below 2^31 and x below 2^32 bytes; else
- * BSP_EUNSUPPORTED.  Async. */
+ * Made for small batches (decoding), right for larger ones.  Sums are in fp32 of exact products (x of
+ * BSP_F32 counts in full, in three parts, of which an Inf makes NaN): a weight of 0 adds exactly 0,
+ * however large its x.  A group's sum must not pass 2^128: |x| below 2^125.  No workspace.  rows and
+ * cols up to 2^26, batch up to 2^19, rows * batch and cols * batch below 2^31 and x below 2^32 bytes;
+ * else BSP_EUNSUPPORTED.  Async. */
 bsp_status bsp_q4_linear(int32_t rows, int32_t cols, int32_t group, int32_t batch, bsp_dtype in_dt, bsp_dtype out_dt,
                          const void *x, const uint8_t *codes, const void *scales, const float *bias_or_null,
                          int32_t relu, void *y, void *stream);
@@ -344,11 +344,13 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
 
 /* Care of the pages.  The state is on the device and the host never waits for it: table
  * [seqs][width], lens [seqs], and refs [pages], the number of table entries that name a page (0: the
- * page is free); these calls alone change it, and an entry past a sequence's length names no page.  Free pages are given out lowest first, so results are unique.  `data` are the
- * planes of a model that share one table (keys and values of every layer): `planes` arrays of pages,
- * plane_stride elements apart, one after the other or page by page beside each other.  Rows that are not in 0 .. seqs - 1 are left out; the rows that one
- * call changes must differ.  scratch: bsp_cache_scratch bytes (n: the longest list of the calls),
- * 16-byte aligned, whose content does not matter.  All async. */
+ * page is free); these calls alone change it, and an entry past a sequence's length names no page.
+ * Free pages are given out lowest first, so results are unique.  `data` are the planes of a model
+ * that share one table (keys and values of every layer): `planes` arrays of pages, plane_stride
+ * elements apart, one after the other or page by page beside each other.  Rows that are not in 0 ..
+ * seqs - 1 are left out; the rows that one call changes must differ.  scratch: bsp_cache_scratch
+ * bytes (n: the longest list of the calls), 16-byte aligned, whose content does not matter.  All
+ * async. */
 bsp_status bsp_cache_scratch(const bsp_cache *cache, int32_t seqs, int32_t width, int32_t n, int64_t *bytes);
 
 /* Sequence children[i] becomes sequence parents[i]: the same pages, now shared.  All parents are read
