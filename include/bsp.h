@@ -342,6 +342,103 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
                          const int32_t *rows_or_null, const int32_t *lens, float scale, int32_t window, void *y,
                          const bsp_strides *ys, float *lse_or_null, void *workspace, void *stream);
 
+/* Rotary positions.  The first `dims` dimensions of a head are rotated in pairs, pair i of a token at
+ * position p by the angle t = p * freqs[i] (the others are passed on):
+ *   (a, b) -> factor * (a cos t - b sin t, b cos t + a sin t)
+ * freqs: dims / 2 angles a token in fp64, on the device; angles are reduced in fp64 and so hold at far
+ * positions (and negative ones, which turn back). */
+typedef enum {
+    BSP_ROPE_HALF = 0,          /* pair i is dimensions i and i + dims / 2 */
+    BSP_ROPE_INTERLEAVED = 1    /* 2 i and 2 i + 1 */
+} bsp_rope_layout;
+typedef struct {
+    int32_t layout;         /* bsp_rope_layout */
+    int32_t dims;           /* even, 0 .. head_dim */
+    float factor;           /* of what is rotated: 1, or the attention factor of a lengthened context */
+} bsp_rope;
+
+/* Frequencies: freqs[i] = f (r + (1 - r) / factor) with f = base^(-2 i / dims), where r (1: kept, 0: slowed
+ * down by `factor`) is
+ *   BSP_RAMP_NONE   0
+ *   BSP_RAMP_TURNS  (original * f / 2 pi - low) / (high - low), within 0 .. 1: pairs that turn fewer than
+ *                   `low` times in the `original` tokens a model was trained with are slowed down, those
+ *                   of more than `high` kept
+ *   BSP_RAMP_INDEX  1 - (i - a) / (b - a), within 0 .. 1, with c(n) = dims ln(original / 2 pi n) / (2 ln base),
+ *                   a = max(0, floor(c(high))), b = min(dims - 1, ceil(c(low))) (a + 0.001 where b = a): the
+ *                   ramp of YaRN (Peng et al. 2023)
+ * scaling_or_null NULL: f.  freqs is host memory of dims / 2 doubles.  Host-only, pure. */
+typedef enum { BSP_RAMP_NONE = 0, BSP_RAMP_TURNS = 1, BSP_RAMP_INDEX = 2 } bsp_rope_ramp;
+typedef struct {
+    double factor;          /* > 0 */
+    double original;        /* tokens; > 0 for a ramp */
+    double low, high;       /* turns; low < high for a ramp, 0 < low for BSP_RAMP_INDEX */
+    int32_t ramp;           /* bsp_rope_ramp */
+} bsp_rope_scaling;
+bsp_status bsp_rope_freqs(int32_t dims, double base, const bsp_rope_scaling *scaling_or_null, double *freqs);
+
+/* y[i][h] = x[i][h], normed over its head_dim dimensions, rotated to position pos[i], for n tokens (fewer
+ * than 2^24) of `heads` heads (up to 65535) of 1 to 256 dimensions; strides xs and ys.  The norm:
+ *   x / sqrt(mean(x^2) + eps) * norm[d],  norm_or_null of head_dim fp32 (NULL: no norm, eps is not used)
+ * Norm and rotation are in fp32, rounded once to dt (RNE).  y may be x with the same strides; else the two
+ * do not overlap.  x and y are aligned to their elements.  Async. */
+bsp_status bsp_rotary(bsp_dtype dt, const bsp_rope *rope, const double *freqs, int32_t n, int32_t heads,
+                      int32_t head_dim, const void *x, const bsp_strides *xs, const int32_t *pos,
+                      const float *norm_or_null, float eps, void *y, const bsp_strides *ys, void *stream);
+
+/* What a layer does with the queries, keys and values of n new tokens before its attention, in one
+ * launch: q_out = bsp_rotary of q (`heads` heads, q_norm_or_null), and the keys so too (k_norm_or_null)
+ * and the values as they are into the cache, as bsp_cache_append.  pos[i] is the position that token i
+ * is rotated to and written at; a token that has no place is not written (as there), its query is
+ * rotated all the same.  q_out may be q with the same strides.  heads + 2 kv_heads up to 65535.  Async. */
+bsp_status bsp_cache_append_rotary(const bsp_cache *cache, const bsp_rope *rope, const double *freqs, int32_t n,
+                                   int32_t heads, const void *q, const bsp_strides *qs, const void *k,
+                                   const bsp_strides *ks, const void *v, const bsp_strides *vs, void *q_out,
+                                   const bsp_strides *qos, const float *q_norm_or_null, const float *k_norm_or_null,
+                                   float eps, void *keys, void *values, const int32_t *table, int32_t seqs,
+                                   int32_t width, const int32_t *rows_or_null, const int32_t *pos, void *stream);
+
+/* bsp_attention for sequences that share their first tokens, as bsp_cache_fork leaves them: what a group
+ * shares is read once for all of its members.  Group g is entries starts[g] to starts[g + 1] - 1 of the
+ * batch (starts: groups + 1 int32 on the device, ascending; entries outside every group share nothing).
+ * Its members attend to tokens 0 .. shared[g] - 1 in the pages of sequence prefix_rows[g] (NULL: of the
+ * group's first entry), and to the others in their own; no member attends to tokens at or past its own
+ * length or before its window, whatever is shared.  So results are those of bsp_attention where members
+ * and prefix row name the same pages for the shared tokens.  A prefix row not in 0 .. seqs - 1, and
+ * entries that hold nothing, give no tokens; `shared` may be 0 and may be larger than lengths.  batch up
+ * to 1024 and groups up to batch (0: nothing is shared); else BSP_EUNSUPPORTED.  The rest is as for
+ * bsp_attention. */
+bsp_status bsp_attention_prefix_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t groups,
+                                          int32_t width, int64_t *bytes);
+bsp_status bsp_attention_prefix(const bsp_cache *cache, int32_t batch, int32_t heads, const void *q,
+                                const bsp_strides *qs, const void *keys, const void *values, const int32_t *table,
+                                int32_t seqs, int32_t width, const int32_t *rows_or_null, const int32_t *lens,
+                                int32_t groups, const int32_t *starts, const int32_t *shared,
+                                const int32_t *prefix_rows_or_null, float scale, int32_t window, void *y,
+                                const bsp_strides *ys, float *lse_or_null, void *workspace, void *stream);
+
+/* The next token of each of `batch` rows of logits l (of `vocab`, up to 2^20), element (b, i) row_stride * b
+ * + token_stride * i elements from the first, from a random number u[b] (0 <= u < 1, given).  With
+ *   w_i = exp((l_i - max l) / temperature[b])
+ * and tokens in order of falling l (equal ones: the lower index first) what is kept is the shortest of
+ *   top_k   the first top_k[b] tokens (0 or less: all)
+ *   top_p   of these the fewest first whose w add up to top_p[b] of the sum of theirs (1 or more: all of them)
+ *   min_p   those with w_i >= min_p[b]
+ * and of it tokens[b] is the first by index up to which the w kept add up to more than u[b] times their sum.
+ * One token at least is kept.  An array that is NULL stands for temperature 1 or no cut.  A temperature that
+ * is not above 0 takes the first largest logit.  Tokens of -Inf and NaN are never taken; a row of nothing
+ * else gives -1.  Of +Inf the tokens that have it are alike, all others out.  NaN counts as 1 for top_p and
+ * 0 for min_p; u is taken within 0 .. 1 - 2^-24 (NaN: 0).  logp_or_null[b]: log of the probability that the
+ * token was taken with, w over the sum of what was kept (-Inf for token -1).
+ * w is computed in fp64 and summed as whole multiples of 2^-43, so that results do not depend on the order
+ * of sums; a w below 2^-44 counts as 0.  workspace: bsp_sample_workspace bytes, 16-byte aligned, whose content
+ * does not matter; calls that may overlap need one each.  batch fewer than 2^24, batch * vocab below 2^31;
+ * else BSP_EUNSUPPORTED.  Async. */
+bsp_status bsp_sample_workspace(int32_t batch, int32_t vocab, int64_t *bytes);
+bsp_status bsp_sample(bsp_dtype dt, int32_t batch, int32_t vocab, const void *logits, int64_t row_stride,
+                      int64_t token_stride, const float *u, const float *temperature_or_null,
+                      const int32_t *top_k_or_null, const float *top_p_or_null, const float *min_p_or_null,
+                      int32_t *tokens, float *logp_or_null, void *workspace, void *stream);
+
 /* Care of the pages.  The state is on the device and the host never waits for it: table
  * [seqs][width], lens [seqs], and refs [pages], the number of table entries that name a page (0: the
  * page is free); these calls alone change it, and an entry past a sequence's length names no page.

@@ -21,6 +21,9 @@ __all__ = [
     "HEAD_MAJOR", "SLOT_MAJOR", "CacheShape", "bsp_q4_sizes", "bsp_q4_quantize", "bsp_q4_dequantize", "bsp_q4_linear",
     "bsp_attention_workspace", "bsp_attention", "bsp_cache_append", "bsp_cache_scratch", "bsp_cache_fork",
     "bsp_cache_extend", "bsp_cache_release", "bsp_cache_compact", "bsp_cache_copy",
+    "ROPE_HALF", "ROPE_INTERLEAVED", "RAMP_NONE", "RAMP_TURNS", "RAMP_INDEX", "Rope", "RopeScaling", "bsp_rope_freqs",
+    "bsp_rotary", "bsp_cache_append_rotary", "bsp_attention_prefix_workspace", "bsp_attention_prefix",
+    "bsp_sample_workspace", "bsp_sample",
 ]
 
 _I64x4 = ctypes.c_int64 * 4
@@ -28,6 +31,8 @@ F32, BF16 = 0, 1
 ROW, COL, UNSTRUCTURED, DENSE, PUNCHED, ROWCOL, PATTERN = 0, 1, 2, 3, 4, 5, 6
 
 HEAD_MAJOR, SLOT_MAJOR = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+RAMP_NONE, RAMP_TURNS, RAMP_INDEX = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "_build", "libbsp.so")
@@ -87,6 +92,19 @@ class CacheShape(ctypes.Structure):
         return (self.pages, *inner, self.head_dim)
 
 
+class Rope(ctypes.Structure):
+    """bsp_rope: how the pairs of a head lie, dimensions that are rotated, factor of what is rotated."""
+    _fields_ = [("layout", ctypes.c_int32), ("dims", ctypes.c_int32), ("factor", ctypes.c_float)]
+
+    def __init__(self, layout: int = ROPE_HALF, dims: int = 0, factor: float = 1.0):
+        super().__init__(layout, dims, factor)
+
+
+class RopeScaling(ctypes.Structure):
+    """bsp_rope_scaling: how frequencies are slowed down for contexts longer than a model's own."""
+    _fields_ = [(n, ctypes.c_double) for n in ("factor", "original", "low", "high")] + [("ramp", ctypes.c_int32)]
+
+
 class _Strides(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("seq", "head", "dim")]
 
@@ -131,11 +149,22 @@ def lib():
     L.bsp_cache_release.argtypes = [I32, I32, I32, VP, VP, VP, I32, VP, VP]
     L.bsp_cache_compact.argtypes = [ca, I32, I64, VP, I32, I32, VP, VP, VP, VP, VP]
     L.bsp_cache_copy.argtypes = [ca, I32, I64, VP, I32, VP, VP, VP]
+    F, ro = ctypes.c_float, P(Rope)
+    L.bsp_rope_freqs.argtypes = [I32, ctypes.c_double, P(RopeScaling), VP]
+    L.bsp_rotary.argtypes = [I32, ro, VP, I32, I32, I32, VP, sd, VP, VP, F, VP, sd, VP]
+    L.bsp_cache_append_rotary.argtypes = [ca, ro, VP, I32, I32, VP, sd, VP, sd, VP, sd, VP, sd, VP, VP, F, VP, VP, VP, I32,
+                                          I32, VP, VP, VP]
+    L.bsp_attention_prefix_workspace.argtypes = [ca, I32, I32, I32, I32, VP]
+    L.bsp_attention_prefix.argtypes = [ca, I32, I32, VP, sd, VP, VP, VP, I32, I32, VP, VP, I32, VP, VP, VP, F, I32, VP, sd, VP,
+                                       VP, VP]
+    L.bsp_sample_workspace.argtypes = [I32, I32, VP]
+    L.bsp_sample.argtypes = [I32, I32, I32, VP, I64, I64, VP, VP, VP, VP, VP, VP, VP, VP, VP]
     for f in ("bsp_packed_sizes", "bsp_prune", "bsp_prune_noalloc", "bsp_pack", "bsp_unpack", "bsp_conv2d",
               "bsp_linear", "bsp_maxpool2x2", "bsp_version", "bsp_to_bcs", "bsp_q4_sizes", "bsp_q4_quantize",
               "bsp_q4_dequantize", "bsp_q4_linear", "bsp_cache_append", "bsp_attention_workspace", "bsp_attention",
               "bsp_cache_scratch", "bsp_cache_fork", "bsp_cache_extend", "bsp_cache_release", "bsp_cache_compact",
-              "bsp_cache_copy"):
+              "bsp_cache_copy", "bsp_rope_freqs", "bsp_rotary", "bsp_cache_append_rotary", "bsp_attention_prefix_workspace",
+              "bsp_attention_prefix", "bsp_sample_workspace", "bsp_sample"):
         getattr(L, f).restype = I32
     _lib = L
     return L
@@ -567,3 +596,159 @@ def bsp_cache_copy(cache: CacheShape, data, src, dst, stream=None):
     _ints("dst", dst, n)
     _check("bsp_cache_copy", lib().bsp_cache_copy(cache, planes, plane_stride, data.data_ptr(), n, src.data_ptr(),
                                                   dst.data_ptr(), _stream(stream)))
+
+
+# ---- rotary positions, attention over a shared prefix, sampling ----
+
+def bsp_rope_freqs(dims: int, base: float, scaling: RopeScaling | None = None):
+    """-> dims / 2 angles that the pairs turn by in a token (to be kept on the device in float64)."""
+    out = (ctypes.c_double * (max(0, int(dims)) // 2))()
+    _check("bsp_rope_freqs", lib().bsp_rope_freqs(int(dims), float(base), scaling, ctypes.addressof(out)))
+    return list(out)
+
+
+def _freqs(freqs, dims: int):
+    import torch
+    if dims > 0:
+        _dev("freqs", freqs, 4 * dims)
+        if freqs.dtype is not torch.float64:
+            raise ValueError("freqs must be float64")
+
+
+@functools.lru_cache(maxsize=4096)
+def _arrays(dt: int, *arrays):
+    """Strides of arrays of type dt; of each the name, the shape that it must have, and its own shape, strides and type."""
+    out = []
+    for name, want, shape, strides, dtype in zip(*(arrays[i::5] for i in range(5))):
+        if tuple(shape) != want or dtype is not _float_types().get(dt):
+            raise ValueError(f"{name} must be {list(want)} of the type that the call names")
+        out.append(_Strides(*strides))
+    return out
+
+
+def _norm_weights(name: str, t, dim: int):
+    if t is not None:
+        _dev(name, t, 4 * dim, F32)
+
+
+def bsp_rotary(dt: int, rope: Rope, freqs, x, pos, y, norm=None, eps: float = 1e-6, stream=None):
+    """x and y: [tokens, heads, head_dim] of any strides (y's elements distinct)."""
+    if x.dim() != 3:
+        raise ValueError("x must be [tokens, heads, head_dim]")
+    n, heads, dim = want = tuple(x.shape)
+    xs, ys = _arrays(dt, "x", want, x.shape, x.stride(), x.dtype, "y", want, y.shape, y.stride(), y.dtype)
+    _on_device(x=x, y=y)
+    _freqs(freqs, rope.dims)
+    _ints("pos", pos, n)
+    _norm_weights("norm", norm, dim)
+    st = lib().bsp_rotary(dt, rope, _p(freqs), n, heads, dim, x.data_ptr(), xs, pos.data_ptr(), _p(norm), eps, y.data_ptr(), ys,
+                          _stream(stream))
+    if st:
+        raise BspError("bsp_rotary", st)
+
+
+def bsp_cache_append_rotary(cache: CacheShape, rope: Rope, freqs, q, k, v, q_out, keys, values, table, pos, rows=None,
+                            q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
+    """q and q_out: [tokens, heads, head_dim], k and v: [tokens, kv_heads, head_dim], of any strides."""
+    n, heads = q.shape[0], q.shape[1]
+    key, dim = bytes(cache), cache.head_dim
+    ks, vs = _layouts(key, ("k", "v"), n, cache.kv_heads, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
+    want = (n, heads, dim)
+    qs, qos = _arrays(cache.dtype, "q", want, q.shape, q.stride(), q.dtype, "q_out", want, q_out.shape, q_out.stride(), q_out.dtype)
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and q_out.is_cuda and keys.is_cuda and values.is_cuda):
+        _on_device(q=q, k=k, v=v, q_out=q_out, keys=keys, values=values)
+    _freqs(freqs, rope.dims)
+    _norm_weights("q_norm", q_norm, dim)
+    _norm_weights("k_norm", k_norm, dim)
+    seqs, width = _table(table)
+    _ints("pos", pos, n)
+    if rows is not None:
+        _ints("rows", rows, n)
+    st = lib().bsp_cache_append_rotary(cache, rope, _p(freqs), n, heads, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                                       q_out.data_ptr(), qos, _p(q_norm), _p(k_norm), eps, keys.data_ptr(), values.data_ptr(),
+                                       table.data_ptr(), seqs, width, _p(rows), pos.data_ptr(), _stream(stream))
+    if st:
+        raise BspError("bsp_cache_append_rotary", st)
+
+
+def bsp_attention_prefix_workspace(cache: CacheShape, batch: int, heads: int, groups: int, width: int) -> int:
+    """Bytes of bsp_attention_prefix's workspace."""
+    out = ctypes.c_int64()
+    _check("bsp_attention_prefix_workspace", lib().bsp_attention_prefix_workspace(
+        cache, int(batch), int(heads), int(groups), int(width), ctypes.addressof(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _prefix_workspace(key: bytes, batch: int, heads: int, groups: int, width: int) -> int:
+    return bsp_attention_prefix_workspace(CacheShape.from_buffer_copy(key), batch, heads, groups, width)
+
+
+def bsp_attention_prefix(cache: CacheShape, q, keys, values, table, lens, starts, shared, y, scale: float, window: int = 0,
+                         rows=None, prefix_rows=None, lse=None, workspace=None, stream=None):
+    """As bsp_attention; group g is entries starts[g] .. starts[g + 1] - 1 and shares its first shared[g] tokens."""
+    (batch, heads, _), key = q.shape, bytes(cache)
+    qs, ys = _layouts(key, ("q", "y"), batch, heads, q.shape, q.stride(), q.dtype, y.shape, y.stride(), y.dtype,
+                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
+    if not (q.is_cuda and y.is_cuda and keys.is_cuda and values.is_cuda):
+        _on_device(q=q, y=y, keys=keys, values=values)
+    seqs, width = _table(table)
+    groups = shared.numel()
+    _ints("lens", lens, seqs)
+    _ints("shared", shared, groups)
+    _ints("starts", starts, groups + 1)
+    if rows is not None:
+        _ints("rows", rows, batch)
+    elif batch > seqs:
+        raise ValueError(f"{batch} queries for {seqs} sequences")
+    if prefix_rows is not None:
+        _ints("prefix_rows", prefix_rows, groups)
+    if lse is not None:
+        _dev("lse", lse, batch * heads * 4, F32)
+    need = _prefix_workspace(key, batch, heads, groups, width)
+    if need:
+        _dev("workspace", workspace, need)
+    st = lib().bsp_attention_prefix(cache, batch, heads, q.data_ptr(), qs, keys.data_ptr(), values.data_ptr(), table.data_ptr(),
+                                    seqs, width, _p(rows), lens.data_ptr(), groups, starts.data_ptr(), shared.data_ptr(),
+                                    _p(prefix_rows), scale, window, y.data_ptr(), ys, _p(lse), _p(workspace), _stream(stream))
+    if st:
+        raise BspError("bsp_attention_prefix", st)
+
+
+def bsp_sample_workspace(batch: int, vocab: int) -> int:
+    """Bytes of bsp_sample's workspace."""
+    out = ctypes.c_int64()
+    _check("bsp_sample_workspace", lib().bsp_sample_workspace(int(batch), int(vocab), ctypes.addressof(out)))
+    return out.value
+
+
+_sample_workspace = functools.lru_cache(maxsize=4096)(bsp_sample_workspace)
+
+
+def bsp_sample(dt: int, logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logp=None, workspace=None,
+               stream=None):
+    """logits: [batch, vocab] of any strides (feature-major logits [vocab][batch] as logits.t())."""
+    if logits.dim() != 2 or logits.dtype is not _float_types().get(dt):
+        raise ValueError("logits must be [batch, vocab] of the type that the call names")
+    batch, vocab = logits.shape
+    _on_device(logits=logits)
+    _dev("u", u, 4 * batch, F32)
+    _ints("tokens", tokens, batch)
+    if temperature is not None:
+        _dev("temperature", temperature, 4 * batch, F32)
+    if top_k is not None:
+        _ints("top_k", top_k, batch)
+    if top_p is not None:
+        _dev("top_p", top_p, 4 * batch, F32)
+    if min_p is not None:
+        _dev("min_p", min_p, 4 * batch, F32)
+    if logp is not None:
+        _dev("logp", logp, 4 * batch, F32)
+    need = _sample_workspace(batch, vocab)
+    if need:
+        _dev("workspace", workspace, need)
+    st = lib().bsp_sample(dt, batch, vocab, logits.data_ptr(), logits.stride(0), logits.stride(1), u.data_ptr(), _p(temperature),
+                          _p(top_k), _p(top_p), _p(min_p), tokens.data_ptr(), _p(logp), _p(workspace), _stream(stream))
+    if st:
+        raise BspError("bsp_sample", st)

@@ -1,6 +1,7 @@
 // C ABI entry points of the decode operators: argument validation and dispatch.  Nothing is kept
 // between calls; every device buffer belongs to the caller.
 #include <climits>
+#include <cmath>
 
 #include <hip/hip_runtime.h>
 
@@ -62,6 +63,16 @@ bsp_status check_planes(const bsp_cache *c, int32_t planes, int64_t plane_stride
     const bool after = plane_stride >= (c->pages - 1) * stride + page;
     const bool beside = plane_stride >= page && (planes - 1) * plane_stride + page <= stride;
     return after || beside ? BSP_OK : BSP_EINVAL;
+}
+
+bsp_status check_rotary(int32_t dt, const bsp_rope *rope, const double *freqs, int32_t n, int64_t slots, int32_t head_dim,
+                        const float *norm, float eps) {
+    if (!dtype_ok(dt) || !rope || n < 0 || head_dim < 1) return BSP_EINVAL;
+    if (rope->layout != BSP_ROPE_HALF && rope->layout != BSP_ROPE_INTERLEAVED) return BSP_EINVAL;
+    if (rope->dims < 0 || rope->dims % 2 || rope->dims > head_dim) return BSP_EINVAL;
+    if ((rope->dims > 0 && !freqs) || !aligned(freqs, 8) || !aligned(norm, 4) || (norm && !(eps >= 0.f))) return BSP_EINVAL;
+    // heads are a grid's y
+    return head_dim > 256 || slots > 65535 || n > kMostListed ? BSP_EUNSUPPORTED : BSP_OK;
 }
 
 PlanesArgs planes_args(const bsp_cache *c, int32_t planes, int64_t plane_stride, void *data) {
@@ -160,6 +171,136 @@ bsp_status bsp_attention(const bsp_cache *cache, int32_t batch, int32_t heads, c
     a.group = heads / cache->kv_heads, a.seqs = seqs, a.width = width, a.window = window, a.scale = scale;
     a.workspace = workspace;
     return status(launch_attention(a, S(stream)));
+}
+
+bsp_status bsp_rope_freqs(int32_t dims, double base, const bsp_rope_scaling *scaling, double *freqs) {
+    if (dims < 0 || dims % 2 || (dims > 0 && !freqs) || !(base > 0.0) || !std::isfinite(base)) return BSP_EINVAL;
+    bsp_rope_scaling s = {1.0, 0.0, 0.0, 0.0, BSP_RAMP_NONE};
+    if (scaling) s = *scaling;
+    if (!(s.factor > 0.0) || !std::isfinite(s.factor)) return BSP_EINVAL;
+    if (s.ramp != BSP_RAMP_NONE && s.ramp != BSP_RAMP_TURNS && s.ramp != BSP_RAMP_INDEX) return BSP_EINVAL;
+    double a = 0.0, b = 0.0;
+    constexpr double kTurn = 6.283185307179586477;
+    if (s.ramp != BSP_RAMP_NONE && !(s.original > 0.0 && s.low < s.high && std::isfinite(s.original) && std::isfinite(s.high - s.low)))
+        return BSP_EINVAL;
+    if (s.ramp == BSP_RAMP_INDEX) {
+        if (!(s.low > 0.0) || !(base > 1.0)) return BSP_EINVAL;
+        auto index = [&](double turns) { return dims * std::log(s.original / (turns * kTurn)) / (2.0 * std::log(base)); };
+        a = std::max(std::floor(index(s.high)), 0.0), b = std::min(std::ceil(index(s.low)), dims - 1.0);
+        if (a == b) b = a + 0.001;
+    }
+    for (int i = 0; i < dims / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / dims);
+        double keep = 0.0;
+        if (s.ramp == BSP_RAMP_TURNS) keep = (s.original * f / kTurn - s.low) / (s.high - s.low);
+        if (s.ramp == BSP_RAMP_INDEX) keep = 1.0 - (i - a) / (b - a);
+        keep = std::min(std::max(keep, 0.0), 1.0);
+        freqs[i] = f * (keep + (1.0 - keep) / s.factor);
+    }
+    return BSP_OK;
+}
+
+bsp_status bsp_rotary(bsp_dtype dt, const bsp_rope *rope, const double *freqs, int32_t n, int32_t heads, int32_t head_dim,
+                      const void *x, const bsp_strides *xs, const int32_t *pos, const float *norm, float eps, void *y,
+                      const bsp_strides *ys, void *stream) {
+    if (heads < 1) return BSP_EINVAL;
+    if (const bsp_status st = check_rotary(dt, rope, freqs, n, heads, head_dim, norm, eps); st != BSP_OK) return st;
+    if (!xs || !ys || (n > 0 && (!x || !y || !pos)) || !aligned(x, esize(dt)) || !aligned(y, esize(dt)) || !aligned(pos, 4))
+        return BSP_EINVAL;
+    if (n == 0) return BSP_OK;
+    RotaryArgs a = {};
+    a.dtype = dt, a.n = n, a.heads = heads, a.head_dim = head_dim, a.rope = *rope, a.eps = eps, a.freqs = freqs, a.pos = pos;
+    a.x = x, a.y = y, a.xs = *xs, a.ys = *ys, a.x_norm = norm;
+    return status(launch_rotary(a, S(stream)));
+}
+
+bsp_status bsp_cache_append_rotary(const bsp_cache *cache, const bsp_rope *rope, const double *freqs, int32_t n, int32_t heads,
+                                   const void *q, const bsp_strides *qs, const void *k, const bsp_strides *ks, const void *v,
+                                   const bsp_strides *vs, void *q_out, const bsp_strides *qos, const float *q_norm,
+                                   const float *k_norm, float eps, void *keys, void *values, const int32_t *table,
+                                   int32_t seqs, int32_t width, const int32_t *rows, const int32_t *pos, void *stream) {
+    if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
+    if (heads < 1) return BSP_EINVAL;
+    const int64_t slots = heads + 2 * (int64_t)cache->kv_heads;
+    for (const float *norm : {q_norm, k_norm})
+        if (const bsp_status st = check_rotary(cache->dtype, rope, freqs, n, slots, cache->head_dim, norm, eps); st != BSP_OK) return st;
+    if (!qs || !ks || !vs || !qos || !keys || !values || !aligned(keys, 16) || !aligned(values, 16)) return BSP_EINVAL;
+    if (n > 0 && (!q || !k || !v || !q_out || !pos)) return BSP_EINVAL;
+    for (const void *p : {q, k, v, (const void *)q_out})
+        if (!aligned(p, esize(cache->dtype))) return BSP_EINVAL;
+    if (!aligned(pos, 4) || !aligned(rows, 4)) return BSP_EINVAL;
+    if (const bsp_status st = check_table(table, seqs, width, cache->page_size); st != BSP_OK) return st;
+    if (n == 0) return BSP_OK;
+    RotaryArgs a = {};
+    a.dtype = cache->dtype, a.n = n, a.heads = heads, a.head_dim = cache->head_dim, a.rope = *rope, a.eps = eps;
+    a.freqs = freqs, a.pos = pos, a.x = q, a.y = q_out, a.xs = *qs, a.ys = *qos, a.x_norm = q_norm, a.k_norm = k_norm;
+    a.kv_heads = cache->kv_heads, a.c = cache_args(*cache), a.k = k, a.v = v, a.ks = *ks, a.vs = *vs;
+    a.keys = keys, a.values = values, a.table = table, a.rows = rows, a.seqs = seqs, a.width = width;
+    return status(launch_rotary(a, S(stream)));
+}
+
+bsp_status bsp_attention_prefix_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t groups, int32_t width,
+                                          int64_t *bytes) {
+    if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
+    if (!bytes || batch < 0 || heads < 1 || heads % cache->kv_heads || groups < 0 || width < 0) return BSP_EINVAL;
+    if ((int64_t)width * cache->page_size > kMaxTokens || (int64_t)batch * heads > INT32_MAX / 256) return BSP_EUNSUPPORTED;
+    if (batch > kMostPrefixSeqs || groups > batch) return BSP_EUNSUPPORTED;
+    *bytes = prefix_workspace(cache_args(*cache), batch, heads, groups, width);
+    return BSP_OK;
+}
+
+bsp_status bsp_attention_prefix(const bsp_cache *cache, int32_t batch, int32_t heads, const void *q, const bsp_strides *qs,
+                                const void *keys, const void *values, const int32_t *table, int32_t seqs, int32_t width,
+                                const int32_t *rows, const int32_t *lens, int32_t groups, const int32_t *starts,
+                                const int32_t *shared, const int32_t *prefix_rows, float scale, int32_t window, void *y,
+                                const bsp_strides *ys, float *lse, void *workspace, void *stream) {
+    if (const bsp_status st = check_cache(cache); st != BSP_OK) return st;
+    if (batch < 0 || heads < 1 || heads % cache->kv_heads || groups < 0 || window < 0 || !qs || !ys) return BSP_EINVAL;
+    if (!keys || !values || !aligned(keys, 16) || !aligned(values, 16)) return BSP_EINVAL;
+    if (batch > 0 && (!q || !y || (!lens && seqs > 0))) return BSP_EINVAL;
+    if (groups > 0 && (!starts || !shared)) return BSP_EINVAL;
+    if (!aligned(q, esize(cache->dtype)) || !aligned(y, esize(cache->dtype)) || !aligned(lse, 4)) return BSP_EINVAL;
+    for (const int32_t *p : {table, rows, lens, starts, shared, prefix_rows})
+        if (!aligned(p, 4)) return BSP_EINVAL;
+    if (const bsp_status st = check_table(table, seqs, width, cache->page_size); st != BSP_OK) return st;
+    if ((int64_t)batch * heads > INT32_MAX / 256 || batch > kMostPrefixSeqs || groups > batch) return BSP_EUNSUPPORTED;
+    if (batch == 0) return BSP_OK;
+    PrefixArgs p;
+    AttnArgs &a = p.a;
+    a.c = cache_args(*cache);
+    if (prefix_workspace(a.c, batch, heads, groups, width) > 0 && (!workspace || !aligned(workspace, 16))) return BSP_EINVAL;
+    a.q = q, a.keys = keys, a.values = values, a.y = y, a.lse = lse, a.qs = *qs, a.ys = *ys;
+    a.table = table, a.rows = rows, a.lens = lens, a.batch = batch, a.heads = heads;
+    a.group = heads / cache->kv_heads, a.seqs = seqs, a.width = width, a.window = window, a.scale = scale;
+    a.workspace = workspace, a.shares = 0, a.head_groups = 0;
+    p.groups = groups, p.starts = starts, p.shared = shared, p.prefix_rows = prefix_rows;
+    return status(launch_prefix(p, S(stream)));
+}
+
+bsp_status bsp_sample_workspace(int32_t batch, int32_t vocab, int64_t *bytes) {
+    if (!bytes || batch < 0 || vocab < 1) return BSP_EINVAL;
+    if (vocab > kMostVocab || batch > kMostListed || (int64_t)batch * vocab > INT32_MAX) return BSP_EUNSUPPORTED;
+    *bytes = sample_workspace(batch, vocab);
+    return BSP_OK;
+}
+
+bsp_status bsp_sample(bsp_dtype dt, int32_t batch, int32_t vocab, const void *logits, int64_t row_stride, int64_t token_stride,
+                      const float *u, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                      int32_t *tokens, float *logp, void *workspace, void *stream) {
+    if (!dtype_ok(dt) || batch < 0 || vocab < 1) return BSP_EINVAL;
+    if (batch > 0 && (!logits || !u || !tokens)) return BSP_EINVAL;
+    for (const void *p : {(const void *)u, (const void *)temperature, (const void *)top_k, (const void *)top_p,
+                          (const void *)min_p, (const void *)tokens, (const void *)logp})
+        if (!aligned(p, 4)) return BSP_EINVAL;
+    if (!aligned(logits, esize(dt))) return BSP_EINVAL;
+    if (vocab > kMostVocab || batch > kMostListed || (int64_t)batch * vocab > INT32_MAX) return BSP_EUNSUPPORTED;
+    if (batch == 0) return BSP_OK;
+    if (sample_workspace(batch, vocab) > 0 && (!workspace || !aligned(workspace, 16))) return BSP_EINVAL;
+    SampleArgs a;
+    a.dtype = dt, a.batch = batch, a.vocab = vocab, a.logits = logits, a.row_stride = row_stride, a.token_stride = token_stride;
+    a.u = u, a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.tokens = tokens, a.logp = logp;
+    a.workspace = workspace;
+    return status(launch_sample(a, S(stream)));
 }
 
 bsp_status bsp_cache_scratch(const bsp_cache *cache, int32_t seqs, int32_t width, int32_t n, int64_t *bytes) {

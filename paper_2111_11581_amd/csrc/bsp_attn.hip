@@ -22,6 +22,7 @@
 
 #include "bsp_decode.h"
 #include "bsp_decode_dev.h"
+#include "bsp_paged.h"
 
 namespace bsp {
 
@@ -29,14 +30,6 @@ namespace {
 
 constexpr int kWaves = 4, kTile = 1024;   // waves of a workgroup; tokens whose places it keeps in LDS
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
-// Page of token t of a sequence, or -1 where the entry holds nothing.
-__device__ __forceinline__ int page_of(const CacheArgs &c, const int32_t *row, uint32_t t, uint32_t *slot) {
-    const uint32_t e = fdiv(t, c.div_page);
-    *slot = t - e * (uint32_t)c.page_size;
-    const int p = row[e];
-    return (unsigned)p < (unsigned)c.pages ? p : -1;
-}
 
 // A thread copies elements of a token's key or value.  Bound by the latency of position, entry and
 // store, one after the other; the elements are read meanwhile (32 tokens of 1024 elements 4.0 us, 4.9

@@ -1,5 +1,5 @@
-// Launch interface of the decode operators: 4-bit FC layers, attention over a paged cache, and
-// the care of its pages.  Arguments are checked at the C entry points (bsp_api_decode.cpp).
+// Launch interface of the decode operators: 4-bit FC layers, attention over a paged cache, the care
+// of its pages, rotary positions and sampling.  Arguments are checked at the C entry points (bsp_api_decode.cpp).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -77,6 +77,53 @@ struct AttnArgs {
 };
 int64_t attention_workspace(const CacheArgs &c, int batch, int heads, int width);
 hipError_t launch_attention(AttnArgs a, hipStream_t st);
+
+// ---- rotary positions ----
+struct RotaryArgs {
+    int dtype, n, heads, head_dim;
+    bsp_rope rope;
+    float eps;
+    const double *freqs;
+    const int32_t *pos;
+    const void *x;                // queries, or the one array
+    void *y;
+    bsp_strides xs, ys;
+    const float *x_norm, *k_norm;
+    int kv_heads;                 // keys and values that go into a cache, or 0
+    CacheArgs c;
+    const void *k, *v;
+    bsp_strides ks, vs;
+    void *keys, *values;
+    const int32_t *table, *rows;
+    int seqs, width;
+};
+hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st);
+
+// ---- attention of groups that share their first tokens ----
+constexpr int kMostPrefixSeqs = 1024;   // of a call
+struct PrefixArgs {
+    AttnArgs a;
+    int groups;
+    const int32_t *starts, *shared, *prefix_rows;
+};
+int64_t prefix_workspace(const CacheArgs &c, int batch, int heads, int groups, int width);
+hipError_t launch_prefix(const PrefixArgs &p, hipStream_t st);
+
+// ---- sampling ----
+constexpr int kMostVocab = 1 << 20;   // so many weights of 2^43 add up to 2^63
+struct SampleArgs {
+    int dtype, batch, vocab;
+    const void *logits;
+    int64_t row_stride, token_stride;
+    const float *u, *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int32_t *tokens;
+    float *logp;
+    void *workspace;
+};
+int64_t sample_workspace(int batch, int vocab);
+hipError_t launch_sample(const SampleArgs &a, hipStream_t st);
 
 // ---- pages ----
 struct PagesArgs {
