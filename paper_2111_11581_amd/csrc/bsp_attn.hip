@@ -20,16 +20,11 @@
 
 #include <cmath>
 
-#include "bsp_decode.h"
-#include "bsp_decode_dev.h"
-#include "bsp_paged.h"
+#include "bsp_attn.h"
 
 namespace bsp {
 
 namespace {
-
-constexpr int kWaves = 4, kTile = 1024;   // waves of a workgroup; tokens whose places it keeps in LDS
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // A thread copies elements of a token's key or value.  Bound by the latency of position, entry and
 // store, one after the other; the elements are read meanwhile (32 tokens of 1024 elements 4.0 us, 4.9
@@ -64,13 +59,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
     for (int j = threadIdx.x + kAhead * 256; j < dims; j += 256) put(j, element(j));
 }
 
-__device__ __forceinline__ int row_of(const AttnArgs &a, int b) { return a.rows ? a.rows[b] : b; }
-__device__ __forceinline__ int len_of(const AttnArgs &a, int row) {
-    const int len = (unsigned)row < (unsigned)a.seqs ? a.lens[row] : 0;
-    return max(0, (int)min((int64_t)len, (int64_t)a.width * a.c.page_size));
-}
 // The tokens that a sequence attends to, and their number in blocks of 32.
-constexpr int kBlock = 32;
 struct Span {
     int row, first, len, blocks;
 };
@@ -153,152 +142,6 @@ __device__ __forceinline__ Cut cut_up(const AttnArgs &a, int32_t *s_before, int3
     __syncthreads();
     return c;
 }
-
-// ONCE: past the caches.
-template <bool ONCE, typename T> __device__ __forceinline__ T fetch(const T *p) {
-    if constexpr (ONCE) return __builtin_nontemporal_load(p);
-    else return *p;
-}
-
-// What a wave loads and multiplies in one step, for head_dim up to DP.
-template <typename E, int DP> struct Step;
-
-template <int DP> struct Step<uint16_t, DP> {
-    static constexpr int TOK = 32, NK = DP / 32, VW = DP == 64 ? 4 : 8, NV = DP / (16 * VW);
-    typedef uint32_t VRaw __attribute__((ext_vector_type(VW / 2)));
-    u32x4 q[NK];
-    u32x4 k[2][NK];
-    VRaw v[8][NV];
-
-    __device__ __forceinline__ void load_q(const uint16_t *row, int quad) {
-#pragma unroll
-        for (int c = 0; c < NK; ++c) q[c] = *(const u32x4 *)(row + c * 32 + quad * 8);
-    }
-    // places of tokens r and 16 + r
-    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_k(const uint16_t *keys, const int64_t *ko, int quad, int D) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int c = 0; c < NK; ++c) {
-                if (!FULL && DP < 256 && c * 32 >= D) break;
-                const int d = c * 32 + quad * 8;
-                const bool in = FULL || d < D;
-                k[t][c] = fetch<ONCE>((const u32x4 *)(keys + max(ko[t], (int64_t)0) + (in ? d : 0)));
-                if (!in) k[t][c] = (u32x4){0, 0, 0, 0};
-            }
-    }
-    // places of tokens 4 quad + i and 16 + 4 quad + i
-    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_v(const uint16_t *values, const int64_t *vo, int r, int D) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int h = 0; h < NV; ++h) {
-                const int d = h * 16 * VW + r * VW;
-                v[i][h] = fetch<ONCE>((const VRaw *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0)));
-            }
-    }
-    __device__ __forceinline__ void clear_v(uint32_t dead) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (dead >> i & 1)
-#pragma unroll
-                for (int h = 0; h < NV; ++h) v[i][h] = (VRaw)0;
-    }
-    template <bool FULL> __device__ __forceinline__ void scores(float *s, int D) const {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 c4 = {0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < NK; ++c) {
-                if (!FULL && DP < 256 && c * 32 >= D) break;
-                c4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k[t][c]), as_bf16x8(q[c]), c4, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * t + i] = c4[i];
-        }
-    }
-    // A probability is the sum of two bf16, of which it keeps 16 bits (to 2^-16 of it): the second product
-    // costs nothing that shows beneath the reads, and one rounded to a single bf16 would add as much
-    // error as the output's own rounding.
-    __device__ __forceinline__ void outputs(const float *p, f32x4 (*acc)[VW]) const {
-        u32x4 b[2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            b[0][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-            b[1][i] = pack_bf16(p[2 * i] - bf16_to_f32(b[0][i]), p[2 * i + 1] - __uint_as_float(b[0][i] & 0xffff0000u));
-        }
-#pragma unroll
-        for (int h = 0; h < NV; ++h)
-#pragma unroll
-            for (int j = 0; j < VW; ++j) {
-                const uint32_t sel = j % 2 ? 0x07060302u : 0x05040100u;
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[2 * i + 1][h][j / 2], v[2 * i][h][j / 2], sel);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(b[i]), acc[h][j], 0, 0, 0);
-            }
-    }
-};
-
-template <int DP> struct Step<float, DP> {
-    static constexpr int TOK = 16, NK = DP / 16, VW = 4, NV = DP / 64;
-    f32x4 q[NK];
-    f32x4 k[NK];
-    f32x4 v[4][NV];
-
-    __device__ __forceinline__ void load_q(const float *row, int quad) {
-#pragma unroll
-        for (int c = 0; c < NK; ++c) q[c] = *(const f32x4 *)(row + c * 16 + quad * 4);
-    }
-    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_k(const float *keys, const int64_t *ko, int quad, int D) {
-#pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            if (!FULL && DP < 256 && c * 16 >= D) break;
-            const int d = c * 16 + quad * 4;
-            const bool in = FULL || d < D;
-            k[c] = fetch<ONCE>((const f32x4 *)(keys + max(ko[0], (int64_t)0) + (in ? d : 0)));
-            if (!in) k[c] = (f32x4){0, 0, 0, 0};
-        }
-    }
-    template <bool FULL, bool ONCE> __device__ __forceinline__ void load_v(const float *values, const int64_t *vo, int r, int D) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int h = 0; h < NV; ++h) {
-                const int d = h * 64 + r * 4;
-                v[i][h] = fetch<ONCE>((const f32x4 *)(values + max(vo[i], (int64_t)0) + (FULL || d < D ? d : 0)));
-            }
-    }
-    __device__ __forceinline__ void clear_v(uint32_t dead) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (dead >> i & 1)
-#pragma unroll
-                for (int h = 0; h < NV; ++h) v[i][h] = (f32x4){0, 0, 0, 0};
-    }
-    template <bool FULL> __device__ __forceinline__ void scores(float *s, int D) const {
-        f32x4 c4[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};   // two chains, or each product waits for the one before
-#pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            if (!FULL && DP < 256 && c * 16 >= D) break;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c4[i % 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], q[c][i], c4[i % 2], 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = c4[0][i] + c4[1][i];
-    }
-    __device__ __forceinline__ void outputs(const float *p, f32x4 (*acc)[VW]) const {
-#pragma unroll
-        for (int h = 0; h < NV; ++h)
-#pragma unroll
-            for (int j = 0; j < VW; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][h][j], p[i], acc[h][j], 0, 0, 0);
-    }
-};
 
 // The workspace: maxima and sums, then outputs, of segments' heads; first share and number of segments
 // of each unit.
@@ -388,11 +231,12 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
     const int32_t *table = a.table + (int64_t)sp.row * a.width;
     const E *keys = (const E *)a.keys + j * a.c.head_stride, *values = (const E *)a.values + j * a.c.head_stride;
     St st;
-    f32x4 acc[NV][VW];
+    typename St::Quad q[St::NK];
+    f32x4 acc[1][NV][VW];
 #pragma unroll
     for (int h = 0; h < NV; ++h)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) acc[h][i] = (f32x4){0, 0, 0, 0};
+        for (int i = 0; i < VW; ++i) acc[0][h][i] = (f32x4){0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
     const float scale = a.scale * kLog2e;
 
@@ -409,14 +253,14 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
             place[t] = at;
         }
         if (base == from) {   // queries come while the places do; 0 past the heads and past head_dim
-            const E *q = (const E *)a.q + b * a.qs.seq + h0 * a.qs.head;
+            const E *src = (const E *)a.q + b * a.qs.seq + h0 * a.qs.head;
             for (int i = threadIdx.x; i < 16 * DP; i += 64 * kWaves) {
                 const int h = i / DP, d = i % DP;
-                s_q[h][d] = h < heads && d < D ? q[h * a.qs.head + d * a.qs.dim] : (E)0;
+                s_q[h][d] = h < heads && d < D ? src[h * a.qs.head + d * a.qs.dim] : (E)0;
             }
         }
         __syncthreads();
-        if (base == from) st.load_q(s_q[r], quad);
+        if (base == from) St::load_q(q, s_q[r], quad);
         // A step's keys are asked for once the step before has used its own, and likewise its values, so
         // that one of the two is always on its way.  `dead`: the lane's tokens that hold nothing.
         uint32_t dead;
@@ -440,7 +284,8 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
             st.template load_v<FULL, ONCE>(values, vo, r, D);
             asm volatile("" ::: "memory");
         };
-        float s[TT];
+        float ss[1][TT];
+        float *const s = ss[0];
         auto softmax = [&]() __attribute__((always_inline)) {
             const bool whole = !__any(dead != 0);
             float top = m;
@@ -467,15 +312,15 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
 #pragma unroll
                 for (int h = 0; h < NV; ++h)
 #pragma unroll
-                    for (int i = 0; i < VW; ++i) acc[h][i] *= keep;
-            st.outputs(s, acc);
+                    for (int i = 0; i < VW; ++i) acc[0][h][i] *= keep;
+            st.template outputs<1>(ss, acc);
         };
         int s0 = wave * TOK;
         if (s0 < padded) {
             load_k(s0);
             load_v(s0);
             for (;;) {
-                st.template scores<FULL>(s, D);
+                st.template scores<FULL>(q, s, D);
                 const int next = s0 + kWaves * TOK;
                 if (next >= padded) break;
                 load_k(next);
@@ -505,7 +350,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
 #pragma unroll
                     for (int v = 0; v < VW; v += 4) {
                         f32x4 *o = (f32x4 *)&s_o[wave % 2][r][h * 16 * VW + (quad * 4 + i) * VW + v];
-                        f32x4 x = {acc[h][v][i], acc[h][v + 1][i], acc[h][v + 2][i], acc[h][v + 3][i]};
+                        f32x4 x = {acc[0][h][v][i], acc[0][h][v + 1][i], acc[0][h][v + 2][i], acc[0][h][v + 3][i]};
                         x *= f;
                         *o = turn ? *o + x : x;
                     }
