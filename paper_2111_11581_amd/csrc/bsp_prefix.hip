@@ -2,11 +2,15 @@
 // pages of their first tokens.
 //
 // What a group shares is one matrix of keys and values for the queries of all its members: of a key
-// head, members times the query heads that share it are the columns of the products, 64 at a time (32
-// for more than 128 dimensions), all of which a wave holds in registers; it reads each key and value once
-// for them, straight from memory into the operands as k_attn does.  What a member has of its own is a
-// group of one.  Both are cut into shares for the workgroups, and k_prefix_join joins the parts of
-// every query head by their maxima.
+// head, members times the query heads that share it are the columns of the products.  What a member
+// has of its own is a group of one.
+//  * k_prefix_plan cuts both into tasks of about equal cost, by lengths that only the device knows.
+//  * k_prefix works on the tasks, of which every workgroup takes the next one when it has done its
+//    last.  Up to 32 columns go as in k_attn: keys and values come straight from memory into the
+//    operands, the waves take the tokens in turn (columns_narrow).  More, up to 256, share what is
+//    staged in LDS, 32 a wave (columns_wide).
+//  * k_prefix_join joins the tasks of every query head by their maxima, in the order of their tokens.
+// Tables that hold few tokens take one kernel instead (k_prefix_short).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -17,43 +21,64 @@ namespace bsp {
 
 namespace {
 
-constexpr int kShares = 256;            // workgroups that the work is cut for: one a CU, for its registers
 constexpr int kMost = kMostPrefixSeqs;
-constexpr int columns_of(int dp) { return dp == 256 ? 32 : 64; }
-int dims_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+constexpr int kGrid = 256;              // workgroups: one a CU
+constexpr int kStep = 128;              // tokens by which work is cut, and that are staged at a time
+constexpr int kRounds = 2;              // tasks a workgroup at most, but for what cannot be cut smaller
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// Work is counted in thirds of the time that reading 32 tokens from memory takes a CU; beginning and
-// ending a segment is worth eight of these.
-constexpr int kOwn = 3, kCost = 24, kMinShare = kCost + 24;
+// Columns of a task: staged ones only for what fits LDS and registers.
+template <typename E, int DP> constexpr int kColumns = sizeof(E) == 2 && DP <= 128 ? 256 : 32;
+int columns_of(int dtype, int head_dim) { return dtype == BSP_BF16 && head_dim <= 128 ? 256 : 32; }
+// Waves of k_prefix: two for a SIMD, or one where a wave's registers ask for it.
+template <int DP> constexpr int kTaskWaves = DP == 256 ? 4 : 8;
 
-// The most units that there may be: of what groups share (a group's columns of a key head), and of what
-// sequences have of their own (up to 16 query heads of a key head).
-struct Units {
-    int64_t shared, own;
+// ---- the workspace ---------------------------------------------------------------------------------
+
+// Columns c0 .. of key head j, from sequence `first` on, over tokens number from .. to of a list: number i is token
+// begin + i, and `skip` more from number `cut` on; those below `shared` are in the pages of row `lead`.
+struct Task {
+    int j, first, c0, columns, from, to;
+    int row, lead, shared, begin, cut, skip;
 };
-Units units_of(const CacheArgs &c, int batch, int heads, int groups) {
-    const int group = heads / c.kv_heads;
-    Units u;
-    u.shared = groups ? ((int64_t)batch * group / columns_of(dims_of(c.head_dim)) + groups) * c.kv_heads : 0;
-    u.own = (int64_t)batch * c.kv_heads * ((group + 15) / 16);
-    return u;
-}
-
-// The workspace: outputs, maxima and sums of the columns of segments (share g and unit u of either kind
-// meet in at most one, g + u of the kind's own); first share and number of segments of every unit; of
-// every sequence its group's first unit, that unit's columns and its own place among them.
+struct Member {
+    int task, blocks, pieces, place;   // the group's first task, column blocks, pieces; place in the group
+    int own_task, own_pieces, unused[2];
+};
+struct Head {
+    int tasks, shared;        // all, and of those the ones of what groups share, which come first
+    int next, unused;         // the next one to take
+    int zero[4];
+};
 struct Parts {
     float *o, *m, *l;
     int columns;
-    __device__ __forceinline__ int64_t at(int64_t segment, int column) const { return segment * columns + column; }
+    __device__ __forceinline__ int64_t at(int64_t task, int column) const { return task * columns + column; }
 };
 struct Space {
+    Head *head;
+    Member *member;
+    Task *task;
     Parts shared, own;
-    int2 *shared_count, *own_count;
-    int4 *member;
     int64_t bytes;
 };
-__host__ __device__ inline Space space_of(void *workspace, const Units &u, int batch, int columns, int own_columns, int head_dim) {
+// Of either kind there are as many tasks as units, which nothing cuts, and kRounds * kGrid more at most.
+struct Sizes {
+    int64_t shared_tasks, own_tasks;
+    int columns, own_columns;
+};
+Sizes sizes_of(const CacheArgs &c, int batch, int heads, int groups) {
+    const int64_t group = heads / c.kv_heads;
+    Sizes s;
+    const int block = columns_of(c.dtype, c.head_dim);
+    s.columns = (int)std::min<int64_t>(block, (batch * group + 15) / 16 * 16);
+    s.own_columns = (int)std::min<int64_t>(16, group);
+    s.shared_tasks = groups ? (batch * group / block + groups) * c.kv_heads + kRounds * kGrid : 0;
+    s.own_tasks = (int64_t)batch * c.kv_heads * ((group + 15) / 16) + kRounds * kGrid;
+    return s;
+}
+__host__ __device__ inline Space space_of(void *workspace, const Sizes &z, int batch, int head_dim) {
     Space s;
     char *at = (char *)workspace;
     auto take = [&](int64_t bytes) {
@@ -61,56 +86,32 @@ __host__ __device__ inline Space space_of(void *workspace, const Units &u, int b
         at += (bytes + 15) / 16 * 16;
         return here;
     };
-    auto parts = [&](int64_t units, int cols) {
-        const int64_t n = units ? (kShares + units) * cols : 0;
+    auto parts = [&](int64_t tasks, int columns) {
         Parts p;
-        p.columns = cols, p.o = (float *)take(n * head_dim * 4), p.m = (float *)take(n * 4), p.l = (float *)take(n * 4);
+        const int64_t n = tasks * columns;
+        p.columns = columns, p.o = (float *)take(n * head_dim * 4), p.m = (float *)take(n * 4), p.l = (float *)take(n * 4);
         return p;
     };
-    s.shared = parts(u.shared, columns), s.own = parts(u.own, own_columns);
-    s.shared_count = (int2 *)take(u.shared * 8), s.own_count = (int2 *)take(u.own * 8);
-    s.member = (int4 *)take((int64_t)batch * 16);
+    s.head = (Head *)take(sizeof(Head)), s.member = (Member *)take((int64_t)batch * sizeof(Member));
+    s.task = (Task *)take((z.shared_tasks + z.own_tasks) * sizeof(Task));
+    s.shared = parts(z.shared_tasks, z.columns), s.own = parts(z.own_tasks, z.own_columns);
     s.bytes = at - (char *)workspace;
     return s;
 }
 
-// The work in a row: what groups share, then what sequences have of their own; an item is some units of
-// one length.  Every workgroup works it out for itself.
-struct Item {
-    int units, blocks, weight;
-    __device__ __forceinline__ int length() const { return blocks ? blocks * weight + kCost : 0; }
-};
-struct Plan {
-    int len[kMost];                           // of sequences
-    int16_t group[kMost];                     // or -1
-    int lo[kMost + 1];                        // group g: entries lo[g] to lo[g + 1]
-    int from[kMost], to[kMost];               // tokens that any of its members attends to
-    int64_t before[2 * kMost + 1];            // length of all items before
-    int unit[kMost];                          // number of a group's first unit
-    int64_t wave[kWaves];
+// ---- the plan ----------------------------------------------------------------------------------------
 
-    __device__ __forceinline__ int tokens_from(const AttnArgs &a, int b) const {
-        return a.window && len[b] > a.window ? len[b] - a.window : 0;
-    }
-    __device__ __forceinline__ int shared_of(const PrefixArgs &p, int g) const { return g < 0 ? 0 : max(0, p.shared[g]); }
-    __device__ __forceinline__ Item item(const PrefixArgs &p, int columns_of_unit, int i) const {
-        const AttnArgs &a = p.a;
-        Item it;
-        if (i < p.groups) {
-            const int columns = (lo[i + 1] - lo[i]) * a.group, n = (columns + columns_of_unit - 1) / columns_of_unit;
-            it.units = n * a.c.kv_heads, it.blocks = (max(0, to[i] - from[i]) + kBlock - 1) / kBlock;
-            it.weight = n >= 3 ? 1 : 4 - n;   // more workgroups that read the same
-        } else {
-            const int b = i - p.groups, first = max(tokens_from(a, b), shared_of(p, group[b]));
-            it.units = a.c.kv_heads * a.head_groups, it.weight = kOwn;
-            it.blocks = (int)(((int64_t)max(0, len[b] - first) + kBlock - 1) / kBlock);
-        }
-        return it;
-    }
-};
+// What 128 tokens cost a CU, in units of 1800 cycles: reading keys and values of 128 dimensions from memory takes
+// 4 of these for bf16 and 8 for fp32 (less each where several column blocks read the same), the products 1 for
+// every 64 columns of bf16 and 5 for 32 of fp32.  A task by itself is worth kTaskCost.
+constexpr int kTaskCost = 8;
+__device__ __forceinline__ int cost_of(bool f32, int columns, int blocks) {
+    const int read = f32 ? 8 : 4, compute = f32 ? 5 * ((columns + 31) / 32) : (columns + 63) / 64;
+    return max((read + blocks - 1) / blocks, compute);
+}
 
-// Inclusive scan over the workgroup of one value a thread; *all: of all of them.
-template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wave, T *all, F join) {
+// Inclusive scan of one value a thread over the workgroup.
+template <int WAVES, typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wave, F join) {
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
     for (int d = 1; d < 64; d *= 2) {
         const T o = __shfl_up(v, d);
@@ -119,163 +120,251 @@ template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wa
     __syncthreads();
     if (lane == 63) s_wave[w] = v;
     __syncthreads();
-    T before = s_wave[0];
-    *all = before;
-    T mine = v;
-#pragma unroll
-    for (int i = 1; i <= kWaves; ++i) {
-        if (i == w) mine = join(v, before);
-        if (i < kWaves) before = join(before, s_wave[i]);
-    }
-    *all = before;
-    return mine;
+    for (int i = 0; i < w; ++i) v = join(s_wave[i], v);
+    return v;
 }
 
-template <int COLUMNS> __device__ __forceinline__ int64_t make_plan(const PrefixArgs &p, Plan &s) {
+// A workgroup, a thread for a group and for a sequence.  Bound by latency: a chain of some ten accesses.
+__global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
+    constexpr int W = kMost / 64;
+    __shared__ int s_lo[kMost + 1], s_from[kMost], s_to[kMost], s_wave[W];
+    __shared__ int s_task[2 * kMost + 1], s_pieces[2 * kMost], s_steps[2 * kMost];
+    __shared__ struct {
+        int row, lead, shared, begin, cut, skip, len;
+    } s_own[kMost];
+    __shared__ int64_t s_sum[W][4];
     const AttnArgs &a = p.a;
-    const int t = threadIdx.x, G = p.groups;
-    for (int b = t; b < a.batch; b += 64 * kWaves) s.len[b] = len_of(a, row_of(a, b));
+    const int t = threadIdx.x, G = p.groups, B = a.batch;
+    const Space space = space_of(a.workspace, z, B, a.c.head_dim);
+    const bool f32 = a.c.dtype == BSP_F32;
+    auto bound = [&](int g) { return min(max(p.starts[g], 0), B); };
+
+    const int row = t < B ? row_of(a, t) : -1, len = t < B ? len_of(a, row) : 0;
+    const int begin = a.window && len > a.window ? len - a.window : 0;
+    int group = -1, lead = -1, common = 0, core_from = 0, core_to = 0;
     if (G) {
-        // bounds in order and within the batch, whatever starts holds
-        const int per = (G + 64 * kWaves) / (64 * kWaves);
-        int64_t top = 0, all;
-        for (int i = t * per; i < min(G + 1, (t + 1) * per); ++i) top = max(top, (int64_t)min(max(p.starts[i], 0), a.batch));
-        top = scan(top, s.wave, &all, [](int64_t x, int64_t y) { return max(x, y); });
-        int64_t upto = __shfl_up(top, 1);
-        if (t % 64 == 0) {
-            upto = 0;
-            for (int w = 0; w < t / 64; ++w) upto = max(upto, s.wave[w]);
-        }
-        for (int i = t * per; i < min(G + 1, (t + 1) * per); ++i) {
-            upto = max(upto, (int64_t)min(max(p.starts[i], 0), a.batch));
-            s.lo[i] = (int)upto;
-        }
-        for (int g = t; g < G; g += 64 * kWaves) s.from[g] = INT32_MAX, s.to[g] = 0;
+        // bounds of groups in order and within the batch, whatever starts holds
+        const int mine = t <= G ? bound(t) : 0, last = G == kMost && t == 0 ? bound(G) : 0;
+        const int lo = scan<W>(mine, s_wave, [](int x, int y) { return max(x, y); });
+        if (t <= G) s_lo[t] = lo;
+        s_from[t] = s_to[t] = 0;
         __syncthreads();
-        for (int b = t; b < a.batch; b += 64 * kWaves) {
-            int lo = 0, hi = G;   // the last group that begins at or before b
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (s.lo[mid] <= b) lo = mid; else hi = mid;
+        if (G == kMost && t == 0) s_lo[G] = max(last, s_lo[G - 1]);
+        __syncthreads();
+        if (t < B) {
+            int x = 0, y = G;   // the last group that begins at or before t
+            while (y - x > 1) {
+                const int mid = (x + y) / 2;
+                if (s_lo[mid] <= t) x = mid; else y = mid;
             }
-            const int g = b >= s.lo[lo] && b < s.lo[lo + 1] ? lo : -1;
-            s.group[b] = (int16_t)g;
-            const int first = s.tokens_from(a, b), last = min(s.len[b], s.shared_of(p, g));
-            if (g >= 0 && first < last) atomicMin(&s.from[g], first), atomicMax(&s.to[g], last);
+            if (t >= s_lo[x] && t < s_lo[x + 1]) {
+                group = x, common = max(0, p.shared[x]);
+                lead = p.prefix_rows ? p.prefix_rows[x] : row_of(a, s_lo[x]);
+                atomicMax(&s_to[x], min(len, common));
+            }
         }
-    } else {
-        for (int b = t; b < a.batch; b += 64 * kWaves) s.group[b] = -1;
+        __syncthreads();
+        // What is worked on together is what all members attend to, but for those whose tokens end before those that
+        // are shared, or whose window begins after them, which go by themselves: so that no token that one
+        // attends to, whatever it holds, meets the queries of another that does not.
+        const bool together = group >= 0 && begin < s_to[group] && len >= s_to[group];
+        if (together) atomicMax(&s_from[group], begin);
+        __syncthreads();
+        if (together && s_from[group] < s_to[group]) core_from = s_from[group], core_to = s_to[group];
+    }
+    s_own[t].begin = begin, s_own[t].cut = core_to ? core_from - begin : INT32_MAX, s_own[t].skip = core_to - core_from;
+    s_own[t].row = row, s_own[t].lead = lead, s_own[t].shared = common, s_own[t].len = len - begin - (core_to - core_from);
+    // item t: what group t shares; item G + t: what sequence t has of its own
+    struct Item {
+        int units, steps, cost;
+        int64_t all;
+    } item[2];
+    int blocks = 0;
+    for (int k = 0; k < 2; ++k) {
+        Item &i = item[k];
+        i.units = i.steps = i.cost = 0;
+        if (k == 0 && t < G) {
+            const int columns = (s_lo[t + 1] - s_lo[t]) * a.group;
+            blocks = (columns + block_columns - 1) / block_columns;
+            i.steps = (max(0, s_to[t] - s_from[t]) + kStep - 1) / kStep;
+            i.units = i.steps ? blocks * a.c.kv_heads : 0;
+            if (i.units) i.cost = cost_of(f32, min(columns, block_columns), blocks);
+        } else if (k == 1 && t < B) {
+            i.steps = (s_own[t].len + kStep - 1) / kStep;
+            i.units = i.steps ? a.c.kv_heads * a.head_groups : 0;
+            i.cost = cost_of(f32, min(16, a.group), a.head_groups);
+        }
+        i.all = (int64_t)i.units * i.steps * i.cost;
+    }
+    auto total_of = [&](int64_t v, int which) {
+        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+        if (t % 64 == 0) s_sum[t / 64][which] = v;
+    };
+    total_of(item[0].all + item[1].all, 0);
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < W; ++w) total += s_sum[w][0];
+    // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks in all, in
+    // rounds of the card, at the cost of the largest.
+    auto pieces_of = [&](const Item &i, int64_t most) {
+        return i.units ? (int)max((int64_t)1, min((int64_t)i.steps, ((int64_t)i.steps * i.cost + most - 1) / most)) : 0;
+    };
+    int64_t best = INT64_MAX, most = 1;
+    for (int r = 1; r <= kRounds; ++r) {
+        const int64_t m = max((int64_t)(2 * kTaskCost), (total + kGrid * r - 1) / (kGrid * r));
+        int64_t tasks = 0, cost = 0;
+        for (int k = 0; k < 2; ++k) {
+            const int n = pieces_of(item[k], m);
+            if (!n) continue;
+            if (k == 0) tasks = (int64_t)n * item[k].units;
+            cost = max(cost, k == 0 ? (int64_t)((item[k].steps + n - 1) / n) * item[k].cost : 0);
+        }
+        for (int d = 1; d < 64; d *= 2) cost = max(cost, (int64_t)__shfl_xor(cost, d));
+        if (t % 64 == 0) s_sum[t / 64][3] = cost;
+        total_of(tasks, 2);
+        __syncthreads();
+        int64_t n = 0, largest_task = 0;
+        for (int w = 0; w < W; ++w) n += s_sum[w][2], largest_task = max(largest_task, s_sum[w][3]);
+        __syncthreads();
+        const int64_t time = max((n + kGrid - 1) / kGrid * (largest_task + kTaskCost), total / kGrid + kTaskCost * r);
+        if (time < best) best = time, most = m;
+    }
+    // numbers of tasks: those of groups, then those of sequences
+    int first_task[2], before = 0;
+    for (int k = 0; k < 2; ++k) {
+        const int n = pieces_of(item[k], most), count = n * item[k].units;
+        const int upto = scan<W>(count, s_wave, [](int x, int y) { return x + y; });
+        __syncthreads();
+        if (t == kMost - 1) s_wave[0] = upto;
+        __syncthreads();
+        first_task[k] = before + upto - count;
+        const int items = k ? B : G, at = k ? G : 0;
+        if (t < items) s_task[at + t] = first_task[k], s_pieces[at + t] = n, s_steps[at + t] = item[k].steps;
+        if (k == 0 && t == 0) space.head->shared = s_wave[0];
+        before += s_wave[0];
+        __syncthreads();
+    }
+    if (t == 0) {
+        s_task[G + B] = before;
+        space.head->tasks = before, space.head->next = min(before, kGrid);
+        for (int i = 0; i < 4; ++i) space.head->zero[i] = 0;
     }
     __syncthreads();
-    const int items = G + a.batch, per = (items + 64 * kWaves - 1) / (64 * kWaves);
-    int64_t sum = 0, total, units = 0, all_units;
-    for (int i = t * per; i < min(items, (t + 1) * per); ++i) {
-        const Item it = s.item(p, COLUMNS, i);
-        sum += (int64_t)it.units * it.length(), units += it.units;
+    if (t < B) {
+        Member m = {0, 0, 0, 0, first_task[1] - s_task[G], pieces_of(item[1], most), {0, 0}};
+        if (core_to) {
+            m.task = s_task[group], m.pieces = s_pieces[group], m.place = t - s_lo[group];
+            m.blocks = ((s_lo[group + 1] - s_lo[group]) * a.group + block_columns - 1) / block_columns;
+        }
+        space.member[t] = m;
     }
-    auto add = [](int64_t x, int64_t y) { return x + y; };
-    int64_t upto = scan(sum, s.wave, &total, add) - sum;
-    units = scan(units, s.wave, &all_units, add) - units;
-    for (int i = t * per; i < min(items, (t + 1) * per); ++i) {
-        const Item it = s.item(p, COLUMNS, i);
-        s.before[i] = upto;
-        if (i < G) s.unit[i] = (int)units;
-        upto += (int64_t)it.units * it.length(), units += it.units;
+    for (int task = t; task < before; task += kMost) {
+        int x = 0, y = G + B;   // the last item that begins at or before the task, which has tasks
+        while (y - x > 1) {
+            const int mid = (x + y) / 2;
+            if (s_task[mid] <= task) x = mid; else y = mid;
+        }
+        const int n = s_pieces[x], steps = s_steps[x], in = task - s_task[x];
+        Task k;
+        int piece, end;
+        if (x < G) {   // by head, piece, block of columns: what is read together is worked on together
+            const int all = (s_lo[x + 1] - s_lo[x]) * a.group, nb = (all + block_columns - 1) / block_columns;
+            piece = in / nb % n, k.j = in / nb / n, k.first = s_lo[x], k.c0 = in % nb * block_columns;
+            k.columns = min(block_columns, all - k.c0);
+            k.row = k.lead = p.prefix_rows ? p.prefix_rows[x] : row_of(a, k.first);
+            k.shared = 0, k.begin = s_from[x], k.cut = INT32_MAX, k.skip = 0, end = s_to[x] - s_from[x];
+        } else {
+            const int b = x - G;
+            piece = in % n, k.j = in / n / a.head_groups, k.first = b, k.c0 = in / n % a.head_groups * 16;
+            k.columns = min(16, a.group - k.c0);
+            k.row = s_own[b].row, k.lead = s_own[b].lead, k.shared = s_own[b].shared;
+            k.begin = s_own[b].begin, k.cut = s_own[b].cut, k.skip = s_own[b].skip, end = s_own[b].len;
+        }
+        k.from = (int)((int64_t)steps * piece / n) * kStep, k.to = min(end, (int)((int64_t)steps * (piece + 1) / n) * kStep);
+        space.task[task] = k;
     }
-    if (t == 0) s.before[items] = total;
-    __syncthreads();
-    return total;
 }
 
-// Tokens from .. to of a row of the table, for `columns` columns from column c0 on: query head c % group
-// of key head j and sequence first + c / group.
-struct Segment {
-    int row, j, first, c0, columns, from, to;
-    Parts parts;
-    int64_t number;
-};
+// ---- up to 32 columns --------------------------------------------------------------------------------
 
-template <typename E, int DP> struct Shared {
-    static constexpr int COLUMNS = columns_of(DP), ROW = DP + 4;
-    Plan plan;
+template <typename E, int DP, int N, int WAVES> struct Narrow {
+    static constexpr int ROW = DP + 4;
     int64_t place[kTile];
-    float m[kWaves][16], l[kWaves][16];
-    __attribute__((aligned(16))) float o[2][16][ROW];
-    __attribute__((aligned(16))) E q[COLUMNS][DP + 16 / sizeof(E)];
+    float m[WAVES][16 * N], l[WAVES][16 * N];
+    union {
+        __attribute__((aligned(16))) E q[16 * N][DP + 16 / sizeof(E)];
+        __attribute__((aligned(16))) float o[WAVES][16 * N][ROW];
+    };
 };
 
-// A segment by a workgroup, its waves in turn for the tokens; N: columns in sixteens.  A column's reference
-// of the softmax is not its maximum but within 2^6 of it, or above: it moves only where some score passes
-// it by so much, which costs a vote a step instead of two exchanges and a product for every output.
-template <typename E, int DP, bool FULL, int N>
-__device__ __forceinline__ void run_segment(const PrefixArgs &p, Shared<E, DP> &sh, const Segment &g) {
+// The factor of scores in powers of two, and the sign that queries take instead of it, so that a larger product is a
+// larger score; a scale of 0 makes queries of 0.
+struct Scale {
+    float by, sign;
+    __device__ __forceinline__ explicit Scale(float scale)
+        : by(scale == 0.f ? 1.f : fabsf(scale) * kLog2e), sign(scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f) {}
+    template <typename E> __device__ __forceinline__ E of(E v) const { return sign == 1.f ? v : from_f32<E>(to_f32(v) * sign); }
+};
+
+// Largest score and sum of a softmax, of a lane's column.  The reference is not the maximum but within 2^6 of it, or
+// above: it moves only where some score passes it by so much, which costs a vote a step instead of two
+// exchanges and a product for every output.
+constexpr float kPast = 6.f;
+
+// Element offset of token number i of a task in a plane, or -1 where there is none.
+__device__ __forceinline__ int64_t place_in(const AttnArgs &a, const Task &k, int i) {
+    if (i >= k.to) return -1;
+    const int t = k.begin + i + (i >= k.cut ? k.skip : 0);
+    return place_of(a.c, a.table, t < k.shared ? k.lead : k.row, a.seqs, a.width, t);
+}
+
+// N sixteens of columns over a task's tokens.  finish(column, d, output, reference, sum) takes what comes of
+// them, joined over the waves.
+template <typename E, int DP, bool FULL, int N, int WAVES, typename F>
+__device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, N, WAVES> &sh, const Task &k, F finish) {
     typedef Step<E, DP> St;
-    constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV;
-    constexpr float kPast = 6.f;
-    const AttnArgs &a = p.a;
+    constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV, THREADS = 64 * WAVES;
     const int D = a.c.head_dim, wave = uni(threadIdx.x / 64);
     int lane = threadIdx.x % 64;
-    asm volatile("" : "+v"(lane));   // what goes by the lane is worked out again for each segment, not held in registers
+    asm volatile("" : "+v"(lane));   // what goes by the lane is worked out again for each task, not held in registers
     const int r = lane % 16, quad = lane / 16;
-    const int32_t *table = a.table + (int64_t)g.row * a.width;
-    const bool in = (unsigned)g.row < (unsigned)a.seqs;
-    const E *keys = (const E *)a.keys + g.j * a.c.head_stride, *values = (const E *)a.values + g.j * a.c.head_stride;
+    const E *keys = (const E *)a.keys + k.j * a.c.head_stride, *values = (const E *)a.values + k.j * a.c.head_stride;
+    const Scale scale(a.scale);
 
     St st;
     typename St::Quad q[N][St::NK];
     f32x4 acc[N][NV][VW];
     float m[N], l[N];
-    int begin[N], end[N];   // tokens that a lane's columns attend to
-    int all_from = 0, all_to = INT32_MAX;   // those that every column does
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         m[n] = -INFINITY, l[n] = 0.f;
-        begin[n] = 0, end[n] = INT32_MAX;
-        if (n * 16 + r < g.columns) {
-            const int b = g.first + (g.c0 + n * 16 + r) / a.group;
-            begin[n] = sh.plan.tokens_from(a, b), end[n] = sh.plan.len[b];
-        }
-        all_from = max(all_from, begin[n]), all_to = min(all_to, end[n]);
 #pragma unroll
         for (int h = 0; h < NV; ++h)
 #pragma unroll
             for (int i = 0; i < VW; ++i) acc[n][h][i] = (f32x4){0, 0, 0, 0};
     }
-    for (int d = 1; d < 16; d *= 2) all_from = max(all_from, __shfl_xor(all_from, d)), all_to = min(all_to, __shfl_xor(all_to, d));
-    all_from = uni(all_from), all_to = uni(all_to);
-    // scores in powers of two; queries change their sign with the scale's, so that a larger product is a larger score
-    const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
-    const float by = a.scale == 0.f ? 0.f : a.scale < 0.f ? -1.f : 1.f;
 
-    for (int base = g.from; base < g.to; base += kTile) {
-        const int n = min(kTile, g.to - base), padded = (n + TOK - 1) / TOK * TOK;
-        __syncthreads();   // places and queries of the tile before are no longer read
-        for (int t = threadIdx.x; t < padded; t += 64 * kWaves) {
-            int64_t at = -1;
-            if (in && t < n) {
-                uint32_t slot;
-                const int page = page_of(a.c, table, (uint32_t)(base + t), &slot);
-                if (page >= 0) at = page * a.c.page_stride + slot * a.c.slot_stride;
-            }
-            sh.place[t] = at;
-        }
-        if (base == g.from) {   // queries come while the places do, along the way they lie; 0 past columns and head_dim
+    for (int base = k.from; base < k.to; base += kTile) {
+        const int n = min(kTile, k.to - base), padded = (n + TOK - 1) / TOK * TOK;
+        if (base > k.from) __syncthreads();   // places of the tile before are no longer read
+        for (int t = threadIdx.x; t < padded; t += THREADS)
+            sh.place[t] = place_in(a, k, base + t);
+        if (base == k.from) {   // queries come while the places do, along the way they lie; 0 past columns and head_dim
             const bool by_column = a.qs.dim != 1;
-            for (int i = threadIdx.x; i < 16 * N * DP; i += 64 * kWaves) {
-                const int c = by_column ? i % (16 * N) : i / DP, d = by_column ? i / (16 * N) : i % DP, at = g.c0 + c;
+            for (int i = threadIdx.x; i < 16 * N * DP; i += THREADS) {
+                const int c = by_column ? i % (16 * N) : i / DP, d = by_column ? i / (16 * N) : i % DP, at = k.c0 + c;
                 E v = (E)0;
-                if (c < g.columns && d < D) {
-                    const int k = at / a.group;
-                    v = ((const E *)a.q)[(g.first + k) * a.qs.seq + (g.j * a.group + at - k * a.group) * a.qs.head + d * a.qs.dim];
-                    if (by != 1.f) v = from_f32<E>(to_f32(v) * by);
+                if (c < k.columns && d < D) {
+                    const int s = at / a.group;
+                    v = scale.of(((const E *)a.q)[(k.first + s) * a.qs.seq + (k.j * a.group + at - s * a.group) * a.qs.head + d * a.qs.dim]);
                 }
                 sh.q[c][d] = v;
             }
         }
         __syncthreads();
-        if (base == g.from)
+        if (base == k.from)
 #pragma unroll
-            for (int n = 0; n < N; ++n) St::load_q(q[n], sh.q[n * 16 + r], quad);
+            for (int c = 0; c < N; ++c) St::load_q(q[c], sh.q[c * 16 + r], quad);
         uint32_t dead;   // the lane's tokens that hold nothing
         auto load_k = [&](int s0) __attribute__((always_inline)) {
             int64_t ko[NT];
@@ -298,56 +387,49 @@ __device__ __forceinline__ void run_segment(const PrefixArgs &p, Shared<E, DP> &
             asm volatile("" ::: "memory");
         };
         float s[N][TT];
-        auto softmax = [&](int s0) __attribute__((always_inline)) {
-            const int t0 = base + s0;
-            const bool whole = t0 >= all_from && t0 + TOK <= all_to && !__any(dead != 0);
-            uint32_t out[N];   // a lane's tokens that its columns do not attend to
+        auto softmax = [&]() __attribute__((always_inline)) {
+            const bool whole = !__any(dead != 0);
             if (!whole) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    out[n] = dead;
+                for (int c = 0; c < N; ++c)
 #pragma unroll
-                    for (int i = 0; i < TT; ++i) {
-                        const int t = t0 + 16 * (i / 4) + 4 * quad + i % 4;
-                        if (t < begin[n] || t >= end[n]) out[n] |= 1u << i;
-                        if (out[n] >> i & 1) s[n][i] = -INFINITY;
-                    }
-                }
+                    for (int i = 0; i < TT; ++i)
+                        if (dead >> i & 1) s[c][i] = -INFINITY;
                 st.clear_v(dead);
             }
             float top[N];
             bool past = false;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                top[n] = s[n][0];
+            for (int c = 0; c < N; ++c) {
+                top[c] = s[c][0];
 #pragma unroll
-                for (int i = 1; i < TT; ++i) top[n] = fmaxf(top[n], s[n][i]);
-                top[n] *= scale;
-                past |= top[n] > m[n] + kPast;
+                for (int i = 1; i < TT; ++i) top[c] = fmaxf(top[c], s[c][i]);
+                top[c] *= scale.by;
+                past |= top[c] > m[c] + kPast;
             }
             if (__any(past))
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    float to = fmaxf(top[n], __shfl_xor(top[n], 16));
-                    to = fmaxf(m[n], fmaxf(to, __shfl_xor(to, 32)));
-                    const float keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - to);
-                    m[n] = to, l[n] *= keep;
+                for (int c = 0; c < N; ++c) {
+                    float to = fmaxf(top[c], __shfl_xor(top[c], 16));
+                    to = fmaxf(m[c], fmaxf(to, __shfl_xor(to, 32)));
+                    const float keep = m[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[c] - to);
+                    m[c] = to, l[c] *= keep;
 #pragma unroll
                     for (int h = 0; h < NV; ++h)
 #pragma unroll
-                        for (int i = 0; i < VW; ++i) acc[n][h][i] *= keep;
+                        for (int i = 0; i < VW; ++i) acc[c][h][i] *= keep;
                 }
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const float ref = m[n] == -INFINITY ? 0.f : m[n];
+            for (int c = 0; c < N; ++c) {
+                const float ref = m[c] == -INFINITY ? 0.f : m[c];
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < TT; ++i) {
-                    s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -ref));
-                    if (!whole && (out[n] >> i & 1)) s[n][i] = 0.f;
-                    sum += s[n][i];
+                    s[c][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][i], scale.by, -ref));
+                    if (!whole && (dead >> i & 1)) s[c][i] = 0.f;
+                    sum += s[c][i];
                 }
-                l[n] += sum;
+                l[c] += sum;
             }
             st.template outputs<N>(s, acc);
         };
@@ -357,180 +439,384 @@ __device__ __forceinline__ void run_segment(const PrefixArgs &p, Shared<E, DP> &
             load_v(s0);
             for (;;) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) st.template scores<FULL>(q[n], s[n], D);
-                const int next = s0 + kWaves * TOK;
+                for (int c = 0; c < N; ++c) st.template scores<FULL>(q[c], s[c], D);
+                const int next = s0 + WAVES * TOK;
                 if (next >= padded) break;
                 load_k(next);
-                softmax(s0);
+                softmax();
                 load_v(next);
                 s0 = next;
             }
-            softmax(s0);
+            softmax();
         }
     }
 
-    // join the waves, sixteen columns at a time: all on the common reference, then 2 and 3 onto 0 and 1
+    __syncthreads();   // queries are no longer read: their place is taken
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
+    for (int c = 0; c < N; ++c) {
+        l[c] += __shfl_xor(l[c], 16);
+        l[c] += __shfl_xor(l[c], 32);
+        if (quad == 0) sh.m[wave][c * 16 + r] = m[c], sh.l[wave][c * 16 + r] = l[c];
+        if (c * 16 + r < k.columns)
+#pragma unroll
+            for (int h = 0; h < NV; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int v = 0; v < VW; v += 4)
+                        *(f32x4 *)&sh.o[wave][c * 16 + r][h * 16 * VW + (quad * 4 + i) * VW + v] =
+                            (f32x4){acc[c][h][v][i], acc[c][h][v + 1][i], acc[c][h][v + 2][i], acc[c][h][v + 3][i]};
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < k.columns * DP; i += THREADS) {
+        const int c = i / DP, d = i % DP;
+        if (d >= D) continue;
+        float top = sh.m[0][c], sum = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh.m[w][c]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(sh.m[w][c] - ref);
+            sum += sh.l[w][c] * f, o += sh.o[w][c][d] * f;
+        }
+        finish(c, d, o, top, sum);
+    }
+    __syncthreads();   // the next task writes these arrays
+}
+
+// ---- more columns ------------------------------------------------------------------------------------
+
+// Keys and values of 128 tokens, twice: one is worked on while the other comes.  Rows of DP dimensions, in which 16
+// bytes lie at the place that the row turns them to: sixteen lanes that read a piece of sixteen rows, or 32 bytes of
+// four, then meet all banks.
+template <int DP> struct Wide {
+    static constexpr int ROW = DP + 4;
+    uint16_t stage[2][2][kStep * DP];   // [which][keys, values]
+    int64_t place[2][kTile];
+    int holes[2];                       // whether a tile has a token that holds nothing
+    float m[8][32], l[8][32];
+    __device__ __forceinline__ float *joined(int wave) { return (float *)stage + wave * 32 * ROW; }
+};
+template <int DP> __device__ __forceinline__ int turn_of(int row) { return DP == 128 ? row & 15 : row >> 1 & 7; }
+
+// 16 bytes from each lane's source to LDS byte address base + 16 lane; counted as one load of the wave.
+__device__ __forceinline__ void copy16(const void *src, uint32_t base) {
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "v"(src), "s"(base) : "memory");
+}
+
+// CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.
+template <int DP, bool FULL, int CW>
+__device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, const Task &k, const void *zero, const Parts &parts,
+                                             int64_t task) {
+    typedef uint16_t E;
+    constexpr int NC = DP / 32, ND = DP / 16, GR = DP / 8, SETS = 8 / CW, TOKENS = kStep / SETS;
+    const int D = a.c.head_dim, wave = uni(threadIdx.x / 64), set = wave / CW, c_wave = wave % CW * 32;
+    int lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));
+    const int r = lane % 16, quad = lane / 16;
+    const E *keys = (const E *)a.keys + k.j * a.c.head_stride, *values = (const E *)a.values + k.j * a.c.head_stride;
+    const Scale scale(a.scale);
+    const uint32_t stage0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)sh.stage;
+
+    auto fill_places = [&](int tile, const int64_t (&at)[kTile / 512]) {
+        bool hole = false;
+#pragma unroll
+        for (int i = 0; i < kTile / 512; ++i) {
+            const int t = threadIdx.x + 512 * i;
+            sh.place[tile % 2][t] = at[i], hole |= at[i] < 0 && k.from + tile * kTile + t < k.to;
+        }
+        if (hole) sh.holes[tile % 2] = 1;
+    };
+    // A wave copies 1 KB at a time of a stage's keys and values, each lane 16 bytes of the row that they belong to.
+    auto copy = [&](int s) {
+        constexpr int ROWS = 64 / GR, N = kStep / ROWS / 8;   // rows of a copy, copies of a wave
+        const uint32_t to = stage0 + (uint32_t)(s % 2 * 2 * kStep * DP * 2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int part = wave * N + i, row = part * ROWS + lane / GR, g = lane % GR ^ turn_of<DP>(row);
+            const int64_t at = sh.place[s * kStep / kTile % 2][(s * kStep + row) % kTile];
+            const bool in = at >= 0 && (FULL || g * 8 < D);
+            const void *ks = in ? (const void *)(keys + at + g * 8) : zero, *vs = in ? (const void *)(values + at + g * 8) : zero;
+            const uint32_t base = uni((int)(to + part * 1024));
+            copy16(ks, base);
+            copy16(vs, base + kStep * DP * 2);
+        }
+    };
+
+    const int stages = (k.to - k.from + kStep - 1) / kStep;
+    if (threadIdx.x < 2) sh.holes[threadIdx.x] = 0;
+    __syncthreads();
+    int64_t ahead[kTile / 512];
+#pragma unroll
+    for (int i = 0; i < kTile / 512; ++i) ahead[i] = place_in(a, k, k.from + threadIdx.x + 512 * i);
+    fill_places(0, ahead);
+    // queries, through the second stage: 0 past columns and head_dim
+    {
+        E *q = sh.stage[1][0];
+        const bool by_column = a.qs.dim != 1;
+        for (int i = threadIdx.x; i < CW * 32 * DP; i += 512) {
+            const int c = by_column ? i % (CW * 32) : i / DP, d = by_column ? i / (CW * 32) : i % DP, at = k.c0 + c;
+            E v = 0;
+            if (c < k.columns && d < D) {
+                const int s = at / a.group;
+                v = scale.of(((const E *)a.q)[(k.first + s) * a.qs.seq + (k.j * a.group + at - s * a.group) * a.qs.head + d * a.qs.dim]);
+            }
+            q[c * DP + ((d / 8 ^ turn_of<DP>(c)) * 8 + d % 8)] = v;
+        }
+    }
+    __syncthreads();
+    copy(0);
+    u32x4 q[2][NC];
+    f32x4 acc[2][ND];
+    float m[2], l[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int c = c_wave + n * 16 + r;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)&sh.stage[1][0][c * DP + ((i * 4 + quad) ^ turn_of<DP>(c)) * 8];
+        m[n] = -INFINITY, l[n] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[n][d] = (f32x4){0, 0, 0, 0};
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+
+    for (int s = 0; s < stages; ++s) {
+        // the next stage comes, and with a tile's first stage the places of the next tile
+        const bool more_places = s * kStep % kTile == 0 && (s * kStep / kTile + 1) * kTile < k.to - k.from;
+        if (s + 1 < stages) copy(s + 1);
+        if (more_places)
+#pragma unroll
+            for (int i = 0; i < kTile / 512; ++i) ahead[i] = place_in(a, k, k.from + (s * kStep / kTile + 1) * kTile + threadIdx.x + 512 * i);
+        const E *ks = sh.stage[s % 2][0], *vs = sh.stage[s % 2][1];
+        const bool holes = sh.holes[s * kStep / kTile % 2];
+        for (int t0 = set * TOKENS; t0 < (set + 1) * TOKENS; t0 += 32) {
+            const int token = k.from + s * kStep + t0;
+            if (token >= k.to) break;
+            float p[2][8];
+            // scores of 32 tokens: rows are tokens, columns queries
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int row = t0 + 16 * t + r;
+                f32x4 c4[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const u32x4 kv = *(const u32x4 *)&ks[row * DP + ((i * 4 + quad) ^ turn_of<DP>(row)) * 8];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        c4[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kv), as_bf16x8(q[n][i]), c4[n], 0, 0, 0);
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[n][4 * t + i] = c4[n][i];
+            }
+            const bool whole = !holes && token + 32 <= k.to;
+            uint32_t dead = 0;   // a lane's tokens that hold nothing; their keys and values came as 0
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (sh.place[s * kStep / kTile % 2][(s * kStep + t0 + 16 * (i / 4) + 4 * quad + i % 4) % kTile] < 0) {
+                        dead |= 1u << i;
+                        p[0][i] = p[1][i] = -INFINITY;
+                    }
+            float top[2];
+            bool past = false;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                top[n] = p[n][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], p[n][i]);
+                top[n] *= scale.by;
+                past |= top[n] > m[n] + kPast;
+            }
+            if (__any(past))
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float to = fmaxf(top[n], __shfl_xor(top[n], 16));
+                    to = fmaxf(m[n], fmaxf(to, __shfl_xor(to, 32)));
+                    const float keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - to);
+                    m[n] = to, l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[n][d] *= keep;
+                }
+            u32x4 b[2][2];   // a probability is the sum of two bf16, as in k_attn
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const float ref = m[n] == -INFINITY ? 0.f : m[n];
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][i], scale.by, -ref));
+                    if (!whole && (dead >> i & 1)) p[n][i] = 0.f;
+                    sum += p[n][i];
+                }
+                l[n] += sum;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    b[n][0][i] = pack_bf16(p[n][2 * i], p[n][2 * i + 1]);
+                    b[n][1][i] = pack_bf16(p[n][2 * i] - bf16_to_f32(b[n][0][i]), p[n][2 * i + 1] - __uint_as_float(b[n][0][i] & 0xffff0000u));
+                }
+            }
+            // outputs: rows are dimensions; of sixteen lanes, lane i names token i / 4 and four dimensions, and gets
+            // one dimension of four tokens
+            const int row = t0 + 4 * quad + r / 4;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                u32x2 w[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const E *at = &vs[(row + 16 * t) * DP + ((2 * d + r % 4 / 2) ^ turn_of<DP>(row + 16 * t)) * 8 + r % 2 * 4];
+                    w[t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const E *)at));
+                }
+                const bf16x8 v = as_bf16x8((u32x4){w[0].x, w[0].y, w[1].x, w[1].y});
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) acc[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16x8(b[n][i]), acc[n][d], 0, 0, 0);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the copies have landed
+        if (more_places) {
+            const int tile = s * kStep / kTile + 1;
+            if (threadIdx.x == 0) sh.holes[tile % 2] = 0;
+            __syncthreads();
+            fill_places(tile, ahead);
+        }
+        __syncthreads();
+    }
+
+    // join the sets, then to the parts: a lane has four dimensions of a column
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
         l[n] += __shfl_xor(l[n], 16);
         l[n] += __shfl_xor(l[n], 32);
-        if (n) __syncthreads();   // the sixteen before have been read
-        if (quad == 0) sh.m[wave][r] = m[n], sh.l[wave][r] = l[n];
-        __syncthreads();
-        float top = sh.m[0][r];
+        if (SETS > 1 && quad == 0) sh.m[wave][n * 16 + r] = m[n], sh.l[wave][n * 16 + r] = l[n];
+        if (SETS > 1 && set > 0)
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh.m[w][r]);
-        const float f = __builtin_amdgcn_exp2f(m[n] - (top == -INFINITY ? 0.f : top));
-        for (int turn = 0; turn < 2; ++turn) {
-            if (wave / 2 == 1 - turn)
-#pragma unroll
-                for (int h = 0; h < NV; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int v = 0; v < VW; v += 4) {
-                            f32x4 *o = (f32x4 *)&sh.o[wave % 2][r][h * 16 * VW + (quad * 4 + i) * VW + v];
-                            f32x4 x = {acc[n][h][v][i], acc[n][h][v + 1][i], acc[n][h][v + 2][i], acc[n][h][v + 3][i]};
-                            x *= f;
-                            *o = turn ? *o + x : x;
-                        }
-            __syncthreads();
-        }
-        const int columns = min(16, g.columns - n * 16);
-        for (int i = threadIdx.x; i < columns * DP; i += 64 * kWaves) {
-            const int c = i / DP, d = i % DP;
-            if (d >= D) continue;
-            const int64_t at = g.parts.at(g.number, n * 16 + c);
-            g.parts.o[at * D + d] = sh.o[0][c][d] + sh.o[1][c][d];
-            if (d == 0) {
-                float mm = sh.m[0][c], sum = 0.f;
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, sh.m[w][c]);
-                const float ref = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) sum += sh.l[w][c] * __builtin_amdgcn_exp2f(sh.m[w][c] - ref);
-                g.parts.m[at] = mm, g.parts.l[at] = sum;
-            }
-        }
+            for (int d = 0; d < ND; ++d) *(f32x4 *)&sh.joined(wave - CW)[(n * 16 + r) * Wide<DP>::ROW + d * 16 + quad * 4] = acc[n][d];
     }
-    __syncthreads();   // the next segment writes these arrays
+    if (SETS > 1) __syncthreads();
+    if (set == 0)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int c = c_wave + n * 16 + r;
+            if (SETS > 1) {
+                float to = m[n];
+                for (int w = wave + CW; w < 8; w += CW) to = fmaxf(to, sh.m[w][n * 16 + r]);
+                const float ref = to == -INFINITY ? 0.f : to, keep = __builtin_amdgcn_exp2f(m[n] - ref);
+                l[n] *= keep;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) acc[n][d] *= keep;
+                for (int w = wave + CW; w < 8; w += CW) {
+                    const float f = __builtin_amdgcn_exp2f(sh.m[w][n * 16 + r] - ref);
+                    l[n] += sh.l[w][n * 16 + r] * f;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+                        acc[n][d] += *(const f32x4 *)&sh.joined(w - CW)[(n * 16 + r) * Wide<DP>::ROW + d * 16 + quad * 4] * f;
+                }
+                m[n] = to;
+            }
+            if (c >= k.columns) continue;
+            const int64_t at = parts.at(task, c);
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                if (FULL || d * 16 + quad * 4 < D) *(f32x4 *)&parts.o[at * D + d * 16 + quad * 4] = acc[n][d];
+            if (quad == 0) parts.m[at] = m[n], parts.l[at] = l[n];
+        }
+    __syncthreads();   // the next task writes these arrays
 }
+
+// ---- the kernels -------------------------------------------------------------------------------------
+
+template <typename E, int DP> struct Shared {
+    static constexpr int WAVES = kTaskWaves<DP>;
+    static constexpr bool WIDE = kColumns<E, DP> > 32;
+    struct Nothing {};
+    union {
+        Narrow<E, DP, 1, WAVES> one;
+        Narrow<E, DP, 2, WAVES> two;
+        std::conditional_t<WIDE, Wide<DP == 256 ? 128 : DP>, Nothing> wide;
+    };
+    int next;
+    __device__ Shared() {}
+};
 
 template <typename E, int DP, bool FULL>
-__global__ __launch_bounds__(64 * kWaves, 1) void k_prefix(PrefixArgs p, Units units) {
-    constexpr int COLUMNS = columns_of(DP);
+__global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_prefix(PrefixArgs p, Sizes z) {
     __shared__ Shared<E, DP> sh;
     const AttnArgs &a = p.a;
-    const int G = p.groups, items = G + a.batch;
-    // consecutive shares on one XCD, whose L2 then holds what several of them read
-    const int share_number = blockIdx.x % 8 * (kShares / 8) + blockIdx.x / 8;
-    const Space space = space_of(a.workspace, units, a.batch, COLUMNS, min(16, a.group), a.c.head_dim);
-    const int64_t total = make_plan<COLUMNS>(p, sh.plan);
-    const int64_t share = max((int64_t)kMinShare, (total + kShares - 1) / kShares);
-
-    // for k_prefix_join: where a member's columns are, and units without tokens
-    int64_t pos = share_number * share;
-    const int64_t end = min(pos + share, total);
-    for (int i = share_number; i < items; i += kShares) {
-        const Item it = sh.plan.item(p, COLUMNS, i);
-        if (i >= G) {
-            const int b = i - G, g = sh.plan.group[b];
-            if (threadIdx.x == 0) {
-                space.member[b] = g < 0 ? make_int4(-1, 0, 0, 0) :
-                    make_int4(sh.plan.unit[g], sh.plan.item(p, COLUMNS, g).units / a.c.kv_heads, b - sh.plan.lo[g], 0);
-            }
+    const Space space = space_of(a.workspace, z, a.batch, a.c.head_dim);
+    const int tasks = uni(space.head->tasks), shared = uni(space.head->shared);
+    // the first tasks by place: those that read the same on the same XCD, whose L2 then holds it
+    const int each = (min(tasks, kGrid) + 7) / 8;
+    int task = (int)blockIdx.x / 8 < each ? blockIdx.x % 8 * each + blockIdx.x / 8 : tasks;
+    if (tasks < kGrid && task >= tasks) return;
+    while (task < tasks) {
+        const Task *at = space.task + task;
+        Task k;
+        k.j = uni(at->j), k.first = uni(at->first), k.c0 = uni(at->c0), k.columns = uni(at->columns), k.from = uni(at->from);
+        k.to = uni(at->to), k.row = uni(at->row), k.lead = uni(at->lead), k.shared = uni(at->shared), k.begin = uni(at->begin);
+        k.cut = uni(at->cut), k.skip = uni(at->skip);
+        if (tasks > kGrid && threadIdx.x == 0) sh.next = atomicAdd(&space.head->next, 1);
+        const bool common = task < shared;
+        const Parts parts = common ? space.shared : space.own;
+        const int64_t number = common ? task : task - shared;
+        auto finish = [&](int c, int d, float o, float m, float l) {
+            const int64_t i = parts.at(number, c);
+            parts.o[i * a.c.head_dim + d] = o;
+            if (d == 0) parts.m[i] = m, parts.l[i] = l;
+        };
+        if (k.columns <= 16) {
+            columns_narrow<E, DP, FULL, 1, kTaskWaves<DP>>(a, sh.one, k, finish);
+        } else if (k.columns <= 32 || !Shared<E, DP>::WIDE) {
+            columns_narrow<E, DP, FULL, 2, kTaskWaves<DP>>(a, sh.two, k, finish);
+        } else if constexpr (Shared<E, DP>::WIDE) {
+            const void *zero = space.head->zero;
+            if (k.columns <= 64)
+                columns_wide<DP, FULL, 2>(a, sh.wide, k, zero, parts, number);
+            else if (k.columns <= 128)
+                columns_wide<DP, FULL, 4>(a, sh.wide, k, zero, parts, number);
+            else
+                columns_wide<DP, FULL, 8>(a, sh.wide, k, zero, parts, number);
         }
-        if (it.blocks) continue;
-        int2 *count = i < G ? space.shared_count + sh.plan.unit[i] : space.own_count + (int64_t)(i - G) * it.units;
-        for (int u = threadIdx.x; u < it.units; u += 64 * kWaves) count[u] = make_int2(0, 0);
-    }
-
-    while (pos < end) {
-        int lo = 0, hi = items;   // the last item that begins at or before pos, which has length
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (sh.plan.before[mid] <= pos) lo = mid; else hi = mid;
-        }
-        const int i = uni(lo);
-        const Item it = sh.plan.item(p, COLUMNS, i);
-        const int length = uni(it.length()), weight = uni(it.weight);
-        const int64_t rest = pos - sh.plan.before[i];
-        const int u = uni((int)(rest / length)), off = uni((int)(rest - (int64_t)u * length));
-        const int n = uni((int)min(end - pos, (int64_t)(length - off)));
-        const int first = max(0, off - kCost) / weight, last = max(0, off + n - kCost) / weight;   // blocks of the segment
-        const int64_t start = pos - off;
-        pos += n;
-        if (first == last) continue;
-        Segment g;
-        int64_t unit;
-        int2 *count;
-        int whole_from, whole_to;
-        if (i < G) {
-            const int blocks = uni(it.units) / a.c.kv_heads, all = (uni(sh.plan.lo[i + 1]) - uni(sh.plan.lo[i])) * a.group;
-            g.first = uni(sh.plan.lo[i]), g.j = u / blocks, g.c0 = (u - g.j * blocks) * COLUMNS;
-            g.columns = min(COLUMNS, all - g.c0);
-            g.row = uni(p.prefix_rows ? p.prefix_rows[i] : row_of(a, g.first));
-            whole_from = uni(sh.plan.from[i]), whole_to = uni(sh.plan.to[i]);
-            unit = uni(sh.plan.unit[i]) + u, count = space.shared_count + unit, g.parts = space.shared;
-        } else {
-            const int b = i - G;
-            g.first = b, g.j = u / a.head_groups, g.c0 = (u - g.j * a.head_groups) * 16;
-            g.columns = min(16, a.group - g.c0);
-            g.row = uni(row_of(a, b));
-            whole_from = uni(max(sh.plan.tokens_from(a, b), sh.plan.shared_of(p, sh.plan.group[b]))), whole_to = uni(sh.plan.len[b]);
-            unit = (int64_t)b * it.units + u, count = space.own_count + unit, g.parts = space.own;
-        }
-        g.from = whole_from + first * kBlock, g.to = min(whole_to, whole_from + last * kBlock);
-        g.number = share_number + unit;
-        if (first == 0 && threadIdx.x == 0)
-            *count = make_int2(share_number, (int)((start + length - 1) / share) - share_number + 1);
-        if (g.columns <= 16)
-            run_segment<E, DP, FULL, 1>(p, sh, g);
-        else if (g.columns <= 32 || COLUMNS == 32)
-            run_segment<E, DP, FULL, 2>(p, sh, g);
-        else if constexpr (COLUMNS == 64)
-            run_segment<E, DP, FULL, 4>(p, sh, g);
+        if (tasks <= kGrid) break;
+        task = uni(sh.next);
+        __syncthreads();   // read before the next one is written
     }
 }
 
-// Joins the segments of a query head, those of its group and its own: 4 dimensions a thread, eight segments
-// at a time.
+// Joins the tasks of a query head, those of its group and its own: 4 dimensions a thread, eight tasks at a time.
+constexpr int kMostJoined = 512;   // whose factors are held at a time
 template <typename E>
-__global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Units units, int columns) {
+__global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int block_columns) {
     constexpr int LANES = 32, GROUPS = 256 / LANES;
-    __shared__ float s_m[2 * kShares + 2], s_top[4], s_sum[4];
+    __shared__ float s_f[kMostJoined], s_top[4], s_sum[4];
     __shared__ f32x4 s_o[GROUPS][LANES];
     const AttnArgs &a = p.a;
     const int h = blockIdx.x % a.heads, b = blockIdx.x / a.heads, t = threadIdx.x, D = a.c.head_dim;
-    const int j = h / a.group, hh = h - j * a.group, own_columns = min(16, a.group);
-    const Space space = space_of(a.workspace, units, a.batch, columns, own_columns, D);
-    const int64_t own_unit = ((int64_t)b * a.c.kv_heads + j) * a.head_groups + hh / 16;
-    const int4 member = space.member[b];
-    const int2 own = space.own_count[own_unit];
-    int2 shared = make_int2(0, 0);
-    int64_t shared_unit = 0;
-    int column = 0;
-    if (member.x >= 0) {
-        column = member.z * a.group + hh;
-        shared_unit = member.x + (int64_t)j * member.y + column / columns, column %= columns;
-        shared = space.shared_count[shared_unit];
-    }
-    const int n = shared.y + own.y;
-    auto at = [&](int k, const Parts **parts) {
-        if (k < shared.y) {
-            *parts = &space.shared;
-            return space.shared.at(shared_unit + shared.x + k, column);
-        }
-        *parts = &space.own;
-        return space.own.at(own_unit + own.x + k - shared.y, hh % 16);
+    const int j = h / a.group, hh = h - j * a.group;
+    const Space space = space_of(a.workspace, z, a.batch, D);
+    const Member me = space.member[b];
+    const int column = me.place * a.group + hh, block = column / block_columns;
+    const int n = me.pieces + me.own_pieces;
+    auto at = [&](int k, Parts *parts) {
+        const bool common = k < me.pieces;
+        *parts = common ? space.shared : space.own;
+        return common ? space.shared.at(me.task + (int64_t)(j * me.pieces + k) * me.blocks + block, column - block * block_columns)
+                      : space.own.at(me.own_task + (int64_t)(j * a.head_groups + hh / 16) * me.own_pieces + k - me.pieces, hh % 16);
     };
     auto finite = [](float top) { return top == -INFINITY ? 0.f : top; };   // what is taken off: -Inf - -Inf is none
     float top = -INFINITY, sum = 0.f;
     for (int k = t; k < n; k += 256) {
-        const Parts *parts;
+        Parts parts;
         const int64_t i = at(k, &parts);
-        const float m = parts->m[i], l = parts->l[i], to = fmaxf(top, m), ref = finite(to);
-        s_m[k] = m;
+        const float m = parts.m[i], l = parts.l[i], to = fmaxf(top, m), ref = finite(to);
+        if (k < kMostJoined) s_f[k] = m;
         sum = sum * __builtin_amdgcn_exp2f(top - ref) + l * __builtin_amdgcn_exp2f(m - ref);
         top = to;
     }
@@ -548,9 +834,10 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Units units, 
     const int from = blockIdx.y * (4 * LANES), d = from + t % LANES * 4;
     f32x4 v = {0, 0, 0, 0};
     for (int k = t / LANES; k < n; k += GROUPS) {
-        const Parts *parts;
+        Parts parts;
         const int64_t i = at(k, &parts);
-        v += *(const f32x4 *)(parts->o + i * D + min(d, D - 4)) * __builtin_amdgcn_exp2f(s_m[k] - ref);
+        const float m = k < kMostJoined ? s_f[k] : parts.m[i];
+        v += *(const f32x4 *)(parts.o + i * D + min(d, D - 4)) * __builtin_amdgcn_exp2f(m - ref);
     }
     s_o[t / LANES][t % LANES] = v;
     __syncthreads();
@@ -563,33 +850,83 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Units units, 
     if (dim == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;
 }
 
-template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, const Units &units, hipStream_t st) {
-    k_prefix<E, DP, FULL><<<kShares, 64 * kWaves, 0, st>>>(p, units);
+// A workgroup for up to 16 query heads of a key head of a sequence.
+template <typename E, int DP, bool FULL>
+__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short(PrefixArgs p) {
+    __shared__ Narrow<E, DP, 1, kWaves> sh;
+    const AttnArgs &a = p.a;
+    const int per_seq = a.c.kv_heads * a.head_groups, b = blockIdx.x / per_seq, u = blockIdx.x - b * per_seq, lane = threadIdx.x % 64;
+    Task k;
+    k.row = uni(row_of(a, b)), k.j = u / a.head_groups, k.first = b, k.c0 = (u - k.j * a.head_groups) * 16;
+    k.columns = min(16, a.group - k.c0);
+    k.begin = k.from = 0, k.to = uni(len_of(a, k.row)), k.cut = INT32_MAX, k.skip = 0, k.shared = 0, k.lead = -1;
+    if (a.window && k.to > a.window) k.begin = k.to - a.window, k.to = a.window;
+    for (int g0 = 0; g0 < p.groups; g0 += 64) {
+        const int g = g0 + lane;
+        const int lo = g < p.groups ? p.starts[g] : 0, hi = g < p.groups ? p.starts[g + 1] : 0;
+        const uint64_t hit = __ballot(lo >= 0 && b >= lo && b < hi);
+        if (!hit) continue;
+        const int at = __ffsll((unsigned long long)hit) - 1;
+        k.shared = uni(p.shared[g0 + at]);
+        k.lead = uni(p.prefix_rows ? p.prefix_rows[g0 + at] : row_of(a, __shfl(lo, at)));
+        break;
+    }
+    if (k.from >= k.to) {   // no tokens
+        for (int i = threadIdx.x; i < k.columns * a.c.head_dim; i += 64 * kWaves) {
+            const int c = i / a.c.head_dim, h = k.j * a.group + k.c0 + c, d = i - c * a.c.head_dim;
+            ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = (E)0;
+            if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = -INFINITY;
+        }
+        return;
+    }
+    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, [&](int c, int d, float o, float m, float l) {
+        const int h = k.j * a.group + k.c0 + c;
+        ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
+        if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;
+    });
+}
+
+// Sequences of few tokens take one kernel, in which each reads what it shares by itself.
+constexpr int64_t kShort = 1024;
+bool is_short(int64_t tokens) { return tokens <= kShort; }
+
+template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, bool few, hipStream_t st) {
+    const AttnArgs &a = p.a;
+    if (few) {
+        k_prefix_short<E, DP, FULL><<<a.batch * a.c.kv_heads * a.head_groups, 64 * kWaves, 0, st>>>(p);
+        return hipGetLastError();
+    }
+    const Sizes z = sizes_of(a.c, a.batch, a.heads, p.groups);
+    k_prefix_plan<<<1, kMost, 0, st>>>(p, z, kColumns<E, DP>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const dim3 grid(p.a.batch * p.a.heads, (p.a.c.head_dim + 127) / 128);
-    k_prefix_join<E><<<grid, 256, 0, st>>>(p, units, columns_of(DP));
+    k_prefix<E, DP, FULL><<<kGrid, 64 * kTaskWaves<DP>, 0, st>>>(p, z);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    k_prefix_join<E><<<dim3(a.batch * a.heads, (a.c.head_dim + 127) / 128), 256, 0, st>>>(p, z, kColumns<E, DP>);
     return hipGetLastError();
 }
 
-template <typename E> hipError_t run(const PrefixArgs &p, const Units &units, hipStream_t st) {
+template <typename E> hipError_t run(const PrefixArgs &p, bool few, hipStream_t st) {
     const int D = p.a.c.head_dim;
-    if (D <= 64) return D == 64 ? run<E, 64, true>(p, units, st) : run<E, 64, false>(p, units, st);
-    if (D <= 128) return D == 128 ? run<E, 128, true>(p, units, st) : run<E, 128, false>(p, units, st);
-    return D == 256 ? run<E, 256, true>(p, units, st) : run<E, 256, false>(p, units, st);
+    if (D <= 64) return D == 64 ? run<E, 64, true>(p, few, st) : run<E, 64, false>(p, few, st);
+    if (D <= 128) return D == 128 ? run<E, 128, true>(p, few, st) : run<E, 128, false>(p, few, st);
+    return D == 256 ? run<E, 256, true>(p, few, st) : run<E, 256, false>(p, few, st);
 }
 
 }  // namespace
 
-int64_t prefix_workspace(const CacheArgs &c, int batch, int heads, int groups, int) {
-    const Units u = units_of(c, batch, heads, groups);
-    return space_of(nullptr, u, batch, columns_of(dims_of(c.head_dim)), std::min(16, heads / c.kv_heads), c.head_dim).bytes;
+// A window may make a call short: the workspace goes by the table alone.
+int64_t prefix_workspace(const CacheArgs &c, int batch, int heads, int groups, int width) {
+    if (is_short((int64_t)width * c.page_size)) return 0;
+    return space_of(nullptr, sizes_of(c, batch, heads, groups), batch, c.head_dim).bytes;
 }
 
 hipError_t launch_prefix(const PrefixArgs &args, hipStream_t st) {
     PrefixArgs p = args;
-    p.a.head_groups = (p.a.group + 15) / 16, p.a.shares = kShares;
-    const Units u = units_of(p.a.c, p.a.batch, p.a.heads, p.groups);
-    return p.a.c.dtype == BSP_F32 ? run<float>(p, u, st) : run<uint16_t>(p, u, st);
+    AttnArgs &a = p.a;
+    a.head_groups = (a.group + 15) / 16, a.shares = 0;
+    int64_t tokens = (int64_t)a.width * a.c.page_size;
+    if (a.window) tokens = std::min<int64_t>(tokens, a.window);
+    return a.c.dtype == BSP_F32 ? run<float>(p, is_short(tokens), st) : run<uint16_t>(p, is_short(tokens), st);
 }
 
 }  // namespace bsp

@@ -19,10 +19,20 @@ def B():
     return B
 
 
+@pytest.fixture(autouse=True, params=["short", "long"])
+def table_width(request):
+    """Tables that hold no more than the sequences need, and those that could hold long ones."""
+    Setup.least = 0 if request.param == "short" else 1100
+    yield
+    Setup.least = 0
+
+
 class Setup:
     """Groups of sequences: sizes[g] members that share shared[g] tokens and have own[g][i] of their own after them
     (or, below 0, so many fewer than are shared).  Slots that hold no token are NaN.  prefix_rows: the shared pages
     belong to sequences of their own, of whose entries the members know nothing."""
+
+    least = 0   # tokens that a table has room for
 
     def __init__(self, B, sizes, shared, own, kv, heads, dim, page, dt="bf16", order="heads", seed=0, spread=1.0, holes=0.0,
                  prefix_rows=False, extra=0):
@@ -33,7 +43,7 @@ class Setup:
         self.n, self.starts, self.shared = n, np.concatenate([[0], np.cumsum(sizes)]).astype(int), list(shared)
         lens = [max(0, shared[g] + own[g][i]) for g in range(len(sizes)) for i in range(sizes[g])] + [int(x) for x in rng.integers(0, 90, extra)]
         self.lens = lens + ([0] * len(sizes) if prefix_rows else [])
-        self.width = max([M.ceil(x, page) for x in lens + list(shared)] + [1]) + 1
+        self.width = max([M.ceil(x, page) for x in lens + list(shared)] + [M.ceil(self.least, page), 1]) + 1
         self.group = [g for g in range(len(sizes)) for _ in range(sizes[g])] + [None] * extra
         table, k = np.full((len(self.lens), self.width), -1, np.int64), 0
         for g, m in enumerate(sizes):
@@ -264,6 +274,43 @@ def test_long_prefix(B, dt, order):
 def test_one_long_prefix_few_heads(B):
     s = Setup(B, [2], [20011], [[1, 300]], 1, 1, 64, 64, "bf16", seed=10)
     s.check(*s.run(0.125), 0.125)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 72, 128, 256])
+def test_column_blocks(B, dim, dt):
+    """Groups of every number of columns that is worked on in another way, over several stages and tiles."""
+    rng = np.random.default_rng(dim)
+    sizes = [1, 4, 8, 9, 16, 17, 32, 33, 64, 71, 100]
+    shared = [int(x) for x in rng.integers(900, 2300, len(sizes))]
+    s = Setup(B, sizes, shared, [rng.integers(0, 150, m) for m in sizes], 1, 4, dim, 16, dt, "slots" if dim == 72 else "heads", seed=dim, holes=0.02)
+    s.check(*s.run(dim ** -0.5), dim ** -0.5)
+    s.check(*s.run(dim ** -0.5, feature_major=True, window=1500), dim ** -0.5, 1500)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_what_one_member_attends_to_does_not_reach_another(B, dt):
+    """NaN and Inf in tokens past the end, or before the window, of some members of a group."""
+    import torch
+    for seed, (m, group) in enumerate(((3, 2), (24, 4), (70, 4))):
+        rng = np.random.default_rng(seed)
+        s = Setup(B, [m], [1300], [[100, 40] + list(rng.integers(-900, 100, m - 2))], 1, group, 64, 16, dt, seed=seed)
+        for window in (0, 1150):
+            longest = s.run(0.125, window)[0]
+            bad = sorted((n - (window or n), n) for n in s.lens)
+            assert bad[0] != bad[-1]
+            for at, value in ((s.lens[0] - 1, float("nan")), (1250, float("inf")), (1299, float("nan")), (160, float("nan"))):
+                keys, values = s.keys.copy(), s.values.copy()
+                page, slot = s.table[0, at // 16], at % 16
+                keys[page, slot] = value
+                values[page, slot] = value
+                t = Setup.__new__(Setup)
+                t.__dict__.update(s.__dict__)
+                t.data = [t.plane(a) for a in (keys, values)]
+                y, lse = t.run(0.125, window)
+                for b in range(s.n):
+                    if (page, slot) not in s.tokens(b, window):
+                        assert torch.equal(y[b], longest[b]) or (y[b].isfinite().all() and lse[b].isfinite().all() or s.lens[b] == 0), (b, at)
 
 
 def test_scores_far_apart(B):
