@@ -27,6 +27,7 @@ constexpr int kStep = 128;              // tokens by which work is cut, and that
 constexpr int kRounds = 2;              // tasks a workgroup at most, but for what cannot be cut smaller
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
 
 // Columns of a task: staged ones only for what fits LDS and registers.
 template <typename E, int DP> constexpr int kColumns = sizeof(E) == 2 && DP <= 128 ? 256 : 32;
@@ -41,6 +42,7 @@ template <int DP> constexpr int kTaskWaves = DP == 256 ? 4 : 8;
 struct Task {
     int j, first, c0, columns, from, to;
     int row, lead, shared, begin, cut, skip;
+    int number, unused[3];   // among all tasks
 };
 struct Member {
     int task, blocks, pieces, place;   // the group's first task, column blocks, pieces; place in the group
@@ -93,7 +95,7 @@ __host__ __device__ inline Space space_of(void *workspace, const Sizes &z, int b
         return p;
     };
     s.head = (Head *)take(sizeof(Head)), s.member = (Member *)take((int64_t)batch * sizeof(Member));
-    s.task = (Task *)take((z.shared_tasks + z.own_tasks) * sizeof(Task));
+    s.task = (Task *)take((kGrid + z.shared_tasks + z.own_tasks) * sizeof(Task));
     s.shared = parts(z.shared_tasks, z.columns), s.own = parts(z.own_tasks, z.own_columns);
     s.bytes = at - (char *)workspace;
     return s;
@@ -111,7 +113,7 @@ __device__ __forceinline__ int cost_of(bool f32, int columns, int blocks) {
 }
 
 // Inclusive scan of one value a thread over the workgroup.
-template <int WAVES, typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wave, F join) {
+template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wave, F join) {
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
     for (int d = 1; d < 64; d *= 2) {
         const T o = __shfl_up(v, d);
@@ -124,15 +126,17 @@ template <int WAVES, typename T, typename F> __device__ __forceinline__ T scan(T
     return v;
 }
 
-// A workgroup, a thread for a group and for a sequence.  Bound by latency: a chain of some ten accesses.
+// A workgroup, a thread for a group and for a sequence: as many waves as these need, since each wave makes every
+// scan and sum longer.  Bound by latency.
 __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
-    constexpr int W = kMost / 64;
-    __shared__ int s_lo[kMost + 1], s_from[kMost], s_to[kMost], s_wave[W];
+    constexpr int MOST = kMost / 64;
+    const int T = blockDim.x, W = T / 64;
+    __shared__ int s_lo[kMost + 1], s_from[kMost], s_to[kMost], s_wave[MOST];
     __shared__ int s_task[2 * kMost + 1], s_pieces[2 * kMost], s_steps[2 * kMost];
     __shared__ struct {
         int row, lead, shared, begin, cut, skip, len;
     } s_own[kMost];
-    __shared__ int64_t s_sum[W][4];
+    __shared__ int64_t s_sum[MOST][4];
     const AttnArgs &a = p.a;
     const int t = threadIdx.x, G = p.groups, B = a.batch;
     const Space space = space_of(a.workspace, z, B, a.c.head_dim);
@@ -144,12 +148,12 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
     int group = -1, lead = -1, common = 0, core_from = 0, core_to = 0;
     if (G) {
         // bounds of groups in order and within the batch, whatever starts holds
-        const int mine = t <= G ? bound(t) : 0, last = G == kMost && t == 0 ? bound(G) : 0;
-        const int lo = scan<W>(mine, s_wave, [](int x, int y) { return max(x, y); });
+        const int mine = t <= G ? bound(t) : 0, last = G == T && t == 0 ? bound(G) : 0;
+        const int lo = scan(mine, s_wave, [](int x, int y) { return max(x, y); });
         if (t <= G) s_lo[t] = lo;
         s_from[t] = s_to[t] = 0;
         __syncthreads();
-        if (G == kMost && t == 0) s_lo[G] = max(last, s_lo[G - 1]);
+        if (G == T && t == 0) s_lo[G] = max(last, s_lo[G - 1]);
         __syncthreads();
         if (t < B) {
             int x = 0, y = G;   // the last group that begins at or before t
@@ -207,11 +211,12 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
     // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks in all, in
     // rounds of the card, at the cost of the largest.
     auto pieces_of = [&](const Item &i, int64_t most) {
-        return i.units ? (int)max((int64_t)1, min((int64_t)i.steps, ((int64_t)i.steps * i.cost + most - 1) / most)) : 0;
+        // in fp64, which holds these whole numbers, as a division of 64 bits takes a hundred instructions
+        return i.units ? max(1, min(i.steps, (int)min(ceil((double)i.steps * i.cost / (double)most), 1e9))) : 0;
     };
     int64_t best = INT64_MAX, most = 1;
     for (int r = 1; r <= kRounds; ++r) {
-        const int64_t m = max((int64_t)(2 * kTaskCost), (total + kGrid * r - 1) / (kGrid * r));
+        const int64_t m = max((int64_t)(2 * kTaskCost), (int64_t)ceil((double)total / (kGrid * r)));
         int64_t tasks = 0, cost = 0;
         for (int k = 0; k < 2; ++k) {
             const int n = pieces_of(item[k], m);
@@ -233,9 +238,9 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
     int first_task[2], before = 0;
     for (int k = 0; k < 2; ++k) {
         const int n = pieces_of(item[k], most), count = n * item[k].units;
-        const int upto = scan<W>(count, s_wave, [](int x, int y) { return x + y; });
+        const int upto = scan(count, s_wave, [](int x, int y) { return x + y; });
         __syncthreads();
-        if (t == kMost - 1) s_wave[0] = upto;
+        if (t == T - 1) s_wave[0] = upto;
         __syncthreads();
         first_task[k] = before + upto - count;
         const int items = k ? B : G, at = k ? G : 0;
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
         }
         space.member[t] = m;
     }
-    for (int task = t; task < before; task += kMost) {
+    for (int task = t; task < before; task += T) {
         int x = 0, y = G + B;   // the last item that begins at or before the task, which has tasks
         while (y - x > 1) {
             const int mid = (x + y) / 2;
@@ -280,9 +285,18 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
             k.row = s_own[b].row, k.lead = s_own[b].lead, k.shared = s_own[b].shared;
             k.begin = s_own[b].begin, k.cut = s_own[b].cut, k.skip = s_own[b].skip, end = s_own[b].len;
         }
-        k.from = (int)((int64_t)steps * piece / n) * kStep, k.to = min(end, (int)((int64_t)steps * (piece + 1) / n) * kStep);
-        space.task[task] = k;
+        const int each_steps = steps / n, more = steps - each_steps * n;   // the first `more` pieces have one step more
+        k.from = (each_steps * piece + min(piece, more)) * kStep;
+        k.to = min(end, (each_steps * (piece + 1) + min(piece + 1, more)) * kStep);
+        k.number = task;
+        // The first tasks go by workgroup: those that read the same to the same XCD, whose L2 then holds it.
+        const int each = (min(before, kGrid) + 7) / 8;
+        space.task[task < kGrid ? task % each * 8 + task / each : task] = k;
     }
+    // workgroups for which there is none
+    const int each = (min(before, kGrid) + 7) / 8;
+    for (int i = t; i < kGrid; i += T)
+        if (i / 8 >= each || i % 8 * each + i / 8 >= before) space.task[i].number = -1;
 }
 
 // ---- up to 32 columns --------------------------------------------------------------------------------
@@ -318,6 +332,23 @@ __device__ __forceinline__ int64_t place_in(const AttnArgs &a, const Task &k, in
     return place_of(a.c, a.table, t < k.shared ? k.lead : k.row, a.seqs, a.width, t);
 }
 
+// Queries of a task's columns to LDS, put(column, dimension, value), 0 past the columns and head_dim: every thread
+// has a column, so that what divides is done once.
+template <typename E, int COLUMNS, int DP, int THREADS, typename P>
+__device__ __forceinline__ void stage_queries(const AttnArgs &a, const Task &k, P put) {
+    const Scale scale(a.scale);
+    constexpr int EACH = THREADS / COLUMNS, AHEAD = DP / EACH < 16 ? DP / EACH : 16;   // dimensions at a time; loads under way
+    const int c = threadIdx.x % COLUMNS, at = k.c0 + min(c, k.columns - 1), s = at / a.group, D = a.c.head_dim;
+    const E *q = (const E *)a.q + (k.first + s) * a.qs.seq + (k.j * a.group + at - s * a.group) * a.qs.head;
+    for (int d0 = threadIdx.x / COLUMNS; d0 < DP; d0 += EACH * AHEAD) {
+        E v[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v[i] = q[min(d0 + i * EACH, D - 1) * a.qs.dim];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) put(c, d0 + i * EACH, c < k.columns && d0 + i * EACH < D ? scale.of(v[i]) : (E)0);
+    }
+}
+
 // N sixteens of columns over a task's tokens.  finish(column, d, output, reference, sum) takes what comes of
 // them, joined over the waves.
 template <typename E, int DP, bool FULL, int N, int WAVES, typename F>
@@ -334,10 +365,10 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
     St st;
     typename St::Quad q[N][St::NK];
     f32x4 acc[N][NV][VW];
-    float m[N], l[N];
+    float m[N], ref[N], l[N];   // ref: m, or 0 before any
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        m[n] = -INFINITY, l[n] = 0.f;
+        m[n] = -INFINITY, ref[n] = l[n] = 0.f;
 #pragma unroll
         for (int h = 0; h < NV; ++h)
 #pragma unroll
@@ -349,18 +380,8 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
         if (base > k.from) __syncthreads();   // places of the tile before are no longer read
         for (int t = threadIdx.x; t < padded; t += THREADS)
             sh.place[t] = place_in(a, k, base + t);
-        if (base == k.from) {   // queries come while the places do, along the way they lie; 0 past columns and head_dim
-            const bool by_column = a.qs.dim != 1;
-            for (int i = threadIdx.x; i < 16 * N * DP; i += THREADS) {
-                const int c = by_column ? i % (16 * N) : i / DP, d = by_column ? i / (16 * N) : i % DP, at = k.c0 + c;
-                E v = (E)0;
-                if (c < k.columns && d < D) {
-                    const int s = at / a.group;
-                    v = scale.of(((const E *)a.q)[(k.first + s) * a.qs.seq + (k.j * a.group + at - s * a.group) * a.qs.head + d * a.qs.dim]);
-                }
-                sh.q[c][d] = v;
-            }
-        }
+        if (base == k.from)   // queries come while the places do
+            stage_queries<E, 16 * N, DP, THREADS>(a, k, [&](int c, int d, E v) { sh.q[c][d] = v; });
         __syncthreads();
         if (base == k.from)
 #pragma unroll
@@ -413,7 +434,7 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
                     float to = fmaxf(top[c], __shfl_xor(top[c], 16));
                     to = fmaxf(m[c], fmaxf(to, __shfl_xor(to, 32)));
                     const float keep = m[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[c] - to);
-                    m[c] = to, l[c] *= keep;
+                    m[c] = to, ref[c] = to == -INFINITY ? 0.f : to, l[c] *= keep;
 #pragma unroll
                     for (int h = 0; h < NV; ++h)
 #pragma unroll
@@ -421,12 +442,10 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
                 }
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const float ref = m[c] == -INFINITY ? 0.f : m[c];
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < TT; ++i) {
-                    s[c][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][i], scale.by, -ref));
-                    if (!whole && (dead >> i & 1)) s[c][i] = 0.f;
+                    s[c][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][i], scale.by, -ref[c]));
                     sum += s[c][i];
                 }
                 l[c] += sum;
@@ -500,12 +519,20 @@ template <int DP> struct Wide {
 };
 template <int DP> __device__ __forceinline__ int turn_of(int row) { return DP == 128 ? row & 15 : row >> 1 & 7; }
 
-// 16 bytes from each lane's source to LDS byte address base + 16 lane; counted as one load of the wave.
-__device__ __forceinline__ void copy16(const void *src, uint32_t base) {
+// N times 16 bytes from each lane's sources to LDS, byte address base + 1024 i + 16 lane; counted as N loads of the
+// wave.  The offset moves source and destination alike.
+template <int N> __device__ __forceinline__ void copy16(const char *const *src, uint32_t base) {
     uint32_t saved;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-                 : "=&s"(saved) : "v"(src), "s"(base) : "memory");
+    static_assert(N == 2 || N == 4, "");
+    if constexpr (N == 2)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:1024\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved) : "v"(src[0]), "v"(src[1] - 1024), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:1024\n\t"
+                     "global_load_lds_dwordx4 %3, off offset:2048\n\tglobal_load_lds_dwordx4 %4, off offset:3072\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved) : "v"(src[0]), "v"(src[1] - 1024), "v"(src[2] - 2048), "v"(src[3] - 3072), "s"(base) : "memory");
 }
 
 // CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.
@@ -532,19 +559,27 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
         if (hole) sh.holes[tile % 2] = 1;
     };
     // A wave copies 1 KB at a time of a stage's keys and values, each lane 16 bytes of the row that they belong to.
+    constexpr int ROWS = 64 / GR, N = kStep / ROWS / 8;   // rows of a copy, copies of a wave
     auto copy = [&](int s) {
-        constexpr int ROWS = 64 / GR, N = kStep / ROWS / 8;   // rows of a copy, copies of a wave
-        const uint32_t to = stage0 + (uint32_t)(s % 2 * 2 * kStep * DP * 2);
+        const uint32_t to = (uint32_t)uni((int)(stage0 + (uint32_t)(s % 2 * 2 * kStep * DP * 2) + wave * N * 1024));
+        const int64_t *place = &sh.place[s * kStep / kTile % 2][s * kStep % kTile + wave * N * ROWS + lane / GR];
+        int64_t at[N];
+        bool all = true;
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] = place[i * ROWS], all &= at[i] >= 0;
+        const char *ks[N], *vs[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int part = wave * N + i, row = part * ROWS + lane / GR, g = lane % GR ^ turn_of<DP>(row);
-            const int64_t at = sh.place[s * kStep / kTile % 2][(s * kStep + row) % kTile];
-            const bool in = at >= 0 && (FULL || g * 8 < D);
-            const void *ks = in ? (const void *)(keys + at + g * 8) : zero, *vs = in ? (const void *)(values + at + g * 8) : zero;
-            const uint32_t base = uni((int)(to + part * 1024));
-            copy16(ks, base);
-            copy16(vs, base + kStep * DP * 2);
+            const int g = lane % GR ^ turn_of<DP>(i * ROWS + lane / GR);   // of the wave's rows, which begin at a multiple of 16
+            ks[i] = (const char *)(keys + g * 8) + 2 * at[i], vs[i] = (const char *)(values + g * 8) + 2 * at[i];
+            if (!FULL && g * 8 >= D) ks[i] = vs[i] = (const char *)zero;
         }
+        if (__any(!all))
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (at[i] < 0) ks[i] = vs[i] = (const char *)zero;
+        copy16<N>(ks, to);
+        copy16<N>(vs, to + kStep * DP * 2);
     };
 
     const int stages = (k.to - k.from + kStep - 1) / kStep;
@@ -554,37 +589,36 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
 #pragma unroll
     for (int i = 0; i < kTile / 512; ++i) ahead[i] = place_in(a, k, k.from + threadIdx.x + 512 * i);
     fill_places(0, ahead);
-    // queries, through the second stage: 0 past columns and head_dim
-    {
-        E *q = sh.stage[1][0];
-        const bool by_column = a.qs.dim != 1;
-        for (int i = threadIdx.x; i < CW * 32 * DP; i += 512) {
-            const int c = by_column ? i % (CW * 32) : i / DP, d = by_column ? i / (CW * 32) : i % DP, at = k.c0 + c;
-            E v = 0;
-            if (c < k.columns && d < D) {
-                const int s = at / a.group;
-                v = scale.of(((const E *)a.q)[(k.first + s) * a.qs.seq + (k.j * a.group + at - s * a.group) * a.qs.head + d * a.qs.dim]);
-            }
-            q[c * DP + ((d / 8 ^ turn_of<DP>(c)) * 8 + d % 8)] = v;
-        }
-    }
+    // queries, through the second stage
+    stage_queries<E, CW * 32, DP, 512>(a, k, [&](int c, int d, E v) {
+        sh.stage[1][0][c * DP + ((d / 8 ^ turn_of<DP>(c)) * 8 + d % 8)] = v;
+    });
     __syncthreads();
     copy(0);
     u32x4 q[2][NC];
     f32x4 acc[2][ND];
-    float m[2], l[2];
+    float m[2], ref[2], l[2];   // ref: m, or 0 before any
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         const int c = c_wave + n * 16 + r;
 #pragma unroll
         for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)&sh.stage[1][0][c * DP + ((i * 4 + quad) ^ turn_of<DP>(c)) * 8];
-        m[n] = -INFINITY, l[n] = 0.f;
+        m[n] = -INFINITY, ref[n] = l[n] = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[n][d] = (f32x4){0, 0, 0, 0};
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 
+    // where a lane reads in a stage: its part of a key, and its four tokens' values
+    uint32_t k_at[NC], v_at[ND];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) k_at[i] = stage0 + (r * DP + ((i * 4 + quad) ^ turn_of<DP>(r)) * 8) * 2;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {   // of sixteen lanes, lane i names token i / 4 and four dimensions, and gets one dimension of four tokens
+        const int row = 4 * quad + r / 4;
+        v_at[d] = stage0 + (kStep * DP + row * DP + ((2 * d + r % 4 / 2) ^ turn_of<DP>(row)) * 8 + r % 2 * 4) * 2;
+    }
     for (int s = 0; s < stages; ++s) {
         // the next stage comes, and with a tile's first stage the places of the next tile
         const bool more_places = s * kStep % kTile == 0 && (s * kStep / kTile + 1) * kTile < k.to - k.from;
@@ -592,38 +626,59 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
         if (more_places)
 #pragma unroll
             for (int i = 0; i < kTile / 512; ++i) ahead[i] = place_in(a, k, k.from + (s * kStep / kTile + 1) * kTile + threadIdx.x + 512 * i);
-        const E *ks = sh.stage[s % 2][0], *vs = sh.stage[s % 2][1];
+        uint32_t ka[NC], va[ND];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) ka[i] = k_at[i] + (uint32_t)((s % 2 * 2 * kStep + set * TOKENS) * DP * 2);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) va[d] = v_at[d] + (uint32_t)((s % 2 * 2 * kStep + set * TOKENS) * DP * 2);
         const bool holes = sh.holes[s * kStep / kTile % 2];
+#pragma unroll 1
         for (int t0 = set * TOKENS; t0 < (set + 1) * TOKENS; t0 += 32) {
             const int token = k.from + s * kStep + t0;
             if (token >= k.to) break;
             float p[2][8];
-            // scores of 32 tokens: rows are tokens, columns queries
+            // Scores of 32 tokens: rows are tokens, columns queries.  All reads of a step go out before what waits for them.
+            u32x4 kv[2][NC];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int row = t0 + 16 * t + r;
-                f32x4 c4[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+            for (int i = 0; i < NC; ++i)
 #pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    const u32x4 kv = *(const u32x4 *)&ks[row * DP + ((i * 4 + quad) ^ turn_of<DP>(row)) * 8];
+                for (int t = 0; t < 2; ++t) kv[t][i] = *(lds_u32x4 *)(uintptr_t)(ka[i] + 16 * t * DP * 2);
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 c4[2][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) c4[n][t] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
-                        c4[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kv), as_bf16x8(q[n][i]), c4[n], 0, 0, 0);
-                }
+                        c4[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kv[t][i]), as_bf16x8(q[n][i]), c4[n][t], 0, 0, 0);
+            u32x2 w[ND][2];
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    w[d][t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(va[d] + 16 * t * DP * 2)));
+#pragma unroll
+            for (int i = 0; i < NC; ++i) ka[i] += 32 * DP * 2;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) va[d] += 32 * DP * 2;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[n][4 * t + i] = c4[n][i];
-            }
-            const bool whole = !holes && token + 32 <= k.to;
-            uint32_t dead = 0;   // a lane's tokens that hold nothing; their keys and values came as 0
-            if (!whole)
+                    for (int i = 0; i < 4; ++i) p[n][4 * t + i] = c4[n][t][i];
+            // tokens that hold nothing, whose keys and values came as 0: their scores are -Inf, and so what they weigh 0
+            if (holes || token + 32 > k.to)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (sh.place[s * kStep / kTile % 2][(s * kStep + t0 + 16 * (i / 4) + 4 * quad + i % 4) % kTile] < 0) {
-                        dead |= 1u << i;
+                    if (sh.place[s * kStep / kTile % 2][(s * kStep + t0 + 16 * (i / 4) + 4 * quad + i % 4) % kTile] < 0)
                         p[0][i] = p[1][i] = -INFINITY;
-                    }
             float top[2];
             bool past = false;
 #pragma unroll
@@ -640,19 +695,17 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
                     float to = fmaxf(top[n], __shfl_xor(top[n], 16));
                     to = fmaxf(m[n], fmaxf(to, __shfl_xor(to, 32)));
                     const float keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - to);
-                    m[n] = to, l[n] *= keep;
+                    m[n] = to, ref[n] = to == -INFINITY ? 0.f : to, l[n] *= keep;
 #pragma unroll
                     for (int d = 0; d < ND; ++d) acc[n][d] *= keep;
                 }
             u32x4 b[2][2];   // a probability is the sum of two bf16, as in k_attn
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const float ref = m[n] == -INFINITY ? 0.f : m[n];
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    p[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][i], scale.by, -ref));
-                    if (!whole && (dead >> i & 1)) p[n][i] = 0.f;
+                    p[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][i], scale.by, -ref[n]));
                     sum += p[n][i];
                 }
                 l[n] += sum;
@@ -662,18 +715,10 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
                     b[n][1][i] = pack_bf16(p[n][2 * i] - bf16_to_f32(b[n][0][i]), p[n][2 * i + 1] - __uint_as_float(b[n][0][i] & 0xffff0000u));
                 }
             }
-            // outputs: rows are dimensions; of sixteen lanes, lane i names token i / 4 and four dimensions, and gets
-            // one dimension of four tokens
-            const int row = t0 + 4 * quad + r / 4;
+            // outputs: rows are dimensions
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-                u32x2 w[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const E *at = &vs[(row + 16 * t) * DP + ((2 * d + r % 4 / 2) ^ turn_of<DP>(row + 16 * t)) * 8 + r % 2 * 4];
-                    w[t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const E *)at));
-                }
-                const bf16x8 v = as_bf16x8((u32x4){w[0].x, w[0].y, w[1].x, w[1].y});
+                const bf16x8 v = as_bf16x8((u32x4){w[d][0].x, w[d][0].y, w[d][1].x, w[d][1].y});
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -752,20 +797,18 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
     const AttnArgs &a = p.a;
     const Space space = space_of(a.workspace, z, a.batch, a.c.head_dim);
     const int tasks = uni(space.head->tasks), shared = uni(space.head->shared);
-    // the first tasks by place: those that read the same on the same XCD, whose L2 then holds it
-    const int each = (min(tasks, kGrid) + 7) / 8;
-    int task = (int)blockIdx.x / 8 < each ? blockIdx.x % 8 * each + blockIdx.x / 8 : tasks;
-    if (tasks < kGrid && task >= tasks) return;
-    while (task < tasks) {
-        const Task *at = space.task + task;
+    int slot = blockIdx.x;   // of the task; later ones have their own number's
+    for (;;) {
+        const Task *at = space.task + slot;
         Task k;
         k.j = uni(at->j), k.first = uni(at->first), k.c0 = uni(at->c0), k.columns = uni(at->columns), k.from = uni(at->from);
         k.to = uni(at->to), k.row = uni(at->row), k.lead = uni(at->lead), k.shared = uni(at->shared), k.begin = uni(at->begin);
-        k.cut = uni(at->cut), k.skip = uni(at->skip);
+        k.cut = uni(at->cut), k.skip = uni(at->skip), k.number = uni(at->number);
+        if (k.number < 0) return;
         if (tasks > kGrid && threadIdx.x == 0) sh.next = atomicAdd(&space.head->next, 1);
-        const bool common = task < shared;
+        const bool common = k.number < shared;
         const Parts parts = common ? space.shared : space.own;
-        const int64_t number = common ? task : task - shared;
+        const int64_t number = common ? k.number : k.number - shared;
         auto finish = [&](int c, int d, float o, float m, float l) {
             const int64_t i = parts.at(number, c);
             parts.o[i * a.c.head_dim + d] = o;
@@ -784,8 +827,9 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
             else
                 columns_wide<DP, FULL, 8>(a, sh.wide, k, zero, parts, number);
         }
-        if (tasks <= kGrid) break;
-        task = uni(sh.next);
+        if (tasks <= kGrid) return;
+        slot = uni(sh.next);
+        if (slot >= tasks) return;
         __syncthreads();   // read before the next one is written
     }
 }
@@ -897,7 +941,7 @@ template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, boo
         return hipGetLastError();
     }
     const Sizes z = sizes_of(a.c, a.batch, a.heads, p.groups);
-    k_prefix_plan<<<1, kMost, 0, st>>>(p, z, kColumns<E, DP>);
+    k_prefix_plan<<<1, std::max(256, (a.batch + 63) / 64 * 64), 0, st>>>(p, z, kColumns<E, DP>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     k_prefix<E, DP, FULL><<<kGrid, 64 * kTaskWaves<DP>, 0, st>>>(p, z);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
