@@ -2,7 +2,14 @@
 //
 // What is kept is always the first of the tokens in order (falling logit, rising index), so that it is
 // told by a logit and by how many of the tokens that have just it are kept.  Both are found without a sort, by
-// counting and by adding up whole numbers, which has no order that could show.
+// counting and by adding up whole numbers, which has no order that could show: tokens fall into bins by
+// their logit's distance from the largest, and the bin in which a cut falls is cut further by the bits of
+// its keys.
+//  * Rows of up to 32768 tokens stay in the LDS of a workgroup (k_sample_row).
+//  * Of longer ones k_sample_scan finds the largest logits, k_sample_bins fills the bins of each chunk, and in
+//    k_sample_pick a workgroup a row finds cuts and token; it reads again the tokens of the bins where the cuts
+//    are, and one chunk.
+//  * Rows whose elements lie apart are laid out by k_sample_scan.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -14,8 +21,12 @@ namespace bsp {
 
 namespace {
 
-constexpr int kRowThreads = 1024, kWaves = kRowThreads / 64;
 constexpr double kOne = 8796093022208.0;   // 2^43: what a weight of 1 counts; 2^20 of them stay below 2^63
+constexpr int kBins = 1024, kSpan = 32;    // bins, and the distance that they cover: e^-32 is below 2^-44
+constexpr int kScan = 2048;                // tokens whose largest logit k_sample_scan finds
+constexpr int kChunk = 8192;               // tokens whose bins k_sample_bins fills
+constexpr int kRow = 32768;                // tokens that a workgroup holds in LDS
+constexpr int kList = 4096;                // tokens of a bin that k_sample_pick holds in LDS
 
 // Logits as numbers that are in the same order; NaN and -Inf, which are never taken, are 0.
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -23,172 +34,344 @@ __device__ __forceinline__ uint32_t key_of(float l) {
     const uint32_t u = __float_as_uint(l + 0.f);   // -0 as 0
     return u >> 31 ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ uint32_t key_of(uint16_t l) { return key_of(bf16_to_f32(l)); }
+__device__ __forceinline__ uint32_t key_of(uint32_t key) { return key; }   // laid out by k_sample_scan
 __device__ __forceinline__ float logit_of(uint32_t key) {
     return key == 0 ? -INFINITY : __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
 }
 
+typedef __attribute__((ext_vector_type(4))) uint16_t u16x4;
+
 struct Row {
-    float top;        // the largest logit
-    double inv;       // 1 / temperature; 0 for the largest logit only
+    uint32_t top_key;
+    float top;           // the largest logit
+    double steps;        // 64 / (temperature ln 2)
+    float bins;          // of a distance of 1
     bool greedy;
-    __device__ __forceinline__ double weight(float l) const {   // in units of 1
-        if (l == top) return 1.0;
-        if (greedy || !(l > -INFINITY) || top == INFINITY) return 0.0;
-        return exp(((double)l - top) * inv);
+    const double *powers;   // 2^(i / 64)
+
+    __device__ __forceinline__ Row(const SampleArgs &a, int b, uint32_t key, const double *p) : top_key(key), powers(p) {
+        const float t = a.temperature ? a.temperature[b] : 1.f;
+        greedy = !(t > 0.f);
+        top = logit_of(key), steps = 92.332482616893656877 / t, bins = (float)((double)(kBins / kSpan) / t);
     }
-    __device__ __forceinline__ uint64_t mass(float l) const { return (uint64_t)rint(weight(l) * kOne); }
+    // The weight in units of 2^-43.  2^(x / 64) for x = i + f, |f| <= 1/2, is 2^(i / 64) (1 + ... + (f ln 2 / 64)^5 / 120),
+    // to 2^-53; adding 2^52 rounds to a whole number, to the nearest, ties to even.
+    __device__ __forceinline__ uint64_t mass(uint32_t key) const {
+        if (key == top_key) return (uint64_t)kOne;
+        const double x = ((double)logit_of(key) - (double)top) * steps;
+        if (!(x > -64.0 * 46)) return 0;   // also where the largest is Inf, or the key that of no token
+        const double whole = rint(x), r = (x - whole) * 0.010830424696249145;
+        double p = __builtin_fma(r, 1.0 / 120, 1.0 / 24);
+        p = __builtin_fma(p, r, 1.0 / 6), p = __builtin_fma(p, r, 0.5), p = __builtin_fma(p, r, 1.0), p = __builtin_fma(p, r, 1.0);
+        const int i = (int)whole;
+        const double w = __builtin_ldexp(p * powers[i & 63], 43 + (i >> 6));
+        return __builtin_bit_cast(uint64_t, w + 0x1p52) - __builtin_bit_cast(uint64_t, 0x1p52);
+    }
+    // Whether the weight is at least min_p.
+    __device__ __forceinline__ bool reaches(uint32_t key, float min_p) const {
+        if (key == top_key) return true;
+        if (top == INFINITY) return !(0.f < min_p);
+        return !(exp(((double)logit_of(key) - (double)top) * (steps * 0.010830424696249145)) < min_p);
+    }
+    // Never less for a smaller logit, as each rounding keeps the order.
+    __device__ __forceinline__ int bin(uint32_t key) const {
+        if (key == top_key) return 0;
+        const float x = (top - logit_of(key)) * bins;
+        return x < (float)(kBins - 1) ? (int)x : kBins - 1;   // not a number (Inf * 0): the last
+    }
+};
+constexpr uint32_t kLeast = 0x00800000u;   // key of the smallest number
+
+template <int THREADS> struct Scratch {
+    static constexpr int WAVES = THREADS / 64;
+    uint64_t mass[2][kBins];   // of bins, and of the pieces into which one is cut
+    double powers[64];
+    uint64_t part[2][WAVES], found[4];
+    uint32_t count[2][kBins], key[WAVES];
 };
 
-// Sum over the workgroup, for all its threads.
-template <typename T> __device__ __forceinline__ T sum_of(T v, T *s_part) {
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+// Inclusive scan over the workgroup.
+template <int THREADS, typename T> __device__ __forceinline__ T scan(T v, T *s_part) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (int d = 1; d < 64; d *= 2) {
+        const T o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();
+    if (lane == 63) s_part[wave] = v;
+    __syncthreads();
+    T before = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) before += w < wave ? s_part[w] : 0;
+    return v + before;
+}
+// Largest over the workgroup, for all.
+template <int THREADS> __device__ __forceinline__ uint32_t largest(uint32_t v, uint32_t *s_part) {
+    for (int d = 1; d < 64; d *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, d));
     __syncthreads();
     if (threadIdx.x % 64 == 0) s_part[threadIdx.x / 64] = v;
     __syncthreads();
-    T all = 0;
-    for (int w = 0; w < kWaves; ++w) all += s_part[w];
-    return all;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) v = max(v, s_part[w]);
+    return v;
 }
 
-// A row's tokens down to a logit, and of those that have it the first `equal`.
+template <int THREADS> __device__ __forceinline__ void start(Scratch<THREADS> &s) {
+    if (threadIdx.x < 64) s.powers[threadIdx.x] = exp2(threadIdx.x / 64.0);
+}
+template <int THREADS> __device__ __forceinline__ void clear(Scratch<THREADS> &s, int which) {
+    for (int i = threadIdx.x; i < kBins; i += THREADS) s.count[which][i] = 0, s.mass[which][i] = 0;
+}
+template <int THREADS> __device__ __forceinline__ void add(Scratch<THREADS> &s, int which, int bin, uint64_t mass) {
+    atomicAdd(&s.count[which][bin], 1u);
+    if (mass) atomicAdd((unsigned long long *)&s.mass[which][bin], (unsigned long long)mass);
+}
+
+// The first bin up to which `target` tokens, or that much mass, come together; there is one.
+struct Found {
+    int bin;
+    uint64_t count_before, mass_before, count;
+};
+template <int THREADS> __device__ __forceinline__ Found locate(Scratch<THREADS> &s, int which, bool by_mass, uint64_t target) {
+    constexpr int PER = kBins / THREADS;
+    const int t = threadIdx.x;
+    uint64_t count = 0, mass = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) count += s.count[which][t * PER + i], mass += s.mass[which][t * PER + i];
+    uint64_t counts = scan<THREADS>(count, s.part[0]), masses = scan<THREADS>(mass, s.part[1]);
+    const uint64_t upto = by_mass ? masses : counts, before = upto - (by_mass ? mass : count);
+    if (before < target && target <= upto) {
+        counts -= count, masses -= mass;
+        int i = t * PER;
+        for (; i < t * PER + PER - 1; ++i) {
+            if ((by_mass ? masses + s.mass[which][i] : counts + s.count[which][i]) >= target) break;
+            counts += s.count[which][i], masses += s.mass[which][i];
+        }
+        s.found[0] = i, s.found[1] = counts, s.found[2] = masses, s.found[3] = s.count[which][i];
+    }
+    __syncthreads();
+    const Found f = {(int)s.found[0], s.found[1], s.found[2], s.found[3]};
+    __syncthreads();
+    return f;
+}
+
+// Of the keys lo .. hi that each(f) calls f with, in any order, the one down to which `target` of them, or that much of
+// mass(key), come together; ten bits at a time.  `count`: how many have it.
+template <int THREADS, typename F, typename M>
+__device__ __forceinline__ Found select(Scratch<THREADS> &s, uint32_t lo, uint32_t hi, bool by_mass, uint64_t target, F each, M mass,
+                                        uint32_t *key) {
+    uint64_t counts = 0, masses = 0;
+    for (;;) {
+        const int shift = max(0, 32 - (hi == lo ? 32 : __clz((int)(hi - lo))) - 10);
+        clear(s, 1);
+        __syncthreads();
+        each([&](uint32_t k) {
+            if (k >= lo && k <= hi) add(s, 1, (int)((hi - k) >> shift), mass(k));
+        });
+        __syncthreads();
+        Found f = locate(s, 1, by_mass, target);
+        target -= by_mass ? f.mass_before : f.count_before;
+        counts += f.count_before, masses += f.mass_before;
+        const uint32_t top = hi - ((uint32_t)f.bin << shift);
+        if (shift == 0) {
+            *key = top;
+            f.count_before = counts, f.mass_before = masses;
+            return f;
+        }
+        lo = max((int64_t)lo, (int64_t)top - ((1ll << shift) - 1)), hi = top;
+    }
+}
+
+// The first key of lo .. hi for which `holds`, which does for all above and for hi: by a wave, 64 places at a time.
+template <typename P> __device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, P holds) {
+    while (lo < hi) {
+        const uint32_t step = (hi - lo - 1) / 64 + 1;
+        const uint64_t at = lo + (uint64_t)(threadIdx.x % 64) * step;
+        const uint64_t hit = __ballot(at >= hi || holds((uint32_t)at));
+        const int first = hit ? __ffsll((unsigned long long)hit) - 1 : 64;   // of 64 places
+        hi = (uint32_t)min((uint64_t)hi, lo + (uint64_t)first * step);
+        if (first) lo += (first - 1) * step + 1;
+    }
+    return hi;
+}
+
+// What is kept of a row: tokens whose key is above, and of those that have it the ones up to an index.
 struct Kept {
-    uint32_t key;
-    uint32_t equal;
+    uint32_t key, index;
 };
 
-// A workgroup for a row, which is read again for each step.
-template <typename E> __global__ __launch_bounds__(kRowThreads) void k_sample(SampleArgs a) {
-    __shared__ uint64_t s_part[kWaves], s_mass[256], s_seg[kWaves + 1];
-    __shared__ uint32_t s_count[256], s_pick[2];
-    __shared__ uint64_t s_rest;
-    const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
-    const E *row = (const E *)a.logits + b * a.row_stride;
-    auto logit = [&](int i) { return logit_of(key_of(to_f32(row[i * a.token_stride]))); };
+// Finds it for a row whose bins are filled.  prepare(lo, hi, count) is told the keys that are asked for next, and how many
+// tokens have them; each_key(f) calls f(key) and each_token(f) f(key, index) for these at least.
+template <int THREADS, typename R, typename K, typename T>
+__device__ __forceinline__ Kept cut(const SampleArgs &a, int b, Scratch<THREADS> &s, const Row &row, uint64_t live, uint64_t all, R prepare,
+                                    K each_key, T each_token) {
+    const int top_k = a.top_k ? a.top_k[b] : 0;
+    const float top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
+    const bool by_k = top_k > 0 && (uint64_t)top_k < live, by_p = top_p < 1.f;
+    uint32_t key = kLeast;
+    uint64_t equal = UINT64_MAX, have = 0;   // of those that have the key: kept, and in all
+    auto range = [&](const Found &f, uint32_t *lo, uint32_t *hi) {
+        *hi = f.bin == 0 ? row.top_key : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) < f.bin; }) - 1;
+        *lo = f.bin == kBins - 1 ? kLeast : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) <= f.bin; });
+        prepare(*lo, *hi, f.count);
+    };
+    auto mass = [&](uint32_t k) { return row.mass(k); };
+    uint32_t lo, hi;
+    if (by_k) {
+        const Found in = locate(s, 0, false, (uint64_t)top_k);
+        range(in, &lo, &hi);
+        const Found at = select(s, lo, hi, false, top_k - in.count_before, each_key, [&](uint32_t k) { return by_p ? row.mass(k) : 0; }, &key);
+        equal = top_k - in.count_before - at.count_before, have = at.count;
+        all = in.mass_before + at.mass_before + equal * row.mass(key);
+    }
+    if (by_p) {
+        const uint64_t target = max((uint64_t)1, (uint64_t)ceil(fmax((double)top_p, 0.0) * (double)all));
+        const Found in = locate(s, 0, true, target);   // at most the bin of the first cut, of which not all is kept
+        range(in, &lo, &hi);
+        uint32_t at_key;
+        const Found at = select(s, max(lo, key), hi, true, target - in.mass_before, each_key, mass, &at_key);
+        const uint64_t one = row.mass(at_key), rest = target - in.mass_before - at.mass_before;
+        equal = min(at_key == key ? equal : UINT64_MAX, (rest + one - 1) / one), have = at.count, key = at_key;
+    }
+    if (min_p > 0.f) {
+        const uint32_t least = first_key(kLeast, row.top_key, [&](uint32_t k) { return row.reaches(k, min_p); });
+        if (least > key) key = least, equal = UINT64_MAX;
+    }
+    Kept kept = {key, 0xffffffffu};
+    if (equal < have) {   // the lower index first
+        uint32_t from_end;
+        select(s, 0, kMostVocab - 1, false, equal, [&](auto f) {
+            each_token([&](uint32_t k, int i) {
+                if (k == key) f((uint32_t)(kMostVocab - 1 - i));
+            });
+        }, [](uint32_t) { return (uint64_t)0; }, &from_end);
+        kept.index = kMostVocab - 1 - from_end;
+    }
+    return kept;
+}
 
-    Row r;
-    uint32_t top = 0;
-    for (int i = t; i < a.vocab; i += kRowThreads) top = max(top, key_of(to_f32(row[i * a.token_stride])));
-    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if (lane == 0) s_count[wave] = top;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) top = max(top, s_count[w]);
-    if (top == 0) {
-        if (t == 0) {
-            a.tokens[b] = -1;
-            if (a.logp) a.logp[b] = -INFINITY;
+// Where among a sum the token is.
+__device__ __forceinline__ uint64_t place_of(const SampleArgs &a, int b, uint64_t total) {
+    const float u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);
+    return (uint64_t)((double)u * (double)total);   // the sum has to be more
+}
+__device__ __forceinline__ void put(const SampleArgs &a, int b, int token, uint64_t mass, uint64_t total) {
+    a.tokens[b] = token;
+    if (a.logp) a.logp[b] = token < 0 ? -INFINITY : (float)log((double)mass / (double)total);
+}
+
+// Keys of elements i .. i + 3 of a row, 0 past its end; ALONG: elements are side by side.
+template <typename E, bool ALONG> struct Source {
+    const E *row;
+    int64_t stride;
+    int vocab;
+    bool whole;   // whether four at a time begin at a multiple of their size
+    __device__ __forceinline__ Source(const void *logits, int b, int64_t row_stride, int64_t token_stride, int v)
+        : row((const E *)logits + b * row_stride), stride(token_stride), vocab(v), whole(ALONG && (uintptr_t)row % (4 * sizeof(E)) == 0) {}
+    __device__ __forceinline__ uint32_t one(int i) const { return i < vocab ? key_of(row[ALONG ? i : i * stride]) : 0; }
+    __device__ __forceinline__ void four(int i, uint32_t *key) const {
+        if (ALONG && whole && i + 4 <= vocab) {
+            if constexpr (sizeof(E) == 4) {
+                const u32x4 v = *(const u32x4 *)(row + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t bits = v[e];   // a bit cast of v[e] itself takes the first element
+                    key[e] = key_of(__builtin_bit_cast(E, bits));
+                }
+            } else {
+                const u16x4 v = *(const u16x4 *)(row + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) key[e] = key_of((E)v[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) key[e] = one(i + e);
         }
+    }
+};
+
+// A workgroup for a row of up to MOST tokens, whose keys it holds in LDS, four at a time.
+template <typename E, bool ALONG, int THREADS, int MOST>
+__global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ Scratch<THREADS> s;
+    __shared__ u32x4 s_key[MOST / 4];
+    __shared__ uint64_t s_sum[MOST / (4 * THREADS) * WAVES];
+    const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
+    const Source<E, ALONG> src(a.logits, b, a.row_stride, a.token_stride, a.vocab);
+    const int fours = (a.vocab + 3) / 4, rounds = (fours + THREADS - 1) / THREADS;
+    uint32_t top = 0;
+#pragma unroll 4
+    for (int i = t; i < rounds * THREADS; i += THREADS) {
+        uint32_t key[4];
+        src.four(4 * i, key);
+        s_key[i] = (u32x4){key[0], key[1], key[2], key[3]};
+        top = max(max(top, max(key[0], key[1])), max(key[2], key[3]));
+    }
+    start(s);
+    top = largest<THREADS>(top, s.key);
+    if (top == 0) {
+        if (t == 0) put(a, b, -1, 0, 0);
         return;
     }
-    r.top = logit_of(top);
-    const float temperature = a.temperature ? a.temperature[b] : 1.f;
-    r.greedy = !(temperature > 0.f);
-    r.inv = 1.0 / temperature;
-
-    // The tokens up to which `target` tokens, or that much mass, come together, among the kept ones; by
-    // 8 bits of the key at a time.
-    Kept kept = {1, 0xffffffffu};
-    auto select = [&](bool by_mass, uint64_t target) {
-        uint32_t prefix = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            __syncthreads();
-            if (t < 256) s_count[t] = 0, s_mass[t] = 0;
-            __syncthreads();
-            for (int i = t; i < a.vocab; i += kRowThreads) {
-                const float l = logit(i);
-                const uint32_t key = key_of(l);
-                if (key < kept.key || (shift < 24 && key >> (shift + 8) != prefix >> (shift + 8))) continue;
-                atomicAdd(&s_count[key >> shift & 255], 1u);
-                if (by_mass) atomicAdd((unsigned long long *)&s_mass[key >> shift & 255], (unsigned long long)r.mass(l));
-            }
-            __syncthreads();
-            if (t == 0) {
-                uint64_t before = 0;
-                int bin = 255;
-                // of the last kept logit only some tokens are kept: the last bin may hold less than it says,
-                // which matters to no one as the target does not exceed what is kept
-                for (; bin > 0; --bin) {
-                    const uint64_t here = by_mass ? s_mass[bin] : s_count[bin];
-                    if (before + here >= target) break;
-                    before += here;
-                }
-                s_pick[0] = bin, s_pick[1] = s_count[bin], s_rest = before;
-            }
-            __syncthreads();
-            prefix |= s_pick[0] << shift;
-            target -= s_rest;
+    const Row row(a, b, top, s.powers);
+    auto each_token = [&](auto f) {   // of the thread's own
+#pragma unroll 1
+        for (int i = t; i < fours; i += THREADS) {
+            const u32x4 k = s_key[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f(k[e], 4 * i + e);
         }
-        Kept k;
-        k.key = prefix;
-        if (by_mass) {
-            const uint64_t one = r.mass(logit_of(prefix));
-            target = one ? (target + one - 1) / one : s_pick[1];
-        }
-        k.equal = (uint32_t)min((uint64_t)s_pick[1], max((uint64_t)1, target));
-        if (k.key == kept.key) k.equal = min(k.equal, kept.equal);
-        kept = k;
     };
-    const int top_k = a.top_k ? a.top_k[b] : 0;
-    if (r.greedy) {
-        kept = {top, 1};
-    } else if (top_k > 0 && top_k < a.vocab) {
-        uint64_t live = 0;
-        for (int i = t; i < a.vocab; i += kRowThreads) live += key_of(to_f32(row[i * a.token_stride])) != 0;
-        if (sum_of(live, s_part) > (uint64_t)top_k) select(false, top_k);
+    if (row.greedy) {
+        uint32_t from_end = 0;
+        each_token([&](uint32_t k, int i) { if (k == top) from_end = max(from_end, (uint32_t)(kMostVocab - i)); });
+        from_end = largest<THREADS>(from_end, s.key);
+        if (t == 0) put(a, b, kMostVocab - from_end, 1, 1);
+        return;
     }
-    const float top_p = a.top_p ? a.top_p[b] : 1.f;
-    if (!r.greedy && top_p < 1.f) {
-        uint64_t mass = 0, equal = 0;
-        for (int i = t; i < a.vocab; i += kRowThreads) {
-            const float l = logit(i);
-            const uint32_t key = key_of(l);
-            if (key > kept.key) mass += r.mass(l);
-            equal += key == kept.key;
-        }
-        mass = sum_of(mass, s_part), equal = sum_of(equal, s_part);
-        mass += min(equal, (uint64_t)kept.equal) * r.mass(logit_of(kept.key));
-        select(true, max((uint64_t)1, (uint64_t)ceil(fmax((double)top_p, 0.0) * (double)mass)));
+    Kept kept = {kLeast, 0xffffffffu};
+    if (a.top_k || a.top_p || a.min_p) {
+        clear(s, 0);
+        __syncthreads();
+        const bool by_mass = a.top_p != nullptr;
+        uint64_t live = 0, all = 0;
+        each_token([&](uint32_t k, int) {
+            if (!k) return;
+            const uint64_t m = by_mass ? row.mass(k) : 0;
+            add(s, 0, row.bin(k), m);
+            ++live, all += m;
+        });
+        live = scan<THREADS>(live, s.part[0]), all = scan<THREADS>(all, s.part[1]);
+        if (t == THREADS - 1) s.found[0] = live, s.found[1] = all;
+        __syncthreads();
+        live = s.found[0], all = s.found[1];
+        kept = cut(a, b, s, row, live, all, [](uint32_t, uint32_t, uint64_t) {},
+                   [&](auto f) { each_token([&](uint32_t k, int) { f(k); }); }, each_token);
     }
-    const float min_p = a.min_p ? a.min_p[b] : 0.f;
-    auto likely = [&](float l) { return l == r.top || !(r.weight(l) < min_p); };   // NaN: no cut
-
-    // Each wave adds up what is kept of a stretch of the row; then the wave of the stretch in which the sum
-    // passes u looks for the token.
-    const int per = (a.vocab + kWaves * 64 - 1) / (kWaves * 64) * 64;
-    const int from = min(a.vocab, wave * per), to = min(a.vocab, from + per);
-    uint32_t equal = 0;
-    uint64_t above = 0;
-    const uint64_t one = likely(logit_of(kept.key)) ? r.mass(logit_of(kept.key)) : 0;
-    for (int i = from + lane; i < to; i += 64) {
-        const float l = logit(i);
-        const uint32_t key = key_of(l);
-        equal += key == kept.key;
-        if (key > kept.key && likely(l)) above += r.mass(l);
+    auto mass = [&](uint32_t k, int i) { return k > kept.key || (k == kept.key && (uint32_t)i <= kept.index) ? row.mass(k) : 0; };
+#pragma unroll 1
+    for (int q = 0; q < rounds; ++q) {
+        const u32x4 k = s_key[q * THREADS + t];
+        uint64_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m += mass(k[e], 4 * (q * THREADS + t) + e);
+        if (__any(m != 0))
+            for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+        if (lane == 0) s_sum[q * WAVES + wave] = m;
     }
-    for (int d = 1; d < 64; d *= 2) equal += __shfl_xor(equal, d), above += __shfl_xor(above, d);
     __syncthreads();
-    if (lane == 0) s_count[wave] = equal, s_seg[wave] = above;
-    __syncthreads();
-    uint32_t seen = 0;   // of the last logit, before this wave
-    uint64_t before = 0, total = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before = total;
-        const uint32_t upto = min(kept.equal, seen + s_count[w]);
-        total += s_seg[w] + (upto - min(kept.equal, seen)) * one;
-        seen += s_count[w];
-    }
-    seen = 0;
-    for (int w = 0; w < wave; ++w) seen += s_count[w];
-    const float u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);
-    const uint64_t target = (uint64_t)((double)u * (double)total);   // the sum has to be more
-    uint64_t mine = s_seg[wave] + (min(kept.equal, seen + s_count[wave]) - min(kept.equal, seen)) * one;
-    if (target < before || target >= before + mine) return;
-    for (int i0 = from; i0 < to; i0 += 64) {
-        const int i = i0 + lane;
-        const float l = i < to ? logit(i) : -INFINITY;
-        const uint32_t key = key_of(l);
-        const uint64_t same = __ballot(key == kept.key);
-        const uint32_t rank = seen + __popcll(same & ((1ull << lane) - 1));
-        const uint64_t m = key == kept.key ? (rank < kept.equal ? one : 0) : key > kept.key && likely(l) ? r.mass(l) : 0;
+    // by each wave for itself: where among these sums the token is
+    const int sums = rounds * WAVES;
+    uint64_t total = 0;
+    for (int i = lane; i < sums; i += 64) total += s_sum[i];
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    const uint64_t target = place_of(a, b, total);
+    uint64_t before = 0;
+    int at = 0;
+    for (int i0 = 0; i0 < sums; i0 += 64) {
+        const uint64_t m = i0 + lane < sums ? s_sum[i0 + lane] : 0;
         uint64_t upto = m;
         for (int d = 1; d < 64; d *= 2) {
             const uint64_t o = __shfl_up(upto, d);
@@ -196,27 +379,323 @@ template <typename E> __global__ __launch_bounds__(kRowThreads) void k_sample(Sa
         }
         const uint64_t hit = __ballot(before + upto > target);
         if (hit) {
-            if (lane == __ffsll((unsigned long long)hit) - 1) {
-                a.tokens[b] = i;
-                if (a.logp) a.logp[b] = (float)log((double)m / (double)total);
-            }
-            return;
+            const int first = __ffsll((unsigned long long)hit) - 1;
+            at = i0 + first, before += __shfl(upto - m, first);
+            break;
         }
         before += __shfl(upto, 63);
-        seen += __popcll(same);
     }
+    if (at % WAVES != wave) return;
+    const int i = at / WAVES * THREADS + t;
+    const u32x4 k = s_key[i];
+    uint64_t m[4], upto = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) upto += m[e] = mass(k[e], 4 * i + e);
+    const uint64_t mine = upto;
+    for (int d = 1; d < 64; d *= 2) {
+        const uint64_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    upto += before - mine;   // before the lane's
+    if (upto > target || upto + mine <= target) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (upto <= target && upto + m[e] > target) put(a, b, 4 * i + e, m[e], total);
+        upto += m[e];
+    }
+}
+
+// ---- longer rows -------------------------------------------------------------------------------------
+
+struct Space {
+    uint32_t *keys, *top;        // [batch][vocab] if rows are laid out; [batch][scans]
+    uint32_t *count;             // [batch][chunks][bins]
+    uint64_t *mass;
+    int scans, chunks, row;      // elements from a row of keys to the next
+    int64_t bytes;
+};
+__host__ __device__ inline Space space_of(void *workspace, int batch, int vocab) {
+    Space s;
+    char *at = (char *)workspace;
+    auto take = [&](int64_t bytes) {
+        char *here = at;
+        at += (bytes + 15) / 16 * 16;
+        return here;
+    };
+    s.scans = (vocab + kScan - 1) / kScan, s.chunks = vocab > kRow ? (vocab + kChunk - 1) / kChunk : 0, s.row = (vocab + 3) / 4 * 4;
+    s.keys = (uint32_t *)take((int64_t)batch * s.row * 4);
+    s.top = (uint32_t *)take((int64_t)batch * s.scans * 4);
+    s.mass = (uint64_t *)take((int64_t)batch * s.chunks * kBins * 8);
+    s.count = (uint32_t *)take((int64_t)batch * s.chunks * kBins * 4);
+    s.bytes = at - (char *)workspace;
+    return s;
+}
+
+// The largest key of 2048 elements of a row that lie side by side.
+template <typename E> __global__ __launch_bounds__(256) void k_sample_scan(SampleArgs a, Space sp) {
+    __shared__ uint32_t s_part[4];
+    const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+    const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    uint32_t key[8], top = 0;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) src.four(c * kScan + 4 * (q * 256 + t), key + 4 * q);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, key[j]);
+    top = largest<256>(top, s_part);
+    if (t == 0) sp.top[(int64_t)b * sp.scans + c] = top;
+}
+// The same for 16 rows at a time whose elements lie apart, and their keys, laid out, through LDS: read along the rows
+// where they begin side by side.
+template <typename E> __global__ __launch_bounds__(256) void k_sample_lay(SampleArgs a, Space sp) {
+    constexpr int ROWS = 16, TOKENS = 256;
+    __shared__ uint32_t s_key[ROWS][TOKENS + 1], s_top[ROWS][4];
+    const int b0 = blockIdx.y * ROWS, rows = min(ROWS, a.batch - b0), c = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
+    const bool along_rows = rows > 1 && a.row_stride > -a.token_stride && a.row_stride < a.token_stride;
+    uint32_t top[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) top[r] = 0;
+    for (int i0 = c * kScan; i0 < min(a.vocab, (c + 1) * kScan); i0 += TOKENS) {
+        uint32_t key[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int r = along_rows ? t % ROWS : k, i = along_rows ? k * (256 / ROWS) + t / ROWS : t;
+            key[k] = r < rows && i0 + i < a.vocab ? key_of(((const E *)a.logits)[(b0 + r) * a.row_stride + (i0 + i) * a.token_stride]) : 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int r = along_rows ? t % ROWS : k, i = along_rows ? k * (256 / ROWS) + t / ROWS : t;
+            s_key[r][i] = key[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const uint32_t k = s_key[r][t];
+            top[r] = max(top[r], k);
+            if (r < rows && i0 + t < a.vocab) sp.keys[(int64_t)(b0 + r) * sp.row + i0 + t] = k;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        for (int d = 1; d < 64; d *= 2) top[r] = max(top[r], (uint32_t)__shfl_xor((int)top[r], d));
+        if (lane == 0) s_top[r][wave] = top[r];
+    }
+    __syncthreads();
+    if (t < rows) sp.top[(int64_t)(b0 + t) * sp.scans + c] = max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3]));
+}
+
+// The largest key of a row, for all threads.
+template <int THREADS> __device__ __forceinline__ uint32_t top_of(const Space &sp, int b, uint32_t *s_part) {
+    uint32_t top = 0;
+    for (int i = threadIdx.x; i < sp.scans; i += THREADS) top = max(top, sp.top[(int64_t)b * sp.scans + i]);
+    return largest<THREADS>(top, s_part);
+}
+
+// Bins of a chunk.
+template <typename E> __global__ __launch_bounds__(256) void k_sample_bins(SampleArgs a, Space sp) {
+    constexpr int T = 256;
+    __shared__ Scratch<T> s;
+    const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+    const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    start(s);
+    clear(s, 0);
+    const uint32_t top = top_of<T>(sp, b, s.key);
+    const Row row(a, b, top, s.powers);
+    if (top == 0 || row.greedy) return;
+    __syncthreads();
+#pragma unroll 2
+    for (int q = 0; q < kChunk / (4 * T); ++q) {
+        uint32_t key[4];
+        src.four(c * kChunk + 4 * (q * T + t), key);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (key[e]) add(s, 0, row.bin(key[e]), row.mass(key[e]));
+    }
+    __syncthreads();
+    const int64_t at = ((int64_t)b * sp.chunks + c) * kBins;
+    for (int i = t; i < kBins; i += T) sp.count[at + i] = s.count[0][i], sp.mass[at + i] = s.mass[0][i];
+}
+
+// Cuts and token of a row.
+template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(SampleArgs a, Space sp) {
+    constexpr int T = 1024, WAVES = T / 64, MOST = kMostVocab / kChunk;
+    __shared__ Scratch<T> s;
+    __shared__ uint32_t s_key[kList], s_listed;
+    __shared__ int s_index[kList];
+    __shared__ uint64_t s_chunk[MOST];
+    const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
+    const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    start(s);
+    const uint32_t top = top_of<T>(sp, b, s.key);
+    if (top == 0) {
+        if (t == 0) put(a, b, -1, 0, 0);
+        return;
+    }
+    const Row row(a, b, top, s.powers);
+    if (row.greedy) {   // in the first stretch that has it
+        uint32_t from_end = 0;
+        for (int i = t; i < sp.scans; i += T)
+            if (sp.top[(int64_t)b * sp.scans + i] == top) from_end = max(from_end, (uint32_t)(sp.scans - i));
+        const int first = (sp.scans - largest<T>(from_end, s.key)) * kScan;
+        from_end = 0;
+        for (int i = t; i < kScan; i += T)
+            if (src.one(first + i) == top) from_end = max(from_end, (uint32_t)(kScan - i));
+        from_end = largest<T>(from_end, s.key);
+        if (t == 0) put(a, b, first + kScan - from_end, 1, 1);
+        return;
+    }
+    const uint32_t *counts = sp.count + (int64_t)b * sp.chunks * kBins;
+    const uint64_t *masses = sp.mass + (int64_t)b * sp.chunks * kBins;
+    uint64_t live = 0, all = 0;
+    uint32_t n = 0;
+#pragma unroll 8
+    for (int c = 0; c < sp.chunks; ++c) n += counts[c * kBins + t], all += masses[c * kBins + t];
+    s.count[0][t] = n, s.mass[0][t] = all;
+    live = scan<T>((uint64_t)n, s.part[0]), all = scan<T>(all, s.part[1]);
+    if (t == T - 1) s.found[0] = live, s.found[1] = all;
+    __syncthreads();
+    live = s.found[0], all = s.found[1];
+    __syncthreads();
+
+    // The tokens of the keys lo .. hi: in LDS, or where they are too many read again each time.
+    uint32_t lo = 1, hi = 0;
+    bool listed = false;
+    auto stream = [&](auto f) {
+        for (int c = wave; c < sp.chunks; c += WAVES)
+            for (int i = c * kChunk + 4 * lane; i < min(a.vocab, (c + 1) * kChunk); i += 256) {
+                uint32_t key[4];
+                src.four(i, key);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(key[e], i + e, c);
+            }
+    };
+    auto prepare = [&](uint32_t from, uint32_t to, uint64_t count) {
+        if (from == lo && to == hi) return;
+        lo = from, hi = to, listed = count <= kList;
+        if (!listed) return;
+        __syncthreads();
+        if (t == 0) s_listed = 0;
+        __syncthreads();
+        stream([&](uint32_t k, int i, int) {
+            if (k >= lo && k <= hi) {
+                const uint32_t at = atomicAdd(&s_listed, 1u);
+                if (at < kList) s_key[at] = k, s_index[at] = i;
+            }
+        });
+        __syncthreads();
+    };
+    auto each_token = [&](auto f) {
+        if (listed)
+            for (uint32_t i = t; i < min(s_listed, (uint32_t)kList); i += T) f(s_key[i], s_index[i]);
+        else
+            stream([&](uint32_t k, int i, int) { if (k >= lo && k <= hi) f(k, i); });
+    };
+    const Kept kept = cut(a, b, s, row, live, all, prepare, [&](auto f) { each_token([&](uint32_t k, int) { f(k); }); }, each_token);
+
+    // What is kept of each chunk: whole bins, and of the one where the cut is the tokens that are kept.
+    const bool cuts = kept.key > kLeast || kept.index != 0xffffffffu;
+    const int last = cuts ? row.bin(kept.key) : kBins;
+    for (int c = t; c < MOST; c += T) s_chunk[c] = 0;
+    __syncthreads();
+    for (int c = wave; c < sp.chunks; c += WAVES) {
+        uint64_t m = 0;
+        for (int i = lane; i < last; i += 64) m += masses[c * kBins + i];
+        for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+        if (lane == 0) s_chunk[c] = m;
+    }
+    __syncthreads();
+    auto keeps = [&](uint32_t k, int i) { return k > kept.key || (k == kept.key && (uint32_t)i <= kept.index); };
+    if (cuts) {
+        if (!(row.bin(hi) == last && lo <= hi)) {   // the last cut was that of min_p, in another bin
+            const uint32_t to = last == 0 ? row.top_key : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) < last; }) - 1;
+            prepare(last == kBins - 1 ? kLeast : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) <= last; }), to,
+                    s.count[0][last]);
+        }
+        if (listed) {
+            each_token([&](uint32_t k, int i) {
+                if (keeps(k, i)) atomicAdd((unsigned long long *)&s_chunk[i / kChunk], (unsigned long long)row.mass(k));
+            });
+        } else {
+            int chunk = -1;
+            uint64_t m = 0;
+            auto flush = [&]() {
+                for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+                if (lane == 0 && chunk >= 0) s_chunk[chunk] += m;   // the wave's own chunk
+                m = 0;
+            };
+            for (int c = wave; c < sp.chunks; c += WAVES) {
+                chunk = c;
+                for (int i = c * kChunk + 4 * lane; i < min(a.vocab, (c + 1) * kChunk); i += 256) {
+                    uint32_t key[4];
+                    src.four(i, key);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key[e] >= lo && key[e] <= hi && keeps(key[e], i + e)) m += row.mass(key[e]);
+                }
+                flush();
+            }
+        }
+        __syncthreads();
+    }
+    uint64_t total = 0;
+    for (int c = 0; c < sp.chunks; ++c) total += s_chunk[c];
+    const uint64_t target = place_of(a, b, total);
+    uint64_t before = 0;
+    int c = 0;
+    for (; c < sp.chunks - 1 && before + s_chunk[c] <= target; ++c) before += s_chunk[c];
+    // the chunk again, eight tokens a thread
+    uint32_t key[8];
+    uint64_t m[8], mine = 0;
+    const int i0 = c * kChunk + 8 * t;
+    src.four(i0, key), src.four(i0 + 4, key + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine += m[e] = key[e] && keeps(key[e], i0 + e) ? row.mass(key[e]) : 0;
+    uint64_t upto = before + scan<T>(mine, s.part[0]) - mine;
+    if (upto > target || upto + mine <= target) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (upto <= target && upto + m[e] > target) put(a, b, i0 + e, m[e], total);
+        upto += m[e];
+    }
+}
+
+template <typename E, bool ALONG> hipError_t run_row(const SampleArgs &a, hipStream_t st) {
+    if (a.vocab <= 4096) k_sample_row<E, ALONG, 256, 4096><<<a.batch, 256, 0, st>>>(a);
+    else k_sample_row<E, ALONG, 1024, kRow><<<a.batch, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <typename E> hipError_t run_long(const SampleArgs &a, const Space &sp, hipStream_t st) {
+    k_sample_bins<E><<<dim3(sp.chunks, a.batch), 256, 0, st>>>(a, sp);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    k_sample_pick<E><<<a.batch, 1024, 0, st>>>(a, sp);
+    return hipGetLastError();
+}
+
+// Rows whose elements lie apart are read as they lie up to so many tokens: each element is a line of its own.
+constexpr int kApart = 4096;
+
+template <typename E> hipError_t run(SampleArgs a, hipStream_t st) {
+    const Space sp = space_of(a.workspace, a.batch, a.vocab);
+    const bool along = a.token_stride == 1;
+    if (a.vocab <= kRow && (along || a.vocab <= kApart)) return along ? run_row<E, true>(a, st) : run_row<E, false>(a, st);
+    if (along) {
+        k_sample_scan<E><<<dim3(sp.scans, a.batch), 256, 0, st>>>(a, sp);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        return run_long<E>(a, sp, st);
+    }
+    k_sample_lay<E><<<dim3(sp.scans, (a.batch + 15) / 16), 256, 0, st>>>(a, sp);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    a.logits = sp.keys, a.row_stride = sp.row, a.token_stride = 1;
+    return a.vocab <= kRow ? run_row<uint32_t, true>(a, st) : run_long<uint32_t>(a, sp, st);
 }
 
 }  // namespace
 
-int64_t sample_workspace(int, int) { return 0; }
+// Whatever the strides are.
+int64_t sample_workspace(int batch, int vocab) { return vocab <= kApart ? 0 : space_of(nullptr, batch, vocab).bytes; }
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st) {
-    if (a.dtype == BSP_F32)
-        k_sample<float><<<a.batch, kRowThreads, 0, st>>>(a);
-    else
-        k_sample<uint16_t><<<a.batch, kRowThreads, 0, st>>>(a);
-    return hipGetLastError();
+    return a.dtype == BSP_F32 ? run<float>(a, st) : run<uint16_t>(a, st);
 }
 
 }  // namespace bsp
