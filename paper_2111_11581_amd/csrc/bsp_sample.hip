@@ -22,11 +22,13 @@ namespace bsp {
 namespace {
 
 constexpr double kOne = 8796093022208.0;   // 2^43: what a weight of 1 counts; 2^20 of them stay below 2^63
-constexpr int kBins = 1024, kSpan = 32;    // bins, and the distance that they cover: e^-32 is below 2^-44
-constexpr int kScan = 2048;                // tokens whose largest logit k_sample_scan finds
+constexpr int kBins = 512, kSpan = 32;    // bins, and the distance that they cover: e^-32 is below 2^-44
+constexpr int kScan = 2048, kLay = 256;    // tokens whose largest logit k_sample_scan and k_sample_lay find
 constexpr int kChunk = 8192;               // tokens whose bins k_sample_bins fills
 constexpr int kRow = 32768;                // tokens that a workgroup holds in LDS
+constexpr int kQuick = 128;                // tokens of a bin that are compared with each other
 constexpr int kList = 4096;                // tokens of a bin that k_sample_pick holds in LDS
+constexpr int kFirst = 512;                // tokens of a chunk's first bins that k_sample_bins lists
 
 // Logits as numbers that are in the same order; NaN and -Inf, which are never taken, are 0.
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -87,24 +89,24 @@ template <int THREADS> struct Scratch {
     static constexpr int WAVES = THREADS / 64;
     uint64_t mass[2][kBins];   // of bins, and of the pieces into which one is cut
     double powers[64];
-    uint64_t part[2][WAVES], found[4];
-    uint32_t count[2][kBins], key[WAVES];
+    uint64_t part[2][WAVES], found[4], list_mass[kQuick];
+    uint32_t count[2][kBins], key[WAVES], list_key[kQuick], listed;
+    int list_index[kQuick];
 };
 
-// Inclusive scan over the workgroup.
-template <int THREADS, typename T> __device__ __forceinline__ T scan(T v, T *s_part) {
+// Inclusive scans of two values over the workgroup.
+template <int THREADS> __device__ __forceinline__ void scan(uint64_t *x, uint64_t *y, uint64_t (*s_part)[THREADS / 64]) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     for (int d = 1; d < 64; d *= 2) {
-        const T o = __shfl_up(v, d);
-        if (lane >= d) v += o;
+        const uint64_t ox = __shfl_up(*x, d), oy = __shfl_up(*y, d);
+        if (lane >= d) *x += ox, *y += oy;
     }
     __syncthreads();
-    if (lane == 63) s_part[wave] = v;
+    if (lane == 63) s_part[0][wave] = *x, s_part[1][wave] = *y;
     __syncthreads();
-    T before = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) before += w < wave ? s_part[w] : 0;
-    return v + before;
+    for (int w = 0; w < THREADS / 64; ++w)
+        if (w < wave) *x += s_part[0][w], *y += s_part[1][w];
 }
 // Largest over the workgroup, for all.
 template <int THREADS> __device__ __forceinline__ uint32_t largest(uint32_t v, uint32_t *s_part) {
@@ -134,12 +136,14 @@ struct Found {
     uint64_t count_before, mass_before, count;
 };
 template <int THREADS> __device__ __forceinline__ Found locate(Scratch<THREADS> &s, int which, bool by_mass, uint64_t target) {
-    constexpr int PER = kBins / THREADS;
+    constexpr int PER = kBins / THREADS < 1 ? 1 : kBins / THREADS;
     const int t = threadIdx.x;
     uint64_t count = 0, mass = 0;
+    if (t * PER < kBins)
 #pragma unroll
-    for (int i = 0; i < PER; ++i) count += s.count[which][t * PER + i], mass += s.mass[which][t * PER + i];
-    uint64_t counts = scan<THREADS>(count, s.part[0]), masses = scan<THREADS>(mass, s.part[1]);
+        for (int i = 0; i < PER; ++i) count += s.count[which][t * PER + i], mass += s.mass[which][t * PER + i];
+    uint64_t counts = count, masses = mass;
+    scan<THREADS>(&counts, &masses, s.part);
     const uint64_t upto = by_mass ? masses : counts, before = upto - (by_mass ? mass : count);
     if (before < target && target <= upto) {
         counts -= count, masses -= mass;
@@ -157,13 +161,13 @@ template <int THREADS> __device__ __forceinline__ Found locate(Scratch<THREADS> 
 }
 
 // Of the keys lo .. hi that each(f) calls f with, in any order, the one down to which `target` of them, or that much of
-// mass(key), come together; ten bits at a time.  `count`: how many have it.
+// mass(key), come together; nine bits at a time.  `count`: how many have it.
 template <int THREADS, typename F, typename M>
 __device__ __forceinline__ Found select(Scratch<THREADS> &s, uint32_t lo, uint32_t hi, bool by_mass, uint64_t target, F each, M mass,
                                         uint32_t *key) {
     uint64_t counts = 0, masses = 0;
     for (;;) {
-        const int shift = max(0, 32 - (hi == lo ? 32 : __clz((int)(hi - lo))) - 10);
+        const int shift = max(0, 32 - (hi == lo ? 32 : __clz((int)(hi - lo))) - 9);
         clear(s, 1);
         __syncthreads();
         each([&](uint32_t k) {
@@ -199,54 +203,89 @@ template <typename P> __device__ __forceinline__ uint32_t first_key(uint32_t lo,
 // What is kept of a row: tokens whose key is above, and of those that have it the ones up to an index.
 struct Kept {
     uint32_t key, index;
+    __device__ __forceinline__ bool has(uint32_t k, int i) const { return k > key || (k == key && (uint32_t)i <= index); }
 };
 
-// Finds it for a row whose bins are filled.  prepare(lo, hi, count) is told the keys that are asked for next, and how many
-// tokens have them; each_key(f) calls f(key) and each_token(f) f(key, index) for these at least.
-template <int THREADS, typename R, typename K, typename T>
-__device__ __forceinline__ Kept cut(const SampleArgs &a, int b, Scratch<THREADS> &s, const Row &row, uint64_t live, uint64_t all, R prepare,
-                                    K each_key, T each_token) {
+// Cuts what is kept of a row, in a bin of `in.count` tokens, where `target` of its tokens, or that much mass, come together;
+// returns their number and mass in `in`.  prepare(bin, count) is told the bin and how many tokens it has, and
+// each_token(f) calls f(key, index) for these at least.
+//  * Few tokens are compared with each other, a thread for each.
+//  * Of more the key is found by its bits, and where several tokens have it the last index in the same way.
+template <int THREADS, typename R, typename T>
+__device__ __forceinline__ void cut_bin(Scratch<THREADS> &s, const Row &row, Found *in, bool by_mass, uint64_t target, R prepare, T each_token,
+                                        Kept *kept) {
+    prepare(in->bin, in->count);
+    const Kept from = *kept;
+    if (in->count <= kQuick) {
+        const int t = threadIdx.x;
+        if (t == 0) s.listed = 0;
+        __syncthreads();
+        each_token([&](uint32_t k, int i) {
+            if (!from.has(k, i) || row.bin(k) != in->bin) return;
+            const uint32_t at = atomicAdd(&s.listed, 1u);
+            if (at < kQuick) s.list_key[at] = k, s.list_index[at] = i, s.list_mass[at] = row.mass(k);
+        });
+        __syncthreads();
+        const int n = min((int)s.listed, kQuick);
+        if (t < n) {
+            const uint32_t k = s.list_key[t];
+            const int i = s.list_index[t];
+            uint64_t mass = 0, count = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) {
+                const uint32_t o = s.list_key[j];
+                const bool before = o > k || (o == k && s.list_index[j] <= i);
+                count += before, mass += before ? s.list_mass[j] : 0;
+            }
+            const uint64_t upto = by_mass ? mass : count, own = by_mass ? s.list_mass[t] : 1;
+            if (upto >= target && upto - own < target) s.found[0] = k, s.found[1] = i, s.found[2] = count, s.found[3] = mass;
+        }
+        __syncthreads();
+        kept->key = (uint32_t)s.found[0], kept->index = (uint32_t)s.found[1], in->count = s.found[2], in->mass_before += s.found[3];
+        return;
+    }
+    const uint32_t hi = in->bin == 0 ? row.top_key : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) < in->bin; }) - 1;
+    const uint32_t lo = in->bin == kBins - 1 ? kLeast : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) <= in->bin; });
+    uint32_t key;
+    const Found at = select(s, max(lo, from.key), hi, by_mass, target, [&](auto f) {
+        each_token([&](uint32_t k, int i) { if (from.has(k, i)) f(k); });
+    }, [&](uint32_t k) { return row.mass(k); }, &key);
+    const uint64_t one = row.mass(key), rest = target - (by_mass ? at.mass_before : at.count_before);
+    const uint64_t equal = by_mass ? (rest + one - 1) / one : rest;
+    in->mass_before += at.mass_before + equal * one;
+    kept->key = key, kept->index = key == from.key ? from.index : 0xffffffffu;
+    if (equal < at.count) {   // the lower index first
+        uint32_t from_end;
+        select(s, 0, kMostVocab - 1, false, equal, [&](auto f) {
+            each_token([&](uint32_t k, int i) { if (k == key && from.has(k, i)) f((uint32_t)(kMostVocab - 1 - i)); });
+        }, [](uint32_t) { return (uint64_t)0; }, &from_end);
+        kept->index = kMostVocab - 1 - from_end;
+    }
+}
+
+// The cuts of a row of `live` tokens, whose bins hold their numbers; fill_mass(kept) adds their mass for what is kept, and
+// returns all of it.
+template <int THREADS, typename R, typename T, typename M>
+__device__ __forceinline__ Kept cut(const SampleArgs &a, int b, Scratch<THREADS> &s, const Row &row, uint64_t live, R prepare, T each_token,
+                                    M fill_mass) {
     const int top_k = a.top_k ? a.top_k[b] : 0;
     const float top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
     const bool by_k = top_k > 0 && (uint64_t)top_k < live, by_p = top_p < 1.f;
-    uint32_t key = kLeast;
-    uint64_t equal = UINT64_MAX, have = 0;   // of those that have the key: kept, and in all
-    auto range = [&](const Found &f, uint32_t *lo, uint32_t *hi) {
-        *hi = f.bin == 0 ? row.top_key : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) < f.bin; }) - 1;
-        *lo = f.bin == kBins - 1 ? kLeast : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) <= f.bin; });
-        prepare(*lo, *hi, f.count);
-    };
-    auto mass = [&](uint32_t k) { return row.mass(k); };
-    uint32_t lo, hi;
+    Kept kept = {kLeast, 0xffffffffu};
+    Found in;
     if (by_k) {
-        const Found in = locate(s, 0, false, (uint64_t)top_k);
-        range(in, &lo, &hi);
-        const Found at = select(s, lo, hi, false, top_k - in.count_before, each_key, [&](uint32_t k) { return by_p ? row.mass(k) : 0; }, &key);
-        equal = top_k - in.count_before - at.count_before, have = at.count;
-        all = in.mass_before + at.mass_before + equal * row.mass(key);
+        in = locate(s, 0, false, (uint64_t)top_k);
+        cut_bin(s, row, &in, false, top_k - in.count_before, prepare, each_token, &kept);
     }
     if (by_p) {
+        const uint64_t all = fill_mass(kept, by_k, in);
         const uint64_t target = max((uint64_t)1, (uint64_t)ceil(fmax((double)top_p, 0.0) * (double)all));
-        const Found in = locate(s, 0, true, target);   // at most the bin of the first cut, of which not all is kept
-        range(in, &lo, &hi);
-        uint32_t at_key;
-        const Found at = select(s, max(lo, key), hi, true, target - in.mass_before, each_key, mass, &at_key);
-        const uint64_t one = row.mass(at_key), rest = target - in.mass_before - at.mass_before;
-        equal = min(at_key == key ? equal : UINT64_MAX, (rest + one - 1) / one), have = at.count, key = at_key;
+        in = locate(s, 0, true, target);   // at most the bin of the first cut, of which not all is kept
+        cut_bin(s, row, &in, true, target - in.mass_before, prepare, each_token, &kept);
     }
     if (min_p > 0.f) {
         const uint32_t least = first_key(kLeast, row.top_key, [&](uint32_t k) { return row.reaches(k, min_p); });
-        if (least > key) key = least, equal = UINT64_MAX;
-    }
-    Kept kept = {key, 0xffffffffu};
-    if (equal < have) {   // the lower index first
-        uint32_t from_end;
-        select(s, 0, kMostVocab - 1, false, equal, [&](auto f) {
-            each_token([&](uint32_t k, int i) {
-                if (k == key) f((uint32_t)(kMostVocab - 1 - i));
-            });
-        }, [](uint32_t) { return (uint64_t)0; }, &from_end);
-        kept.index = kMostVocab - 1 - from_end;
+        if (least > kept.key) kept = {least, 0xffffffffu};
     }
     return kept;
 }
@@ -333,24 +372,36 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
     }
     Kept kept = {kLeast, 0xffffffffu};
     if (a.top_k || a.top_p || a.min_p) {
+        const bool by_count = a.top_k && a.top_k[b] > 0;
         clear(s, 0);
         __syncthreads();
-        const bool by_mass = a.top_p != nullptr;
         uint64_t live = 0, all = 0;
-        each_token([&](uint32_t k, int) {
-            if (!k) return;
-            const uint64_t m = by_mass ? row.mass(k) : 0;
-            add(s, 0, row.bin(k), m);
-            ++live, all += m;
+        if (by_count) {
+            each_token([&](uint32_t k, int) {
+                if (k) ++live, atomicAdd(&s.count[0][row.bin(k)], 1u);
+            });
+            scan<THREADS>(&live, &all, s.part);
+            if (t == THREADS - 1) s.found[0] = live;
+            __syncthreads();
+            live = s.found[0];
+        }
+        kept = cut(a, b, s, row, live, [](int, uint64_t) {}, each_token, [&](const Kept &k0, bool, const Found &) {
+            if (by_count) clear(s, 0);   // bins of what is kept alone
+            __syncthreads();
+            uint64_t all = 0, none = 0;
+            each_token([&](uint32_t k, int i) {
+                if (!k0.has(k, i)) return;
+                const uint64_t m = row.mass(k);
+                add(s, 0, row.bin(k), m), all += m;
+            });
+            scan<THREADS>(&all, &none, s.part);
+            if (t == THREADS - 1) s.found[0] = all;
+            __syncthreads();
+            all = s.found[0];
+            return all;
         });
-        live = scan<THREADS>(live, s.part[0]), all = scan<THREADS>(all, s.part[1]);
-        if (t == THREADS - 1) s.found[0] = live, s.found[1] = all;
-        __syncthreads();
-        live = s.found[0], all = s.found[1];
-        kept = cut(a, b, s, row, live, all, [](uint32_t, uint32_t, uint64_t) {},
-                   [&](auto f) { each_token([&](uint32_t k, int) { f(k); }); }, each_token);
     }
-    auto mass = [&](uint32_t k, int i) { return k > kept.key || (k == kept.key && (uint32_t)i <= kept.index) ? row.mass(k) : 0; };
+    auto mass = [&](uint32_t k, int i) { return kept.has(k, i) ? row.mass(k) : 0; };
 #pragma unroll 1
     for (int q = 0; q < rounds; ++q) {
         const u32x4 k = s_key[q * THREADS + t];
@@ -411,10 +462,12 @@ struct Space {
     uint32_t *keys, *top;        // [batch][vocab] if rows are laid out; [batch][scans]
     uint32_t *count;             // [batch][chunks][bins]
     uint64_t *mass;
-    int scans, chunks, row;      // elements from a row of keys to the next
+    int2 *listed;                // [batch][chunks]: bins whose tokens are listed, and how many these are
+    uint2 *token;                // [batch][chunks][kFirst]: their keys and indexes, in any order
+    int scan, scans, chunks, row;   // tokens of a scan; elements from a row of keys to the next
     int64_t bytes;
 };
-__host__ __device__ inline Space space_of(void *workspace, int batch, int vocab) {
+__host__ __device__ inline Space space_of(void *workspace, int batch, int vocab, bool apart) {
     Space s;
     char *at = (char *)workspace;
     auto take = [&](int64_t bytes) {
@@ -422,11 +475,13 @@ __host__ __device__ inline Space space_of(void *workspace, int batch, int vocab)
         at += (bytes + 15) / 16 * 16;
         return here;
     };
-    s.scans = (vocab + kScan - 1) / kScan, s.chunks = vocab > kRow ? (vocab + kChunk - 1) / kChunk : 0, s.row = (vocab + 3) / 4 * 4;
-    s.keys = (uint32_t *)take((int64_t)batch * s.row * 4);
+    s.scan = apart ? kLay : kScan, s.scans = (vocab + s.scan - 1) / s.scan, s.chunks = vocab > kRow ? (vocab + kChunk - 1) / kChunk : 0, s.row = (vocab + 3) / 4 * 4;
+    s.keys = (uint32_t *)take(apart ? (int64_t)batch * s.row * 4 : 0);
     s.top = (uint32_t *)take((int64_t)batch * s.scans * 4);
     s.mass = (uint64_t *)take((int64_t)batch * s.chunks * kBins * 8);
     s.count = (uint32_t *)take((int64_t)batch * s.chunks * kBins * 4);
+    s.listed = (int2 *)take((int64_t)batch * s.chunks * 8);
+    s.token = (uint2 *)take((int64_t)batch * s.chunks * kFirst * 8);
     s.bytes = at - (char *)workspace;
     return s;
 }
@@ -444,44 +499,38 @@ template <typename E> __global__ __launch_bounds__(256) void k_sample_scan(Sampl
     top = largest<256>(top, s_part);
     if (t == 0) sp.top[(int64_t)b * sp.scans + c] = top;
 }
-// The same for 16 rows at a time whose elements lie apart, and their keys, laid out, through LDS: read along the rows
-// where they begin side by side.
+// The same for 256 tokens of 16 rows whose elements lie apart, and their keys, laid out, through LDS: read along the
+// rows where they begin side by side.
 template <typename E> __global__ __launch_bounds__(256) void k_sample_lay(SampleArgs a, Space sp) {
-    constexpr int ROWS = 16, TOKENS = 256;
-    __shared__ uint32_t s_key[ROWS][TOKENS + 1], s_top[ROWS][4];
-    const int b0 = blockIdx.y * ROWS, rows = min(ROWS, a.batch - b0), c = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
+    constexpr int ROWS = 16;
+    __shared__ uint32_t s_key[ROWS][kLay + 1], s_top[ROWS][4];
+    const int b0 = blockIdx.y * ROWS, rows = min(ROWS, a.batch - b0), t = threadIdx.x, lane = t % 64, wave = t / 64, i0 = blockIdx.x * kLay;
     const bool along_rows = rows > 1 && a.row_stride > -a.token_stride && a.row_stride < a.token_stride;
-    uint32_t top[ROWS];
+    const int r0 = along_rows ? t % ROWS : 0, at0 = along_rows ? t / ROWS : t;         // the thread's first, and from
+    const int next_r = along_rows ? 0 : 1, next_at = along_rows ? kLay / ROWS : 0;   // each to the next
+    E v[ROWS];
+    const E *src = (const E *)a.logits + b0 * a.row_stride + i0 * a.token_stride;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) top[r] = 0;
-    for (int i0 = c * kScan; i0 < min(a.vocab, (c + 1) * kScan); i0 += TOKENS) {
-        uint32_t key[ROWS];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const int r = along_rows ? t % ROWS : k, i = along_rows ? k * (256 / ROWS) + t / ROWS : t;
-            key[k] = r < rows && i0 + i < a.vocab ? key_of(((const E *)a.logits)[(b0 + r) * a.row_stride + (i0 + i) * a.token_stride]) : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const int r = along_rows ? t % ROWS : k, i = along_rows ? k * (256 / ROWS) + t / ROWS : t;
-            s_key[r][i] = key[k];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const uint32_t k = s_key[r][t];
-            top[r] = max(top[r], k);
-            if (r < rows && i0 + t < a.vocab) sp.keys[(int64_t)(b0 + r) * sp.row + i0 + t] = k;
-        }
+    for (int k = 0; k < ROWS; ++k) {
+        const int r = min(r0 + k * next_r, rows - 1), i = min(at0 + k * next_at, a.vocab - 1 - i0);
+        v[k] = src[r * a.row_stride + i * a.token_stride];
     }
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        for (int d = 1; d < 64; d *= 2) top[r] = max(top[r], (uint32_t)__shfl_xor((int)top[r], d));
-        if (lane == 0) s_top[r][wave] = top[r];
+    for (int k = 0; k < ROWS; ++k) {
+        const int r = r0 + k * next_r, i = at0 + k * next_at;
+        s_key[r][i] = r < rows && i0 + i < a.vocab ? key_of(v[k]) : 0;
     }
     __syncthreads();
-    if (t < rows) sp.top[(int64_t)(b0 + t) * sp.scans + c] = max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3]));
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const uint32_t k = s_key[r][t];
+        if (r < rows && i0 + t < a.vocab) sp.keys[(int64_t)(b0 + r) * sp.row + i0 + t] = k;
+        uint32_t top = k;
+        for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        if (lane == 0) s_top[r][wave] = top;
+    }
+    __syncthreads();
+    if (t < rows) sp.top[(int64_t)(b0 + t) * sp.scans + blockIdx.x] = max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3]));
 }
 
 // The largest key of a row, for all threads.
@@ -491,29 +540,55 @@ template <int THREADS> __device__ __forceinline__ uint32_t top_of(const Space &s
     return largest<THREADS>(top, s_part);
 }
 
-// Bins of a chunk.
-template <typename E> __global__ __launch_bounds__(256) void k_sample_bins(SampleArgs a, Space sp) {
-    constexpr int T = 256;
+// Bins of a chunk, and the tokens of its first ones.
+template <typename E> __global__ __launch_bounds__(512) void k_sample_bins(SampleArgs a, Space sp) {
+    constexpr int T = 512, Q = kChunk / (4 * T);
     __shared__ Scratch<T> s;
     const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
     const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    uint32_t key[Q][4];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) src.four(c * kChunk + 4 * (q * T + t), key[q]);
     start(s);
     clear(s, 0);
+    if (t == 0) s.listed = 0;
     const uint32_t top = top_of<T>(sp, b, s.key);
     const Row row(a, b, top, s.powers);
     if (top == 0 || row.greedy) return;
     __syncthreads();
-#pragma unroll 2
-    for (int q = 0; q < kChunk / (4 * T); ++q) {
-        uint32_t key[4];
-        src.four(c * kChunk + 4 * (q * T + t), key);
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (key[e]) add(s, 0, row.bin(key[e]), row.mass(key[e]));
-    }
+            if (key[q][e]) add(s, 0, row.bin(key[q][e]), row.mass(key[q][e]));
     __syncthreads();
     const int64_t at = ((int64_t)b * sp.chunks + c) * kBins;
     for (int i = t; i < kBins; i += T) sp.count[at + i] = s.count[0][i], sp.mass[at + i] = s.mass[0][i];
+    if (!a.top_k && !a.top_p && !a.min_p) return;
+    // the first bins that have no more than kFirst tokens
+    constexpr int PER = kBins / T;
+    uint64_t count = 0, none = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) count += s.count[0][t * PER + i];
+    uint64_t upto = count;
+    scan<T>(&upto, &none, s.part);
+    upto -= count;
+    int mine = 0;   // of the thread's bins
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        upto += s.count[0][t * PER + i];
+        if (upto <= kFirst) mine = t * PER + i + 1;
+    }
+    const int bins = (int)largest<T>((uint32_t)mine, s.key);
+    uint2 *list = sp.token + ((int64_t)b * sp.chunks + c) * kFirst;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (key[q][e] && row.bin(key[q][e]) < bins)
+                list[atomicAdd(&s.listed, 1u)] = make_uint2(key[q][e], (uint32_t)(c * kChunk + 4 * (q * T + t) + e));
+    __syncthreads();
+    if (t == 0) sp.listed[(int64_t)b * sp.chunks + c] = make_int2(bins, (int)s.listed);
 }
 
 // Cuts and token of a row.
@@ -521,7 +596,8 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     constexpr int T = 1024, WAVES = T / 64, MOST = kMostVocab / kChunk;
     __shared__ Scratch<T> s;
     __shared__ uint32_t s_key[kList], s_listed;
-    __shared__ int s_index[kList];
+    __shared__ int s_index[kList], s_bins;
+    __shared__ int2 s_listed_of[MOST];
     __shared__ uint64_t s_chunk[MOST];
     const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
     const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
@@ -536,48 +612,65 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
         uint32_t from_end = 0;
         for (int i = t; i < sp.scans; i += T)
             if (sp.top[(int64_t)b * sp.scans + i] == top) from_end = max(from_end, (uint32_t)(sp.scans - i));
-        const int first = (sp.scans - largest<T>(from_end, s.key)) * kScan;
+        const int first = (sp.scans - largest<T>(from_end, s.key)) * sp.scan;
         from_end = 0;
-        for (int i = t; i < kScan; i += T)
-            if (src.one(first + i) == top) from_end = max(from_end, (uint32_t)(kScan - i));
+        for (int i = t; i < sp.scan; i += T)
+            if (src.one(first + i) == top) from_end = max(from_end, (uint32_t)(sp.scan - i));
         from_end = largest<T>(from_end, s.key);
-        if (t == 0) put(a, b, first + kScan - from_end, 1, 1);
+        if (t == 0) put(a, b, first + sp.scan - from_end, 1, 1);
         return;
     }
     const uint32_t *counts = sp.count + (int64_t)b * sp.chunks * kBins;
     const uint64_t *masses = sp.mass + (int64_t)b * sp.chunks * kBins;
     uint64_t live = 0, all = 0;
-    uint32_t n = 0;
+    if (t < kBins) {
 #pragma unroll 8
-    for (int c = 0; c < sp.chunks; ++c) n += counts[c * kBins + t], all += masses[c * kBins + t];
-    s.count[0][t] = n, s.mass[0][t] = all;
-    live = scan<T>((uint64_t)n, s.part[0]), all = scan<T>(all, s.part[1]);
+        for (int c = 0; c < sp.chunks; ++c) live += counts[c * kBins + t], all += masses[c * kBins + t];
+        s.count[0][t] = (uint32_t)live, s.mass[0][t] = all;
+    }
+    const bool cut_at_all = a.top_k || a.top_p || a.min_p;
+    if (cut_at_all) {   // the first bins whose tokens all chunks list
+        for (int c = t; c < sp.chunks; c += T) s_listed_of[c] = sp.listed[(int64_t)b * sp.chunks + c];
+        if (t == 0) s_bins = kBins;
+        __syncthreads();
+        for (int c = t; c < sp.chunks; c += T) atomicMin(&s_bins, s_listed_of[c].x);
+    }
+    scan<T>(&live, &all, s.part);
     if (t == T - 1) s.found[0] = live, s.found[1] = all;
     __syncthreads();
     live = s.found[0], all = s.found[1];
     __syncthreads();
 
-    // The tokens of the keys lo .. hi: in LDS, or where they are too many read again each time.
-    uint32_t lo = 1, hi = 0;
-    bool listed = false;
-    auto stream = [&](auto f) {
-        for (int c = wave; c < sp.chunks; c += WAVES)
-            for (int i = c * kChunk + 4 * lane; i < min(a.vocab, (c + 1) * kChunk); i += 256) {
-                uint32_t key[4];
-                src.four(i, key);
+    // The tokens of a bin: among those that are listed; or gathered in LDS; or where they are too many read again
+    // each time.
+    enum { kListed, kGathered, kReadAgain } from = kReadAgain;
+    int bin = -1;
+    auto stream = [&](auto f) {   // eight reads under way
+        constexpr int N = 8;
+        for (int c = wave; c < sp.chunks; c += WAVES) {
+            const int end = min(a.vocab, (c + 1) * kChunk);
+#pragma unroll 1
+            for (int i0 = c * kChunk + 4 * lane; i0 - 4 * lane < end; i0 += 256 * N) {
+                uint32_t key[N][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f(key[e], i + e, c);
+                for (int n = 0; n < N; ++n) src.four(i0 + 256 * n, key[n]);
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f(key[n][e], i0 + 256 * n + e, c);
             }
+        }
     };
-    auto prepare = [&](uint32_t from, uint32_t to, uint64_t count) {
-        if (from == lo && to == hi) return;
-        lo = from, hi = to, listed = count <= kList;
-        if (!listed) return;
+    auto prepare = [&](int next, uint64_t count) {
+        if (next == bin) return;
+        bin = next;
+        from = bin < s_bins ? kListed : count <= kList ? kGathered : kReadAgain;
+        if (from != kGathered) return;
         __syncthreads();
         if (t == 0) s_listed = 0;
         __syncthreads();
         stream([&](uint32_t k, int i, int) {
-            if (k >= lo && k <= hi) {
+            if (k && row.bin(k) == bin) {
                 const uint32_t at = atomicAdd(&s_listed, 1u);
                 if (at < kList) s_key[at] = k, s_index[at] = i;
             }
@@ -585,12 +678,25 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
         __syncthreads();
     };
     auto each_token = [&](auto f) {
-        if (listed)
+        if (from == kListed) {
+            for (int c = wave; c < sp.chunks; c += WAVES) {
+                const uint2 *list = sp.token + ((int64_t)b * sp.chunks + c) * kFirst;
+                const int n = s_listed_of[c].y;
+                uint2 v[kFirst / 64];
+#pragma unroll
+                for (int i = 0; i < kFirst / 64; ++i) v[i] = list[64 * i + lane];   // of the last ones, what is there
+#pragma unroll
+                for (int i = 0; i < kFirst / 64; ++i)
+                    if (64 * i + lane < n) f(v[i].x, (int)v[i].y);
+            }
+        } else if (from == kGathered) {
             for (uint32_t i = t; i < min(s_listed, (uint32_t)kList); i += T) f(s_key[i], s_index[i]);
-        else
-            stream([&](uint32_t k, int i, int) { if (k >= lo && k <= hi) f(k, i); });
+        } else {
+            stream([&](uint32_t k, int i, int) { if (k) f(k, i); });
+        }
     };
-    const Kept kept = cut(a, b, s, row, live, all, prepare, [&](auto f) { each_token([&](uint32_t k, int) { f(k); }); }, each_token);
+    const Kept kept = cut(a, b, s, row, live, prepare, each_token,
+                          [&](const Kept &, bool by_k, const Found &in) { return by_k ? in.mass_before : all; });
 
     // What is kept of each chunk: whole bins, and of the one where the cut is the tokens that are kept.
     const bool cuts = kept.key > kLeast || kept.index != 0xffffffffu;
@@ -604,35 +710,24 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
         if (lane == 0) s_chunk[c] = m;
     }
     __syncthreads();
-    auto keeps = [&](uint32_t k, int i) { return k > kept.key || (k == kept.key && (uint32_t)i <= kept.index); };
     if (cuts) {
-        if (!(row.bin(hi) == last && lo <= hi)) {   // the last cut was that of min_p, in another bin
-            const uint32_t to = last == 0 ? row.top_key : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) < last; }) - 1;
-            prepare(last == kBins - 1 ? kLeast : first_key(kLeast, row.top_key, [&](uint32_t k) { return row.bin(k) <= last; }), to,
-                    s.count[0][last]);
-        }
-        if (listed) {
+        prepare(last, s.count[0][last]);   // another bin where the last cut was that of min_p
+        if (from != kReadAgain) {
             each_token([&](uint32_t k, int i) {
-                if (keeps(k, i)) atomicAdd((unsigned long long *)&s_chunk[i / kChunk], (unsigned long long)row.mass(k));
+                if (kept.has(k, i) && row.bin(k) == last) atomicAdd((unsigned long long *)&s_chunk[i / kChunk], (unsigned long long)row.mass(k));
             });
         } else {
-            int chunk = -1;
-            uint64_t m = 0;
-            auto flush = [&]() {
-                for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
-                if (lane == 0 && chunk >= 0) s_chunk[chunk] += m;   // the wave's own chunk
-                m = 0;
-            };
             for (int c = wave; c < sp.chunks; c += WAVES) {
-                chunk = c;
+                uint64_t m = 0;
                 for (int i = c * kChunk + 4 * lane; i < min(a.vocab, (c + 1) * kChunk); i += 256) {
                     uint32_t key[4];
                     src.four(i, key);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (key[e] >= lo && key[e] <= hi && keeps(key[e], i + e)) m += row.mass(key[e]);
+                        if (kept.has(key[e], i + e) && row.bin(key[e]) == last) m += row.mass(key[e]);
                 }
-                flush();
+                for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+                if (lane == 0) s_chunk[c] += m;   // the wave's own
             }
         }
         __syncthreads();
@@ -649,8 +744,10 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     const int i0 = c * kChunk + 8 * t;
     src.four(i0, key), src.four(i0 + 4, key + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mine += m[e] = key[e] && keeps(key[e], i0 + e) ? row.mass(key[e]) : 0;
-    uint64_t upto = before + scan<T>(mine, s.part[0]) - mine;
+    for (int e = 0; e < 8; ++e) mine += m[e] = key[e] && kept.has(key[e], i0 + e) ? row.mass(key[e]) : 0;
+    uint64_t upto = mine, none = 0;
+    scan<T>(&upto, &none, s.part);
+    upto += before - mine;
     if (upto > target || upto + mine <= target) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -665,7 +762,7 @@ template <typename E, bool ALONG> hipError_t run_row(const SampleArgs &a, hipStr
     return hipGetLastError();
 }
 template <typename E> hipError_t run_long(const SampleArgs &a, const Space &sp, hipStream_t st) {
-    k_sample_bins<E><<<dim3(sp.chunks, a.batch), 256, 0, st>>>(a, sp);
+    k_sample_bins<E><<<dim3(sp.chunks, a.batch), 512, 0, st>>>(a, sp);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     k_sample_pick<E><<<a.batch, 1024, 0, st>>>(a, sp);
     return hipGetLastError();
@@ -675,8 +772,8 @@ template <typename E> hipError_t run_long(const SampleArgs &a, const Space &sp, 
 constexpr int kApart = 4096;
 
 template <typename E> hipError_t run(SampleArgs a, hipStream_t st) {
-    const Space sp = space_of(a.workspace, a.batch, a.vocab);
     const bool along = a.token_stride == 1;
+    const Space sp = space_of(a.workspace, a.batch, a.vocab, !along);
     if (a.vocab <= kRow && (along || a.vocab <= kApart)) return along ? run_row<E, true>(a, st) : run_row<E, false>(a, st);
     if (along) {
         k_sample_scan<E><<<dim3(sp.scans, a.batch), 256, 0, st>>>(a, sp);
@@ -692,7 +789,7 @@ template <typename E> hipError_t run(SampleArgs a, hipStream_t st) {
 }  // namespace
 
 // Whatever the strides are.
-int64_t sample_workspace(int batch, int vocab) { return vocab <= kApart ? 0 : space_of(nullptr, batch, vocab).bytes; }
+int64_t sample_workspace(int batch, int vocab) { return vocab <= kApart ? 0 : space_of(nullptr, batch, vocab, true).bytes; }
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st) {
     return a.dtype == BSP_F32 ? run<float>(a, st) : run<uint16_t>(a, st);
