@@ -25,7 +25,7 @@ __device__ __forceinline__ Turn turn(int pos, double freq) {
     return {c - s * rest, s + c * rest};
 }
 
-// A wave for a head of a token: queries, keys, values.
+// Any layout: a wave for a head of a token, queries, keys, values.
 template <typename E> __global__ __launch_bounds__(64) void k_rotary(RotaryArgs a) {
     const int i = blockIdx.x, lane = threadIdx.x, D = a.head_dim, half = a.rope.dims / 2;
     int h = blockIdx.y;
@@ -92,15 +92,155 @@ template <typename E> __global__ __launch_bounds__(64) void k_rotary(RotaryArgs 
     }
 }
 
+// Heads whose dimensions lie side by side in 16-byte vectors, of which a lane has two: the two halves of its pairs, or
+// two neighbours; past the rotated dimensions two that are passed on.  A workgroup has some tokens, whose cosines
+// and sines it works out once, and some of their heads, one after the other.  Bound by reading and writing.
+struct Rows {
+    int lanes_log2, tokens_log2;   // lanes of a head, tokens of a workgroup
+    int each;                      // heads of a workgroup that are worked on at a time
+};
+template <typename E, bool BESIDE> __global__ __launch_bounds__(256) void k_rotary_rows(RotaryArgs a, Rows w) {
+    constexpr int VE = 16 / sizeof(E), AHEAD = 4;
+    __shared__ Turn s_turn[16 * 128];
+    const int D = a.head_dim, pairs = a.rope.dims / 2, t = threadIdx.x;
+    const int lane = t & ((1 << w.lanes_log2) - 1), group = t >> w.lanes_log2, token = group & ((1 << w.tokens_log2) - 1);
+    const int i0 = blockIdx.x << w.tokens_log2, i = i0 + token, slots = a.heads + 2 * a.kv_heads;
+    for (int p = t; p < pairs << w.tokens_log2; p += 256) {
+        const int k = p / pairs, at = p - k * pairs;
+        Turn r = {1.f, 0.f};
+        if (i0 + k < a.n) r = turn(a.pos[i0 + k], a.freqs[at]);
+        s_turn[p] = {r.cos * a.rope.factor, r.sin * a.rope.factor};
+    }
+    // the lane's vectors, or none
+    const int rotated = a.rope.dims / VE, vectors = D / VE;
+    int first, second;
+    bool turned;
+    if (BESIDE) {
+        first = 2 * lane, second = first + 1, turned = first < rotated;   // of an odd number of rotated ones the last has a 1
+    } else {
+        turned = 2 * lane < rotated;
+        first = turned ? lane : 2 * lane, second = turned ? lane + rotated / 2 : first + 1;
+    }
+    const bool in = i < a.n, has[2] = {in && first < vectors, in && second < vectors};
+    const int d[2] = {min(first, vectors - 1) * VE, min(second, vectors - 1) * VE};
+    int64_t place = -1;
+    if (a.kv_heads && in) place = place_of(a.c, a.table, a.rows ? a.rows[i] : i, a.seqs, a.width, a.pos[i]);
+    __syncthreads();
+    // cosines and sines: of pairs of dimensions j of both vectors, or of neighbours in each
+    float c[VE], sn[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+        const int p = BESIDE ? first * (VE / 2) + j : first * VE + j;
+        const Turn r = turned && p < pairs ? s_turn[token * pairs + p] : Turn{1.f, 0.f};
+        c[j] = r.cos, sn[j] = r.sin;
+    }
+    const int h0 = blockIdx.y * w.each * (256 >> (w.lanes_log2 + w.tokens_log2)) + (group >> w.tokens_log2);
+    const int step = 256 >> (w.lanes_log2 + w.tokens_log2);
+    for (int k0 = 0; k0 < w.each; k0 += AHEAD) {
+        u32x4 v[AHEAD][2];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int h = min(h0 + (k0 + k) * step, slots - 1), at = min(i, a.n - 1);
+            const E *src = h < a.heads ? (const E *)a.x + at * a.xs.seq + h * a.xs.head
+                           : h < a.heads + a.kv_heads ? (const E *)a.k + at * a.ks.seq + (h - a.heads) * a.ks.head
+                                                      : (const E *)a.v + at * a.vs.seq + (h - a.heads - a.kv_heads) * a.vs.head;
+            if (k0 + k < w.each) v[k][0] = *(const u32x4 *)(src + d[0]), v[k][1] = *(const u32x4 *)(src + d[1]);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int h = h0 + (k0 + k) * step;
+            const bool query = h < a.heads, value = h >= a.heads + a.kv_heads, go = k0 + k < w.each && h < slots && (query || place >= 0);
+            E *dst = query ? (E *)a.y + i * a.ys.seq + h * a.ys.head
+                           : (E *)(value ? a.values : a.keys) + place + (h - a.heads - (value ? a.kv_heads : 0)) * a.c.head_stride;
+            const float *norm = query ? a.x_norm : value ? nullptr : a.k_norm;
+            if (!value && (norm || turned)) {
+                float x[2][VE];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) {
+                        if constexpr (sizeof(E) == 4) {
+                            const uint32_t bits = v[k][s][j];
+                            x[s][j] = __uint_as_float(bits);
+                        } else {
+                            const uint32_t bits = v[k][s][j / 2];
+                            x[s][j] = __uint_as_float(j % 2 ? bits & 0xffff0000u : bits << 16);
+                        }
+                    }
+                if (norm) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        float part = 0.f;
+#pragma unroll
+                        for (int j = 0; j < VE; ++j) part += x[s][j] * x[s][j];
+                        sum += has[s] ? part : 0.f;
+                    }
+                    for (int o = 1; o < 1 << w.lanes_log2; o *= 2) sum += __shfl_xor(sum, o);
+                    const float by = 1.f / sqrtf(sum / D + a.eps);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int j = 0; j < VE; ++j) x[s][j] *= by * norm[d[s] + j];
+                }
+                if (turned) {
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) {
+                        float *p = BESIDE ? &x[2 * j / VE][2 * j % VE] : &x[0][j], *o = BESIDE ? p + 1 : &x[1][j];
+                        const float y = *p * c[j] - *o * sn[j];
+                        *o = *o * c[j] + *p * sn[j], *p = y;
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (sizeof(E) == 4) v[k][s][j] = __float_as_uint(x[s][j]);
+                        else v[k][s][j] = pack_bf16(x[s][2 * j], x[s][2 * j + 1]);
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (go && has[s]) *(u32x4 *)(dst + d[s]) = v[k][s];
+        }
+    }
+}
+
+// Whether rows of heads begin at 16 bytes.
+bool in_vectors(const void *p, const bsp_strides &s, int esize) {
+    return s.dim == 1 && (uintptr_t)p % 16 == 0 && s.seq * esize % 16 == 0 && s.head * esize % 16 == 0;
+}
+
+template <typename E> hipError_t run(const RotaryArgs &a, hipStream_t st) {
+    constexpr int VE = 16 / sizeof(E);
+    const int slots = a.heads + 2 * a.kv_heads, esize = sizeof(E);
+    const bool beside = a.rope.layout == BSP_ROPE_INTERLEAVED;
+    const bool rows = a.head_dim % VE == 0 && a.rope.dims % (beside ? VE : 2 * VE) == 0 && in_vectors(a.x, a.xs, esize) &&
+                      in_vectors(a.y, a.ys, esize) && (!a.kv_heads || (in_vectors(a.k, a.ks, esize) && in_vectors(a.v, a.vs, esize)));
+    if (!rows) {
+        k_rotary<E><<<dim3(a.n, slots), 64, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    // A workgroup's groups of lanes go to up to 16 tokens, then to heads; few tokens leave each workgroup one head of a
+    // group, many all heads, for which the angles are worked out once.
+    Rows w;
+    w.lanes_log2 = 0;
+    while (2 << w.lanes_log2 < a.head_dim / VE) ++w.lanes_log2;
+    w.tokens_log2 = 0;
+    while (w.tokens_log2 < 4 && w.lanes_log2 + w.tokens_log2 < 6 && a.n >= 32 << w.tokens_log2) ++w.tokens_log2;
+    const int per = 256 >> (w.lanes_log2 + w.tokens_log2), all = (slots + per - 1) / per;
+    const int tokens = (a.n + (1 << w.tokens_log2) - 1) >> w.tokens_log2;
+    w.each = std::max(1, std::min(all, (int)((int64_t)tokens * all / 1024)));
+    const dim3 grid(tokens, (all + w.each - 1) / w.each);
+    if (beside) k_rotary_rows<E, true><<<grid, 256, 0, st>>>(a, w);
+    else k_rotary_rows<E, false><<<grid, 256, 0, st>>>(a, w);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st) {
-    const dim3 grid(a.n, a.heads + 2 * a.kv_heads);
-    if (a.dtype == BSP_F32)
-        k_rotary<float><<<grid, 64, 0, st>>>(a);
-    else
-        k_rotary<uint16_t><<<grid, 64, 0, st>>>(a);
-    return hipGetLastError();
+    return a.dtype == BSP_F32 ? run<float>(a, st) : run<uint16_t>(a, st);
 }
 
 }  // namespace bsp
