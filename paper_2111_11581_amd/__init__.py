@@ -607,40 +607,52 @@ def bsp_rope_freqs(dims: int, base: float, scaling: RopeScaling | None = None):
     return list(out)
 
 
+_float64 = None
+
+
 def _freqs(freqs, dims: int):
-    import torch
-    if dims > 0:
+    global _float64
+    if _float64 is None:
+        import torch
+        _float64 = torch.float64
+    if dims > 0 and (freqs is None or freqs.dtype is not _float64 or freqs.nbytes < 4 * dims or not freqs.is_cuda
+                     or not freqs.is_contiguous()):
         _dev("freqs", freqs, 4 * dims)
-        if freqs.dtype is not torch.float64:
-            raise ValueError("freqs must be float64")
+        raise ValueError("freqs must be float64")
 
 
 @functools.lru_cache(maxsize=4096)
-def _arrays(dt: int, *arrays):
-    """Strides of arrays of type dt; of each the name, the shape that it must have, and its own shape, strides and type."""
+def _arrays(dt: int, names, shape, *arrays):
+    """Strides of arrays of one shape and of type dt; `arrays` are their shape, strides and type."""
     out = []
-    for name, want, shape, strides, dtype in zip(*(arrays[i::5] for i in range(5))):
-        if tuple(shape) != want or dtype is not _float_types().get(dt):
-            raise ValueError(f"{name} must be {list(want)} of the type that the call names")
+    for name, have, strides, dtype in zip(names, arrays[0::3], arrays[1::3], arrays[2::3]):
+        if tuple(have) != shape or dtype is not _float_types().get(dt):
+            raise ValueError(f"{name} must be {list(shape)} of the type that the call names")
         out.append(_Strides(*strides))
     return out
 
 
-def _norm_weights(name: str, t, dim: int):
-    if t is not None:
-        _dev(name, t, 4 * dim, F32)
+@functools.lru_cache(maxsize=4096)
+def _rotary_layouts(key: bytes, n: int, heads: int, *arrays):
+    """Strides of queries, rotated queries, keys and values of n tokens; `arrays` are their, the cache's keys' and its
+    values' shape, strides and type."""
+    cache = CacheShape.from_buffer_copy(key)
+    return (*_arrays(cache.dtype, ("q", "q_out"), (n, heads, cache.head_dim), *arrays[:6]),
+            *_layouts(key, ("k", "v"), n, cache.kv_heads, *arrays[6:]))
 
 
 def bsp_rotary(dt: int, rope: Rope, freqs, x, pos, y, norm=None, eps: float = 1e-6, stream=None):
     """x and y: [tokens, heads, head_dim] of any strides (y's elements distinct)."""
     if x.dim() != 3:
         raise ValueError("x must be [tokens, heads, head_dim]")
-    n, heads, dim = want = tuple(x.shape)
-    xs, ys = _arrays(dt, "x", want, x.shape, x.stride(), x.dtype, "y", want, y.shape, y.stride(), y.dtype)
-    _on_device(x=x, y=y)
+    n, heads, dim = shape = tuple(x.shape)
+    xs, ys = _arrays(dt, ("x", "y"), shape, shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype)
+    if not (x.is_cuda and y.is_cuda):
+        _on_device(x=x, y=y)
     _freqs(freqs, rope.dims)
     _ints("pos", pos, n)
-    _norm_weights("norm", norm, dim)
+    if norm is not None:
+        _dev("norm", norm, 4 * dim, F32)
     st = lib().bsp_rotary(dt, rope, _p(freqs), n, heads, dim, x.data_ptr(), xs, pos.data_ptr(), _p(norm), eps, y.data_ptr(), ys,
                           _stream(stream))
     if st:
@@ -650,17 +662,17 @@ def bsp_rotary(dt: int, rope: Rope, freqs, x, pos, y, norm=None, eps: float = 1e
 def bsp_cache_append_rotary(cache: CacheShape, rope: Rope, freqs, q, k, v, q_out, keys, values, table, pos, rows=None,
                             q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
     """q and q_out: [tokens, heads, head_dim], k and v: [tokens, kv_heads, head_dim], of any strides."""
-    n, heads = q.shape[0], q.shape[1]
-    key, dim = bytes(cache), cache.head_dim
-    ks, vs = _layouts(key, ("k", "v"), n, cache.kv_heads, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
-                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
-    want = (n, heads, dim)
-    qs, qos = _arrays(cache.dtype, "q", want, q.shape, q.stride(), q.dtype, "q_out", want, q_out.shape, q_out.stride(), q_out.dtype)
+    n, heads, _ = q.shape
+    qs, qos, ks, vs = _rotary_layouts(bytes(cache), n, heads, q.shape, q.stride(), q.dtype, q_out.shape, q_out.stride(), q_out.dtype,
+                                      k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                                      keys.shape, keys.stride(), keys.dtype, values.shape, values.stride(), values.dtype)
     if not (q.is_cuda and k.is_cuda and v.is_cuda and q_out.is_cuda and keys.is_cuda and values.is_cuda):
         _on_device(q=q, k=k, v=v, q_out=q_out, keys=keys, values=values)
     _freqs(freqs, rope.dims)
-    _norm_weights("q_norm", q_norm, dim)
-    _norm_weights("k_norm", k_norm, dim)
+    if q_norm is not None:
+        _dev("q_norm", q_norm, 4 * cache.head_dim, F32)
+    if k_norm is not None:
+        _dev("k_norm", k_norm, 4 * cache.head_dim, F32)
     seqs, width = _table(table)
     _ints("pos", pos, n)
     if rows is not None:
@@ -732,7 +744,8 @@ def bsp_sample(dt: int, logits, u, tokens, temperature=None, top_k=None, top_p=N
     if logits.dim() != 2 or logits.dtype is not _float_types().get(dt):
         raise ValueError("logits must be [batch, vocab] of the type that the call names")
     batch, vocab = logits.shape
-    _on_device(logits=logits)
+    if not logits.is_cuda:
+        _on_device(logits=logits)
     _dev("u", u, 4 * batch, F32)
     _ints("tokens", tokens, batch)
     if temperature is not None:
