@@ -10,10 +10,12 @@ import contextlib
 
 import torch
 
-from . import (BF16, F32, HEAD_MAJOR, CacheShape, ConvShape, Scheme, bsp_attention, bsp_attention_workspace,
-               bsp_cache_append, bsp_cache_compact, bsp_cache_copy, bsp_cache_extend, bsp_cache_fork, bsp_cache_release,
-               bsp_cache_scratch, bsp_conv2d, bsp_linear, bsp_pack, bsp_packed_sizes, bsp_prune, bsp_q4_dequantize,
-               bsp_q4_linear, bsp_q4_quantize, bsp_q4_sizes, bsp_unpack)
+from . import (BF16, F32, HEAD_MAJOR, ROPE_HALF, CacheShape, ConvShape, Rope, RopeScaling, Scheme, bsp_attention,
+               bsp_attention_prefix, bsp_attention_prefix_workspace, bsp_attention_workspace, bsp_cache_append,
+               bsp_cache_append_rotary, bsp_cache_compact, bsp_cache_copy, bsp_cache_extend, bsp_cache_fork,
+               bsp_cache_release, bsp_cache_scratch, bsp_conv2d, bsp_linear, bsp_pack, bsp_packed_sizes, bsp_prune,
+               bsp_q4_dequantize, bsp_q4_linear, bsp_q4_quantize, bsp_q4_sizes, bsp_rope_freqs, bsp_rotary, bsp_sample,
+               bsp_sample_workspace, bsp_unpack)
 
 TORCH_DT = {F32: torch.float32, BF16: torch.bfloat16}
 
@@ -100,6 +102,30 @@ class QuantLayer:
                       stream)
 
 
+class Rotary:
+    """Rotary positions of the first ``dims`` dimensions of a head; ``factor`` multiplies what is rotated."""
+
+    def __init__(self, dims: int, base: float = 10000.0, layout: int = ROPE_HALF, factor: float = 1.0,
+                 scaling: RopeScaling | None = None, device="cuda"):
+        self.rope = Rope(layout, dims, factor)
+        self.freqs = torch.tensor(bsp_rope_freqs(dims, base, scaling), dtype=torch.float64, device=device)
+
+    def rotate(self, x, pos, y, dt: int, norm=None, eps: float = 1e-6, stream=None):
+        bsp_rotary(dt, self.rope, self.freqs, x, pos, y, norm, eps, stream)
+
+
+class Sampler:
+    """Chooses tokens of up to ``batch`` rows of logits; its workspace is its own, so its calls belong on one stream (or on
+    streams that wait for each other)."""
+
+    def __init__(self, batch: int, vocab: int, device="cuda"):
+        self.workspace = torch.empty(bsp_sample_workspace(batch, vocab), dtype=torch.uint8, device=device)
+
+    def sample(self, logits, u, tokens, dt: int, temperature=None, top_k=None, top_p=None, min_p=None, logp=None, stream=None):
+        """logits: [rows, vocab] of any strides; tokens (int32) and logp (fp32) receive the tokens and their probabilities."""
+        bsp_sample(dt, logits, u, tokens, temperature, top_k, top_p, min_p, logp, self.workspace, stream)
+
+
 class PagedCache:
     """Keys and values of ``layers`` layers for up to ``seqs`` sequences of up to ``width`` pages, in
     ``pages`` pages.  ``longest`` is the longest list that a call takes.
@@ -132,11 +158,21 @@ class PagedCache:
         keys, values = self.planes[layer]
         bsp_cache_append(self.shape, k, v, keys, values, self.table, pos, rows, stream)
 
-    def reserve(self, batch: int, heads: int, stream=None):
-        """A workspace for attend with `batch` sequences; attend makes one where this was not called.
-        Captured graphs and calls under way hold the one they were given, so that it lives as long as
-        the cache does; each is at least twice the one before, and all before take no more than it."""
-        need = bsp_attention_workspace(self.shape, batch, heads, self.table.shape[1])
+    def append_rotary(self, layer: int, rotary: Rotary, q, k, v, q_out, pos, rows=None, q_norm=None, k_norm=None,
+                      eps: float = 1e-6, stream=None):
+        """append, with the keys normed and rotated to their positions, and q so too into q_out (which may be q)."""
+        keys, values = self.planes[layer]
+        bsp_cache_append_rotary(self.shape, rotary.rope, rotary.freqs, q, k, v, q_out, keys, values, self.table, pos, rows, q_norm,
+                                k_norm, eps, stream)
+
+    def reserve(self, batch: int, heads: int, stream=None, groups: int | None = None):
+        """A workspace for attend with `batch` sequences, or for attend_prefix with `groups` groups of them; these
+        make one where this was not called.  Captured graphs and calls under way hold the one they
+        were given, so that it lives as long as the cache does; each is at least twice the one before, and
+        all before take no more than it."""
+        width = self.table.shape[1]
+        need = bsp_attention_workspace(self.shape, batch, heads, width) if groups is None else \
+            bsp_attention_prefix_workspace(self.shape, batch, heads, groups, width)
         if self.workspace.numel() < need:
             self._outgrown.append(self.workspace)
             need = max(need, 2 * self.workspace.numel())
@@ -148,6 +184,15 @@ class PagedCache:
         self.reserve(q.shape[0], q.shape[1], stream)
         keys, values = self.planes[layer]
         bsp_attention(self.shape, q, keys, values, self.table, self.lens, y, scale, window, rows, lse, self.workspace, stream)
+
+    def attend_prefix(self, layer: int, q, y, scale: float, starts, shared, rows=None, prefix_rows=None, window: int = 0, lse=None,
+                      stream=None):
+        """attend where sequences starts[g] .. starts[g + 1] - 1 of the call share their first shared[g] tokens, which lie
+        in the pages of sequence prefix_rows[g] (by default of the first of them)."""
+        self.reserve(q.shape[0], q.shape[1], stream, shared.numel())
+        keys, values = self.planes[layer]
+        bsp_attention_prefix(self.shape, q, keys, values, self.table, self.lens, starts, shared, y, scale, window, rows, prefix_rows,
+                             lse, self.workspace, stream)
 
     def fork(self, parents, children, stream=None):
         bsp_cache_fork(self.table, self.lens, self.refs, parents, children, self.scratch, stream)

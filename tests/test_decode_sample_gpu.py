@@ -1,0 +1,175 @@
+"""The decoder with rotary positions and norms of heads, and the sampling of continuations that share a prompt, against
+the same model computed in 64 bits without a cache, and against sampling from its own logits."""
+
+import math
+
+import numpy as np
+import pytest
+
+from tests import sampling_model as S
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def D():
+    import torch   # first: the library then runs on torch's HIP runtime
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2111_11581_amd import decode
+    return decode
+
+
+# fp32: a chain of some thirty fp32 sums of up to 200 terms, 2^-24 each; bf16: some twelve roundings of up to 2^-8 (2^-9 in the
+# mean of squares) in a row, whose errors add up as their squares
+TOLERANCE = {"f32": 2e-5, "bf16": 3e-2}
+
+
+def small(D, dt, layout=0, dims=16, **kw):
+    import paper_2111_11581_amd as B
+    scaling = B.RopeScaling(4.0, 40.0, 1.0, 4.0, B.RAMP_TURNS)
+    c = dict(layers=2, heads=4, kv_heads=2, head_dim=24, ffn=200, vocab=77, longest=90, group=32, rate=2, seed=3)
+    c.update(kw)
+    return D.Decoder(dtype=D.F32 if dt == "f32" else D.BF16, rotary=D.Rotary(dims, 100.0, layout, 1.1, scaling), **c)
+
+
+def plain_logits(model, tokens):
+    """Logits [vocab][tokens] of one sequence."""
+    import torch
+
+    def w(layer):
+        return layer.dequantize().double().cpu()
+
+    def norm(x):
+        return x * torch.rsqrt(x.square().mean(0, keepdim=True) + 1e-6)
+
+    n, h, kv, d = len(tokens), model.heads, model.kv_heads, model.head_dim
+    rope = model.rotary.rope
+    freq = S.freqs(rope.dims, 100.0, 4.0, 40.0, 1.0, 4.0, 1)
+
+    def rotate(a, weight, heads):   # [heads * d][tokens] -> [heads, d, tokens]
+        a = a.view(heads, d, n).permute(2, 0, 1).numpy()
+        a, _ = S.rotate(a, np.arange(n), freq, rope.layout == 1, float(np.float32(1.1)), weight.double().cpu().numpy(), 1e-6)
+        return torch.from_numpy(a).permute(1, 2, 0)
+
+    x = model.embedding.double().cpu()[tokens].t()
+    later = torch.ones(n, n, dtype=torch.bool).triu(1)
+    for block in model.blocks:
+        q, k, v = (w(block["qkv"]) @ norm(x)).split([h * d, kv * d, kv * d])
+        q, k, v = rotate(q, block["q_norm"], h), rotate(k, block["k_norm"], kv), v.view(kv, d, n)
+        k, v = (a.repeat_interleave(h // kv, 0) for a in (k, v))
+        score = (q.transpose(1, 2) @ k / math.sqrt(d)).masked_fill(later, -math.inf)
+        x = x + w(block["out"]) @ (v @ score.softmax(2).transpose(1, 2)).reshape(h * d, n)
+        x = x + w(block["down"]) @ (w(block["up"]) @ norm(x)).relu()
+    return w(model.head) @ norm(x)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", [{}, dict(layout=1, dims=24), dict(heads=3, kv_heads=3, head_dim=40, dims=40, ffn=65, rate=1)])
+def test_steps_of_forks_that_share_a_prompt(D, dt, kw):
+    model = small(D, dt, **kw)
+    cache = model.cache(7, 60, page_size=5)
+    text = {r: [] for r in range(7)}
+
+    def step(tokens, rows, groups=None):
+        logits = model.step(cache, D.ints(tokens), D.ints(rows), groups)
+        for j, (t, r) in enumerate(zip(tokens, rows)):
+            text[r] = text[r] + [t]
+            want = plain_logits(model, text[r])[:, -1]
+            err = (logits[:, j].double().cpu() - want).norm() / want.norm()
+            assert err < TOLERANCE[dt], (r, float(err))
+
+    for t in range(12):
+        step([t, 70 - t] if t < 8 else [t], [0, 1] if t < 8 else [0])
+    cache.fork(D.ints([0, 0, 0, 1, 1]), D.ints([2, 3, 4, 5, 6]))
+    for r in (2, 3, 4):
+        text[r] = text[0]
+    text[5] = text[6] = text[1]
+    groups = (D.ints([0, 3, 5]), D.ints([12, 8]), D.ints([0, 1]))
+    for t in range(7):
+        step([10 + t, 20 + t, 30, 40, 50 + t], [2, 3, 4, 5, 6], groups)
+    by_first = (D.ints([0, 2, 4]), D.ints([10, 5]), None)   # whole pages that the first of each has
+    for t in range(3):
+        step([60, 61, 62, t], [4, 2, 6, 5], by_first)
+    cache.release(D.ints([0, 1]))
+    cache.compact()
+    step([1, 2, 3], [3, 4, 5], (D.ints([0, 2]), D.ints([10]), None))
+
+
+def test_samples(D):
+    """Every token is the one that its row's logits, its random number and the cuts give."""
+    import torch
+    model = small(D, "f32")
+    prompts, new, samples = [[1, 2, 3], [4], [5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16, 17, 18, 19, 20, 21]], [6, 1, 9], 5
+    kw = dict(temperature=0.9, top_k=30, top_p=0.95, min_p=0.01)
+    tokens, logp, cache = D.sample(model, prompts, new, samples, seed=7, page_size=4, **kw)
+    assert int(cache.refs.sum()) == 0 and int(cache.lens.sum()) == 0
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    running = list(range(3))
+    for made in range(max(new)):
+        running = [i for i in running if new[i] > made]
+        u = torch.rand(len(running) * samples, generator=gen, device="cuda").tolist()
+        for k, i in enumerate(running):
+            for j in range(samples):
+                row = tokens[i][j].tolist()
+                want = plain_logits(model, prompts[i] + row[:made])[:, -1].numpy()
+                token, lp, _ = S.sample(want, u[k * samples + j], float(np.float32(0.9)), 30, float(np.float32(0.95)), float(np.float32(0.01)))
+                # logits are off by 2e-5 of some units, which moves probabilities by as much of themselves
+                assert row[made] == token and abs(float(logp[i][j, made]) - lp) < 1e-3
+    again, _, _ = D.sample(model, prompts, new, samples, seed=7, page_size=4, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(tokens, again))
+    greedy, scores, _ = D.sample(model, prompts, new, 2, temperature=0.0)
+    for p, n, t, s in zip(prompts, new, greedy, scores):
+        assert torch.equal(t[0], t[1]) and float(s.abs().max()) == 0.0
+        for m in range(n):
+            assert int(plain_logits(model, p + t[0].tolist()[:m])[:, -1].argmax()) == int(t[0, m])
+
+
+def test_a_captured_step(D):
+    """A step of several continuations and the choice of their tokens, in a graph that is replayed."""
+    import torch
+    model = small(D, "bf16")
+    runs = []
+    for captured in (False, True):
+        cache = model.cache(7, 60, page_size=5)
+        for t in range(9):
+            model.step(cache, D.ints([t]), D.ints([0]))
+        cache.fork(D.ints([0] * 6), D.ints([1, 2, 3, 4, 5, 6]))
+        rows, groups = D.ints([1, 2, 3, 4, 5, 6]), (D.ints([0, 6]), D.ints([9]), D.ints([0]))
+        sampler = D.Sampler(6, model.vocab)
+        tokens, u, p = D.ints([1, 2, 3, 4, 5, 6]), torch.zeros(6, device="cuda"), torch.full((6,), 0.9, device="cuda")
+        cache.reserve(6, model.heads, groups=1)
+
+        def step():
+            sampler.sample(model.step(cache, tokens, rows, groups).t(), u, tokens, D.F32, top_p=p)
+        gen = torch.Generator(device="cuda").manual_seed(1)
+        graph, out = torch.cuda.CUDAGraph(), []
+        if captured:
+            side = torch.cuda.Stream()
+            state = [t.clone() for t in (cache.table, cache.lens, cache.refs, cache.data, tokens)]
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                step()   # code is loaded
+            torch.cuda.current_stream().wait_stream(side)
+            for a, b in zip((cache.table, cache.lens, cache.refs, cache.data, tokens), state):
+                a.copy_(b)
+            with torch.cuda.graph(graph):
+                step()
+        for _ in range(20):
+            u.copy_(torch.rand(6, generator=gen, device="cuda"))
+            graph.replay() if captured else step()
+            out.append(tokens.tolist())
+        runs.append((out, cache.lens.tolist()))
+    assert runs[0] == runs[1]
+
+
+def test_refusals(D):
+    model = small(D, "bf16")
+    for prompts, new, samples in (([], [], 1), ([[]], [1], 1), ([[1]], [0], 1), ([[1]], [1, 1], 1), ([[1]], [1], 0), ([[1] * 80], [12], 2)):
+        with pytest.raises(ValueError):
+            D.sample(model, prompts, new, samples)
+
+
+def test_command(D, capsys):
+    D.main(["--prompts", "2", "--samples", "3", "--tokens", "4", "--dtype", "f32", "--layers", "1", "--top-k", "20", "--temperature", "0.7"])
+    assert "0 pages in use" in capsys.readouterr().out
