@@ -31,6 +31,7 @@ typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
 
 // Columns of a task: staged ones only for what fits LDS and registers.
 template <typename E, int DP> constexpr int kColumns = sizeof(E) == 2 && DP <= 128 ? 256 : 32;
+int dims_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 int columns_of(int dtype, int head_dim) { return dtype == BSP_BF16 && head_dim <= 128 ? 256 : 32; }
 // Waves of k_prefix: two for a SIMD, or one where a wave's registers ask for it.
 template <int DP> constexpr int kTaskWaves = DP == 256 ? 4 : 8;
@@ -60,6 +61,7 @@ struct Parts {
 };
 struct Space {
     Head *head;
+    void *q;                  // queries [batch][heads][dims], 0 past head_dim, of the scale's sign
     Member *member;
     Task *task;
     Parts shared, own;
@@ -67,7 +69,7 @@ struct Space {
 };
 // Of either kind there are as many tasks as units, which nothing cuts, and kRounds * kGrid more at most.
 struct Sizes {
-    int64_t shared_tasks, own_tasks;
+    int64_t shared_tasks, own_tasks, query_bytes;
     int columns, own_columns;
 };
 Sizes sizes_of(const CacheArgs &c, int batch, int heads, int groups) {
@@ -76,6 +78,7 @@ Sizes sizes_of(const CacheArgs &c, int batch, int heads, int groups) {
     const int block = columns_of(c.dtype, c.head_dim);
     s.columns = (int)std::min<int64_t>(block, (batch * group + 15) / 16 * 16);
     s.own_columns = (int)std::min<int64_t>(16, group);
+    s.query_bytes = (int64_t)batch * heads * dims_of(c.head_dim) * (c.dtype == BSP_F32 ? 4 : 2);
     s.shared_tasks = groups ? (batch * group / block + groups) * c.kv_heads + kRounds * kGrid : 0;
     s.own_tasks = (int64_t)batch * c.kv_heads * ((group + 15) / 16) + kRounds * kGrid;
     return s;
@@ -94,12 +97,21 @@ __host__ __device__ inline Space space_of(void *workspace, const Sizes &z, int b
         p.columns = columns, p.o = (float *)take(n * head_dim * 4), p.m = (float *)take(n * 4), p.l = (float *)take(n * 4);
         return p;
     };
-    s.head = (Head *)take(sizeof(Head)), s.member = (Member *)take((int64_t)batch * sizeof(Member));
+    s.head = (Head *)take(sizeof(Head)), s.q = take(z.query_bytes), s.member = (Member *)take((int64_t)batch * sizeof(Member));
     s.task = (Task *)take((kGrid + z.shared_tasks + z.own_tasks) * sizeof(Task));
     s.shared = parts(z.shared_tasks, z.columns), s.own = parts(z.own_tasks, z.own_columns);
     s.bytes = at - (char *)workspace;
     return s;
 }
+
+// The factor of scores in powers of two, and the sign that queries take instead of it, so that a larger product is a
+// larger score; a scale of 0 makes queries of 0.
+struct Scale {
+    float by, sign;
+    __device__ __forceinline__ explicit Scale(float scale)
+        : by(scale == 0.f ? 1.f : fabsf(scale) * kLog2e), sign(scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f) {}
+    template <typename E> __device__ __forceinline__ E of(E v) const { return sign == 1.f ? v : from_f32<E>(to_f32(v) * sign); }
+};
 
 // ---- the plan ----------------------------------------------------------------------------------------
 
@@ -128,7 +140,31 @@ template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wa
 
 // A workgroup, a thread for a group and for a sequence: as many waves as these need, since each wave makes every
 // scan and sum longer.  Bound by latency.
-__global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
+// The other workgroups lay the queries out meanwhile, so that a task reads its operands as they lie: eight dimensions a
+// thread, along the sequences where these lie side by side.
+template <typename E, int DP> __device__ __forceinline__ void lay_queries(const AttnArgs &a, E *to, int64_t i) {
+    constexpr int VE = 16 / sizeof(E), N = DP / VE;
+    const int rows = a.batch * a.heads;
+    if (i >= (int64_t)rows * N) return;
+    int b, h, d0;
+    if (a.qs.dim == 1) d0 = (int)(i % N) * VE, h = (int)(i / N % a.heads), b = (int)(i / N / a.heads);
+    else b = (int)(i % a.batch), d0 = (int)(i / a.batch % N) * VE, h = (int)(i / a.batch / N);
+    const E *q = (const E *)a.q + b * a.qs.seq + h * a.qs.head;
+    const Scale scale(a.scale);
+    __attribute__((aligned(16))) E v[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = q[min(d0 + e, a.c.head_dim - 1) * a.qs.dim];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = d0 + e < a.c.head_dim ? scale.of(v[e]) : (E)0;
+    *(u32x4 *)(to + ((int64_t)b * a.heads + h) * DP + d0) = *(const u32x4 *)v;
+}
+
+template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
+    if (blockIdx.x > 0) {
+        const Space space = space_of(p.a.workspace, z, p.a.batch, p.a.c.head_dim);
+        lay_queries<E, DP>(p.a, (E *)space.q, (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x);
+        return;
+    }
     constexpr int MOST = kMost / 64;
     const int T = blockDim.x, W = T / 64;
     __shared__ int s_lo[kMost + 1], s_from[kMost], s_to[kMost], s_wave[MOST];
@@ -136,7 +172,7 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
     __shared__ struct {
         int row, lead, shared, begin, cut, skip, len;
     } s_own[kMost];
-    __shared__ int64_t s_sum[MOST][4];
+    __shared__ int64_t s_sum[MOST][4], s_all;
     const AttnArgs &a = p.a;
     const int t = threadIdx.x, G = p.groups, B = a.batch;
     const Space space = space_of(a.workspace, z, B, a.c.head_dim);
@@ -214,49 +250,45 @@ __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, in
         // in fp64, which holds these whole numbers, as a division of 64 bits takes a hundred instructions
         return i.units ? max(1, min(i.steps, (int)min(ceil((double)i.steps * i.cost / (double)most), 1e9))) : 0;
     };
-    int64_t best = INT64_MAX, most = 1;
-    for (int r = 1; r <= kRounds; ++r) {
-        const int64_t m = max((int64_t)(2 * kTaskCost), (int64_t)ceil((double)total / (kGrid * r)));
-        int64_t tasks = 0, cost = 0;
-        for (int k = 0; k < 2; ++k) {
-            const int n = pieces_of(item[k], m);
-            if (!n) continue;
-            if (k == 0) tasks = (int64_t)n * item[k].units;
-            cost = max(cost, k == 0 ? (int64_t)((item[k].steps + n - 1) / n) * item[k].cost : 0);
+    static_assert(kRounds == 2, "");
+    int64_t most_of[kRounds], tasks[kRounds], longest[kRounds];
+    for (int r = 0; r < kRounds; ++r) {
+        most_of[r] = max((int64_t)(2 * kTaskCost), (int64_t)ceil((double)total / (kGrid * (r + 1))));
+        const int n = pieces_of(item[0], most_of[r]);
+        tasks[r] = (int64_t)n * item[0].units, longest[r] = n ? (int64_t)((item[0].steps + n - 1) / n) * item[0].cost : 0;
+    }
+    for (int d = 1; d < 64; d *= 2)
+        for (int r = 0; r < kRounds; ++r) {
+            tasks[r] += __shfl_xor(tasks[r], d), longest[r] = max(longest[r], (int64_t)__shfl_xor(longest[r], d));
         }
-        for (int d = 1; d < 64; d *= 2) cost = max(cost, (int64_t)__shfl_xor(cost, d));
-        if (t % 64 == 0) s_sum[t / 64][3] = cost;
-        total_of(tasks, 2);
-        __syncthreads();
-        int64_t n = 0, largest_task = 0;
-        for (int w = 0; w < W; ++w) n += s_sum[w][2], largest_task = max(largest_task, s_sum[w][3]);
-        __syncthreads();
-        const int64_t time = max((n + kGrid - 1) / kGrid * (largest_task + kTaskCost), total / kGrid + kTaskCost * r);
-        if (time < best) best = time, most = m;
+    __syncthreads();   // the total has been read
+    if (t % 64 == 0) s_sum[t / 64][0] = tasks[0], s_sum[t / 64][1] = tasks[1], s_sum[t / 64][2] = longest[0], s_sum[t / 64][3] = longest[1];
+    __syncthreads();
+    int64_t best = INT64_MAX, most = 1;
+    for (int r = 0; r < kRounds; ++r) {
+        int64_t n = 0, l = 0;
+        for (int w = 0; w < W; ++w) n += s_sum[w][r], l = max(l, s_sum[w][2 + r]);
+        const int64_t time = max((n + kGrid - 1) / kGrid * (l + kTaskCost), total / kGrid + kTaskCost * (r + 1));
+        if (time < best) best = time, most = most_of[r];
     }
-    // numbers of tasks: those of groups, then those of sequences
-    int first_task[2], before = 0;
-    for (int k = 0; k < 2; ++k) {
-        const int n = pieces_of(item[k], most), count = n * item[k].units;
-        const int upto = scan(count, s_wave, [](int x, int y) { return x + y; });
-        __syncthreads();
-        if (t == T - 1) s_wave[0] = upto;
-        __syncthreads();
-        first_task[k] = before + upto - count;
-        const int items = k ? B : G, at = k ? G : 0;
-        if (t < items) s_task[at + t] = first_task[k], s_pieces[at + t] = n, s_steps[at + t] = item[k].steps;
-        if (k == 0 && t == 0) space.head->shared = s_wave[0];
-        before += s_wave[0];
-        __syncthreads();
-    }
+    // numbers of tasks: those of groups, then those of sequences, both in one scan
+    const int n0 = pieces_of(item[0], most), n1 = pieces_of(item[1], most);
+    const int64_t count = (int64_t)(n0 * item[0].units) << 32 | (uint32_t)(n1 * item[1].units);
+    const int64_t upto = scan(count, &s_sum[0][0], [](int64_t x, int64_t y) { return x + y; });
+    if (t == T - 1) s_all = upto;
+    __syncthreads();
+    const int of_groups = (int)(s_all >> 32), before = of_groups + (int)(uint32_t)s_all;
+    const int first_task[2] = {(int)((upto - count) >> 32), of_groups + (int)(uint32_t)(upto - count)};
+    if (t < G) s_task[t] = first_task[0], s_pieces[t] = n0, s_steps[t] = item[0].steps;
+    if (t < B) s_task[G + t] = first_task[1], s_pieces[G + t] = n1, s_steps[G + t] = item[1].steps;
     if (t == 0) {
         s_task[G + B] = before;
-        space.head->tasks = before, space.head->next = min(before, kGrid);
+        space.head->shared = of_groups, space.head->tasks = before, space.head->next = min(before, kGrid);
         for (int i = 0; i < 4; ++i) space.head->zero[i] = 0;
     }
     __syncthreads();
     if (t < B) {
-        Member m = {0, 0, 0, 0, first_task[1] - s_task[G], pieces_of(item[1], most), {0, 0}};
+        Member m = {0, 0, 0, 0, first_task[1] - of_groups, n1, {0, 0}};
         if (core_to) {
             m.task = s_task[group], m.pieces = s_pieces[group], m.place = t - s_lo[group];
             m.blocks = ((s_lo[group + 1] - s_lo[group]) * a.group + block_columns - 1) / block_columns;
@@ -311,15 +343,6 @@ template <typename E, int DP, int N, int WAVES> struct Narrow {
     };
 };
 
-// The factor of scores in powers of two, and the sign that queries take instead of it, so that a larger product is a
-// larger score; a scale of 0 makes queries of 0.
-struct Scale {
-    float by, sign;
-    __device__ __forceinline__ explicit Scale(float scale)
-        : by(scale == 0.f ? 1.f : fabsf(scale) * kLog2e), sign(scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f) {}
-    template <typename E> __device__ __forceinline__ E of(E v) const { return sign == 1.f ? v : from_f32<E>(to_f32(v) * sign); }
-};
-
 // Largest score and sum of a softmax, of a lane's column.  The reference is not the maximum but within 2^6 of it, or
 // above: it moves only where some score passes it by so much, which costs a vote a step instead of two
 // exchanges and a product for every output.
@@ -349,10 +372,17 @@ __device__ __forceinline__ void stage_queries(const AttnArgs &a, const Task &k, 
     }
 }
 
+// A column's query as it was laid out; past the columns that of the last.
+template <int DP, typename E> __device__ __forceinline__ const E *query_of(const AttnArgs &a, const Task &k, const E *laid, int c) {
+    const int at = k.c0 + min(c, k.columns - 1), s = at / a.group;
+    return laid + ((int64_t)(k.first + s) * a.heads + k.j * a.group + at - s * a.group) * DP;
+}
+
 // N sixteens of columns over a task's tokens.  finish(column, d, output, reference, sum) takes what comes of
 // them, joined over the waves.
+// `laid`: queries as lay_queries leaves them, or none.
 template <typename E, int DP, bool FULL, int N, int WAVES, typename F>
-__device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, N, WAVES> &sh, const Task &k, F finish) {
+__device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, N, WAVES> &sh, const Task &k, const E *laid, F finish) {
     typedef Step<E, DP> St;
     constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV, THREADS = 64 * WAVES;
     const int D = a.c.head_dim, wave = uni(threadIdx.x / 64);
@@ -380,10 +410,13 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
         if (base > k.from) __syncthreads();   // places of the tile before are no longer read
         for (int t = threadIdx.x; t < padded; t += THREADS)
             sh.place[t] = place_in(a, k, base + t);
-        if (base == k.from)   // queries come while the places do
+        if (base == k.from && laid) {   // queries come while the places do
+#pragma unroll
+            for (int c = 0; c < N; ++c) St::load_q(q[c], query_of<DP>(a, k, laid, c * 16 + r), quad);
+        } else if (base == k.from)
             stage_queries<E, 16 * N, DP, THREADS>(a, k, [&](int c, int d, E v) { sh.q[c][d] = v; });
         __syncthreads();
-        if (base == k.from)
+        if (base == k.from && !laid)
 #pragma unroll
             for (int c = 0; c < N; ++c) St::load_q(q[c], sh.q[c * 16 + r], quad);
         uint32_t dead;   // the lane's tokens that hold nothing
@@ -537,8 +570,8 @@ template <int N> __device__ __forceinline__ void copy16(const char *const *src, 
 
 // CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.
 template <int DP, bool FULL, int CW>
-__device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, const Task &k, const void *zero, const Parts &parts,
-                                             int64_t task) {
+__device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, const Task &k, const uint16_t *laid, const void *zero,
+                                             const Parts &parts, int64_t task) {
     typedef uint16_t E;
     constexpr int NC = DP / 32, ND = DP / 16, GR = DP / 8, SETS = 8 / CW, TOKENS = kStep / SETS;
     const int D = a.c.head_dim, wave = uni(threadIdx.x / 64), set = wave / CW, c_wave = wave % CW * 32;
@@ -589,10 +622,6 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
 #pragma unroll
     for (int i = 0; i < kTile / 512; ++i) ahead[i] = place_in(a, k, k.from + threadIdx.x + 512 * i);
     fill_places(0, ahead);
-    // queries, through the second stage
-    stage_queries<E, CW * 32, DP, 512>(a, k, [&](int c, int d, E v) {
-        sh.stage[1][0][c * DP + ((d / 8 ^ turn_of<DP>(c)) * 8 + d % 8)] = v;
-    });
     __syncthreads();
     copy(0);
     u32x4 q[2][NC];
@@ -602,7 +631,7 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
     for (int n = 0; n < 2; ++n) {
         const int c = c_wave + n * 16 + r;
 #pragma unroll
-        for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)&sh.stage[1][0][c * DP + ((i * 4 + quad) ^ turn_of<DP>(c)) * 8];
+        for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)(query_of<DP>(a, k, laid, c) + i * 32 + quad * 8);
         m[n] = -INFINITY, ref[n] = l[n] = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[n][d] = (f32x4){0, 0, 0, 0};
@@ -797,6 +826,7 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
     const AttnArgs &a = p.a;
     const Space space = space_of(a.workspace, z, a.batch, a.c.head_dim);
     const int tasks = uni(space.head->tasks), shared = uni(space.head->shared);
+    const E *laid = (const E *)space.q;
     int slot = blockIdx.x;   // of the task; later ones have their own number's
     for (;;) {
         const Task *at = space.task + slot;
@@ -815,17 +845,17 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
             if (d == 0) parts.m[i] = m, parts.l[i] = l;
         };
         if (k.columns <= 16) {
-            columns_narrow<E, DP, FULL, 1, kTaskWaves<DP>>(a, sh.one, k, finish);
+            columns_narrow<E, DP, FULL, 1, kTaskWaves<DP>>(a, sh.one, k, laid, finish);
         } else if (k.columns <= 32 || !Shared<E, DP>::WIDE) {
-            columns_narrow<E, DP, FULL, 2, kTaskWaves<DP>>(a, sh.two, k, finish);
+            columns_narrow<E, DP, FULL, 2, kTaskWaves<DP>>(a, sh.two, k, laid, finish);
         } else if constexpr (Shared<E, DP>::WIDE) {
             const void *zero = space.head->zero;
             if (k.columns <= 64)
-                columns_wide<DP, FULL, 2>(a, sh.wide, k, zero, parts, number);
+                columns_wide<DP, FULL, 2>(a, sh.wide, k, laid, zero, parts, number);
             else if (k.columns <= 128)
-                columns_wide<DP, FULL, 4>(a, sh.wide, k, zero, parts, number);
+                columns_wide<DP, FULL, 4>(a, sh.wide, k, laid, zero, parts, number);
             else
-                columns_wide<DP, FULL, 8>(a, sh.wide, k, zero, parts, number);
+                columns_wide<DP, FULL, 8>(a, sh.wide, k, laid, zero, parts, number);
         }
         if (tasks <= kGrid) return;
         slot = uni(sh.next);
@@ -923,7 +953,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
         }
         return;
     }
-    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, [&](int c, int d, float o, float m, float l) {
+    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, (const E *)nullptr, [&](int c, int d, float o, float m, float l) {
         const int h = k.j * a.group + k.c0 + c;
         ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
         if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;
@@ -941,7 +971,9 @@ template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, boo
         return hipGetLastError();
     }
     const Sizes z = sizes_of(a.c, a.batch, a.heads, p.groups);
-    k_prefix_plan<<<1, std::max(256, (a.batch + 63) / 64 * 64), 0, st>>>(p, z, kColumns<E, DP>);
+    const int threads = std::max(256, (a.batch + 63) / 64 * 64);
+    const int64_t pieces = z.query_bytes / 16;
+    k_prefix_plan<E, DP><<<(int)(1 + (pieces + threads - 1) / threads), threads, 0, st>>>(p, z, kColumns<E, DP>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     k_prefix<E, DP, FULL><<<kGrid, 64 * kTaskWaves<DP>, 0, st>>>(p, z);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
