@@ -25,70 +25,149 @@ __device__ __forceinline__ Turn turn(int pos, double freq) {
     return {c - s * rest, s + c * rest};
 }
 
-// Any layout: a wave for a head of a token, queries, keys, values.
-template <typename E> __global__ __launch_bounds__(64) void k_rotary(RotaryArgs a) {
-    const int i = blockIdx.x, lane = threadIdx.x, D = a.head_dim, half = a.rope.dims / 2;
-    int h = blockIdx.y;
+// Any layout: a wave for some heads of a token, queries, keys, values, one after the other.
+template <typename E> __global__ __launch_bounds__(64) void k_rotary(RotaryArgs a, int each) {
+    const int i = blockIdx.x, lane = threadIdx.x, D = a.head_dim, half = a.rope.dims / 2, slots = a.heads + 2 * a.kv_heads;
     const int pos = a.pos[i];
-    const E *src;
-    E *dst;
-    int64_t from, to;   // strides of dimensions
-    const float *norm = nullptr;
-    bool rotated = true;
-    if (h < a.heads) {
-        src = (const E *)a.x + i * a.xs.seq + h * a.xs.head, from = a.xs.dim;
-        dst = (E *)a.y + i * a.ys.seq + h * a.ys.head, to = a.ys.dim;
-        norm = a.x_norm;
-    } else {
-        h -= a.heads;
-        const bool value = h >= a.kv_heads;
-        if (value) h -= a.kv_heads;
-        const int64_t at = place_of(a.c, a.table, a.rows ? a.rows[i] : i, a.seqs, a.width, pos);
-        if (at < 0) return;
-        const bsp_strides s = value ? a.vs : a.ks;
-        src = (const E *)(value ? a.v : a.k) + i * s.seq + h * s.head, from = s.dim;
-        dst = (E *)(value ? a.values : a.keys) + at + h * a.c.head_stride, to = 1;
-        norm = value ? nullptr : a.k_norm;
-        rotated = !value;
-    }
-    // a lane's pairs, and its dimensions that are passed on: all are read before any is written
-    const int pairs = rotated ? half : 0, rest = 2 * pairs;
     const bool beside = a.rope.layout == BSP_ROPE_INTERLEAVED;
-    float x[2][2], z[4];
-    E whole[4];
-    float sum = 0.f;
+    Turn r[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int p = lane + 64 * j, d0 = beside ? 2 * p : p, d1 = beside ? 2 * p + 1 : p + pairs;
-        x[j][0] = p < pairs ? to_f32(src[d0 * from]) : 0.f, x[j][1] = p < pairs ? to_f32(src[d1 * from]) : 0.f;
-        sum += x[j][0] * x[j][0] + x[j][1] * x[j][1];
+        const int p = lane + 64 * j;
+        r[j] = p < half && blockIdx.y * each < a.heads + a.kv_heads ? turn(pos, a.freqs[p]) : Turn{1.f, 0.f};
+        r[j].cos *= a.rope.factor, r[j].sin *= a.rope.factor;
     }
+    int64_t place = -1;
+    if ((blockIdx.y + 1) * each > a.heads && a.kv_heads) place = place_of(a.c, a.table, a.rows ? a.rows[i] : i, a.seqs, a.width, pos);
+    for (int slot = blockIdx.y * each; slot < min(slots, (int)(blockIdx.y + 1) * each); ++slot) {
+        const bool query = slot < a.heads, value = slot >= a.heads + a.kv_heads;
+        const int h = query ? slot : slot - a.heads - (value ? a.kv_heads : 0);
+        if (!query && place < 0) return;
+        const bsp_strides s = query ? a.xs : value ? a.vs : a.ks;
+        const E *src = (const E *)(query ? a.x : value ? a.v : a.k) + i * s.seq + h * s.head;
+        E *dst = query ? (E *)a.y + i * a.ys.seq + h * a.ys.head : (E *)(value ? a.values : a.keys) + place + h * a.c.head_stride;
+        const int64_t from = s.dim, to = query ? a.ys.dim : 1;
+        const float *norm = query ? a.x_norm : value ? nullptr : a.k_norm;
+        // a lane's pairs, and its dimensions that are passed on: all are read before any is written
+        const int pairs = value ? 0 : half, rest = 2 * pairs;
+        float x[2][2], z[4];
+        E whole[4];
+        float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int d = rest + lane + 64 * j;
-        whole[j] = d < D ? src[d * from] : (E)0;
-        z[j] = to_f32(whole[j]);
-        sum += z[j] * z[j];
-    }
-    float by = 1.f;
-    if (norm) {
-        for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
-        by = 1.f / sqrtf(sum / D + a.eps);
-    }
+        for (int j = 0; j < 2; ++j) {
+            const int p = lane + 64 * j, d0 = beside ? 2 * p : p, d1 = beside ? 2 * p + 1 : p + pairs;
+            x[j][0] = p < pairs ? to_f32(src[d0 * from]) : 0.f, x[j][1] = p < pairs ? to_f32(src[d1 * from]) : 0.f;
+            sum += x[j][0] * x[j][0] + x[j][1] * x[j][1];
+        }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int p = lane + 64 * j, d0 = beside ? 2 * p : p, d1 = beside ? 2 * p + 1 : p + pairs;
-        if (p >= pairs) break;
-        if (norm) x[j][0] *= by * norm[d0], x[j][1] *= by * norm[d1];
-        Turn t = turn(pos, a.freqs[p]);
-        t.cos *= a.rope.factor, t.sin *= a.rope.factor;
-        dst[d0 * to] = from_f32<E>(x[j][0] * t.cos - x[j][1] * t.sin);
-        dst[d1 * to] = from_f32<E>(x[j][1] * t.cos + x[j][0] * t.sin);
-    }
+        for (int j = 0; j < 4; ++j) {
+            const int d = rest + lane + 64 * j;
+            whole[j] = d < D ? src[d * from] : (E)0;
+            z[j] = to_f32(whole[j]);
+            sum += z[j] * z[j];
+        }
+        float by = 1.f;
+        if (norm) {
+            for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+            by = 1.f / sqrtf(sum / D + a.eps);
+        }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int d = rest + lane + 64 * j;
-        if (d < D) dst[d * to] = norm ? from_f32<E>(z[j] * (by * norm[d])) : whole[j];
+        for (int j = 0; j < 2; ++j) {
+            const int p = lane + 64 * j, d0 = beside ? 2 * p : p, d1 = beside ? 2 * p + 1 : p + pairs;
+            if (p >= pairs) break;
+            if (norm) x[j][0] *= by * norm[d0], x[j][1] *= by * norm[d1];
+            dst[d0 * to] = from_f32<E>(x[j][0] * r[j].cos - x[j][1] * r[j].sin);
+            dst[d1 * to] = from_f32<E>(x[j][1] * r[j].cos + x[j][0] * r[j].sin);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = rest + lane + 64 * j;
+            if (d < D) dst[d * to] = norm ? from_f32<E>(z[j] * (by * norm[d])) : whole[j];
+        }
+    }
+}
+
+// Any layout, many tokens: a workgroup has some tokens, whose cosines and sines it works out once, and some of their
+// heads, one after the other, through LDS: read and written along what lies side by side, worked on a token a lane.
+template <typename E, int MOST> __global__ __launch_bounds__(256) void k_rotary_tile(RotaryArgs a, int each) {
+    constexpr int T = MOST == 128 ? 64 : 32, PARTS = 256 / T, PAD = 4 / sizeof(E);   // rows of an odd number of banks
+    __shared__ E s_x[T][MOST + PAD];
+    __shared__ Turn s_turn[MOST / 2][T];
+    __shared__ float s_sum[PARTS][T];
+    __shared__ int64_t s_place[T];
+    const int D = a.head_dim, pairs = a.rope.dims / 2, t = threadIdx.x, lane = t % 64, wave = t / 64, token = t % T, part = t / T;
+    const int i0 = blockIdx.x * T, n = min(T, a.n - i0), slots = a.heads + 2 * a.kv_heads;
+    const bool beside = a.rope.layout == BSP_ROPE_INTERLEAVED;
+    for (int p = part; p < pairs; p += PARTS) {
+        const Turn r = turn(a.pos[i0 + min(token, n - 1)], a.freqs[p]);
+        s_turn[p][token] = {r.cos * a.rope.factor, r.sin * a.rope.factor};
+    }
+    if (a.kv_heads && t < n) {
+        const int i = i0 + t;
+        s_place[t] = place_of(a.c, a.table, a.rows ? a.rows[i] : i, a.seqs, a.width, a.pos[i]);
+    }
+    for (int slot = blockIdx.y * each; slot < min(slots, (int)(blockIdx.y + 1) * each); ++slot) {
+        const bool query = slot < a.heads, value = slot >= a.heads + a.kv_heads;
+        const int h = query ? slot : slot - a.heads - (value ? a.kv_heads : 0);
+        const bsp_strides xs = query ? a.xs : value ? a.vs : a.ks;
+        const E *src = (const E *)(query ? a.x : value ? a.v : a.k) + i0 * xs.seq + h * xs.head;
+        const float *norm = query ? a.x_norm : value ? nullptr : a.k_norm;
+        __syncthreads();   // the head before has been written; places
+        if (xs.dim == 1) {
+            for (int k = wave; k < n; k += 4)
+#pragma unroll
+                for (int j = 0; j < MOST / 64; ++j)
+                    if (lane + 64 * j < D) s_x[k][lane + 64 * j] = src[k * xs.seq + lane + 64 * j];
+        } else {
+            const E *from = src + min(token, n - 1) * xs.seq;
+#pragma unroll 8
+            for (int d = part; d < D; d += PARTS) s_x[token][d] = from[d * xs.dim];
+        }
+        __syncthreads();
+        if (norm) {
+            float sum = 0.f;
+#pragma unroll 4
+            for (int d = part; d < D; d += PARTS) {
+                const float x = to_f32(s_x[token][d]);
+                sum += x * x;
+            }
+            s_sum[part][token] = sum;
+            __syncthreads();
+        }
+        if (!value && token < n) {
+            float by = 1.f;
+            if (norm) {
+                float sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) sum += s_sum[k][token];
+                by = 1.f / sqrtf(sum / D + a.eps);
+            }
+#pragma unroll 4
+            for (int p = part; p < pairs; p += PARTS) {
+                const int d0 = beside ? 2 * p : p, d1 = beside ? d0 + 1 : p + pairs;
+                float x = to_f32(s_x[token][d0]), y = to_f32(s_x[token][d1]);
+                if (norm) x *= by * norm[d0], y *= by * norm[d1];
+                const Turn r = s_turn[p][token];
+                s_x[token][d0] = from_f32<E>(x * r.cos - y * r.sin), s_x[token][d1] = from_f32<E>(y * r.cos + x * r.sin);
+            }
+            if (norm)
+                for (int d = 2 * pairs + part; d < D; d += PARTS) s_x[token][d] = from_f32<E>(to_f32(s_x[token][d]) * (by * norm[d]));
+        }
+        __syncthreads();
+        if (!query || a.ys.dim == 1) {
+            E *to = query ? (E *)a.y + i0 * a.ys.seq + h * a.ys.head : (E *)(value ? a.values : a.keys) + h * a.c.head_stride;
+            for (int k = wave; k < n; k += 4) {
+                const int64_t at = query ? k * a.ys.seq : s_place[k];
+                if (!query && at < 0) continue;
+#pragma unroll
+                for (int j = 0; j < MOST / 64; ++j)
+                    if (lane + 64 * j < D) to[at + lane + 64 * j] = s_x[k][lane + 64 * j];
+            }
+        } else if (token < n) {
+            E *to = (E *)a.y + (i0 + token) * a.ys.seq + h * a.ys.head;
+#pragma unroll 8
+            for (int d = part; d < D; d += PARTS) to[d * a.ys.dim] = s_x[token][d];
+        }
     }
 }
 
@@ -211,14 +290,25 @@ bool in_vectors(const void *p, const bsp_strides &s, int esize) {
     return s.dim == 1 && (uintptr_t)p % 16 == 0 && s.seq * esize % 16 == 0 && s.head * esize % 16 == 0;
 }
 
+constexpr int kTile = 192, kWavesFew = 16384;
+
 template <typename E> hipError_t run(const RotaryArgs &a, hipStream_t st) {
     constexpr int VE = 16 / sizeof(E);
     const int slots = a.heads + 2 * a.kv_heads, esize = sizeof(E);
     const bool beside = a.rope.layout == BSP_ROPE_INTERLEAVED;
     const bool rows = a.head_dim % VE == 0 && a.rope.dims % (beside ? VE : 2 * VE) == 0 && in_vectors(a.x, a.xs, esize) &&
                       in_vectors(a.y, a.ys, esize) && (!a.kv_heads || (in_vectors(a.k, a.ks, esize) && in_vectors(a.v, a.vs, esize)));
+    if (!rows && (a.xs.dim == 1 || a.n < kTile)) {
+        const int each = (int)std::max<int64_t>(1, std::min<int64_t>(slots, (int64_t)a.n * slots / kWavesFew));
+        k_rotary<E><<<dim3(a.n, (slots + each - 1) / each), 64, 0, st>>>(a, each);
+        return hipGetLastError();
+    }
     if (!rows) {
-        k_rotary<E><<<dim3(a.n, slots), 64, 0, st>>>(a);
+        const bool wide = a.head_dim > 128;
+        const int tiles = (a.n + (wide ? 31 : 63)) / (wide ? 32 : 64), each = std::max(1, std::min(slots, (int)((int64_t)tiles * slots / 768)));
+        const dim3 grid(tiles, (slots + each - 1) / each);
+        if (wide) k_rotary_tile<E, 256><<<grid, 256, 0, st>>>(a, each);
+        else k_rotary_tile<E, 128><<<grid, 256, 0, st>>>(a, each);
         return hipGetLastError();
     }
     // A workgroup's groups of lanes go to up to 16 tokens, then to heads; few tokens leave each workgroup one head of a
