@@ -39,11 +39,12 @@ template <int DP> constexpr int kTaskWaves = DP == 256 ? 4 : 8;
 // ---- the workspace ---------------------------------------------------------------------------------
 
 // Columns c0 .. of key head j, from sequence `first` on, over tokens number from .. to of a list: number i is token
-// begin + i, and `skip` more from number `cut` on; those below `shared` are in the pages of row `lead`.
+// begin + i, and `skip` more from number `cut` on; those below `shared` are in the pages of row `lead`.  With `units` above 0
+// these are so many units of sequence `first` side by side, from number j on, a unit being up to 16 query heads of a key head.
 struct Task {
     int j, first, c0, columns, from, to;
     int row, lead, shared, begin, cut, skip;
-    int number, unused[3];   // among all tasks
+    int number, units, unused[2];   // number: among all tasks
 };
 struct Member {
     int task, blocks, pieces, place;   // the group's first task, column blocks, pieces; place in the group
@@ -51,7 +52,7 @@ struct Member {
 };
 struct Head {
     int tasks, shared;        // all, and of those the ones of what groups share, which come first
-    int next, unused;         // the next one to take
+    int next, bundle;         // the next one to take; log2 of the units in a task of what sequences have of their own
     int zero[4];
 };
 struct Parts {
@@ -69,8 +70,9 @@ struct Space {
 };
 // Of either kind there are as many tasks as units, which nothing cuts, and kRounds * kGrid more at most.
 struct Sizes {
-    int64_t shared_tasks, own_tasks, query_bytes;
+    int64_t shared_tasks, own_tasks, own_parts, query_bytes;
     int columns, own_columns;
+    int bundle_log2;   // units of a sequence's own in a task, at most
 };
 Sizes sizes_of(const CacheArgs &c, int batch, int heads, int groups) {
     const int64_t group = heads / c.kv_heads;
@@ -80,7 +82,12 @@ Sizes sizes_of(const CacheArgs &c, int batch, int heads, int groups) {
     s.own_columns = (int)std::min<int64_t>(16, group);
     s.query_bytes = (int64_t)batch * heads * dims_of(c.head_dim) * (c.dtype == BSP_F32 ? 4 : 2);
     s.shared_tasks = groups ? (batch * group / block + groups) * c.kv_heads + kRounds * kGrid : 0;
-    s.own_tasks = (int64_t)batch * c.kv_heads * ((group + 15) / 16) + kRounds * kGrid;
+    const int64_t per_seq = c.kv_heads * ((group + 15) / 16);
+    s.bundle_log2 = 0;
+    while (s.bundle_log2 < (c.head_dim > 128 ? 2 : 3) && 2 << s.bundle_log2 <= per_seq && batch * per_seq >> (s.bundle_log2 + 1) >= kGrid / 4)
+        ++s.bundle_log2;
+    s.own_tasks = batch * per_seq + kRounds * kGrid;
+    s.own_parts = batch * (per_seq + (1 << s.bundle_log2) - 1) + ((int64_t)kRounds * kGrid << s.bundle_log2);
     return s;
 }
 __host__ __device__ inline Space space_of(void *workspace, const Sizes &z, int batch, int head_dim) {
@@ -99,7 +106,7 @@ __host__ __device__ inline Space space_of(void *workspace, const Sizes &z, int b
     };
     s.head = (Head *)take(sizeof(Head)), s.q = take(z.query_bytes), s.member = (Member *)take((int64_t)batch * sizeof(Member));
     s.task = (Task *)take((kGrid + z.shared_tasks + z.own_tasks) * sizeof(Task));
-    s.shared = parts(z.shared_tasks, z.columns), s.own = parts(z.own_tasks, z.own_columns);
+    s.shared = parts(z.shared_tasks, z.columns), s.own = parts(z.own_parts, z.own_columns);
     s.bytes = at - (char *)workspace;
     return s;
 }
@@ -240,10 +247,16 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
         if (t % 64 == 0) s_sum[t / 64][which] = v;
     };
-    total_of(item[0].all + item[1].all, 0);
+    total_of(item[0].all, 0), total_of(item[1].all, 1), total_of((int64_t)item[1].units * item[1].cost, 2);
     __syncthreads();
-    int64_t total = 0;
-    for (int w = 0; w < W; ++w) total += s_sum[w][0];
+    int64_t of_groups_all = 0, own_all = 0, own_step = 0;
+    for (int w = 0; w < W; ++w) of_groups_all += s_sum[w][0], own_all += s_sum[w][1], own_step += s_sum[w][2];
+    const int64_t total = of_groups_all + own_all;
+    // Where what sequences have of their own is much of the work, and short, its tasks are chains of latencies: several units go
+    // in one, a part of the waves for each (32 sequences of 256 tokens after 4096 shared ones 44 -> 38 us, 64 of 16 tokens after
+    // 3000 64 -> 54; of 2000 tokens after 1 83 -> 90, of 128 tokens after 32768 153 -> 164).
+    const int bundle = own_all <= 2 * own_step && 2 * own_all >= of_groups_all ? z.bundle_log2 : 0;
+    if (bundle) item[1].units = (item[1].units + (1 << bundle) - 1) >> bundle, item[1].cost <<= bundle;
     // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks in all, in
     // rounds of the card, at the cost of the largest.
     auto pieces_of = [&](const Item &i, int64_t most) {
@@ -283,7 +296,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     if (t < B) s_task[G + t] = first_task[1], s_pieces[G + t] = n1, s_steps[G + t] = item[1].steps;
     if (t == 0) {
         s_task[G + B] = before;
-        space.head->shared = of_groups, space.head->tasks = before, space.head->next = min(before, kGrid);
+        space.head->shared = of_groups, space.head->tasks = before, space.head->next = min(before, kGrid), space.head->bundle = bundle;
         for (int i = 0; i < 4; ++i) space.head->zero[i] = 0;
     }
     __syncthreads();
@@ -307,13 +320,13 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         if (x < G) {   // by head, piece, block of columns: what is read together is worked on together
             const int all = (s_lo[x + 1] - s_lo[x]) * a.group, nb = (all + block_columns - 1) / block_columns;
             piece = in / nb % n, k.j = in / nb / n, k.first = s_lo[x], k.c0 = in % nb * block_columns;
-            k.columns = min(block_columns, all - k.c0);
+            k.columns = min(block_columns, all - k.c0), k.units = 0;
             k.row = k.lead = p.prefix_rows ? p.prefix_rows[x] : row_of(a, k.first);
             k.shared = 0, k.begin = s_from[x], k.cut = INT32_MAX, k.skip = 0, end = s_to[x] - s_from[x];
         } else {
             const int b = x - G;
-            piece = in % n, k.j = in / n / a.head_groups, k.first = b, k.c0 = in / n % a.head_groups * 16;
-            k.columns = min(16, a.group - k.c0);
+            piece = in % n, k.j = in / n << bundle, k.first = b, k.c0 = k.columns = 0;
+            k.units = min(1 << bundle, a.c.kv_heads * a.head_groups - k.j);
             k.row = s_own[b].row, k.lead = s_own[b].lead, k.shared = s_own[b].shared;
             k.begin = s_own[b].begin, k.cut = s_own[b].cut, k.skip = s_own[b].skip, end = s_own[b].len;
         }
@@ -372,24 +385,36 @@ __device__ __forceinline__ void stage_queries(const AttnArgs &a, const Task &k, 
     }
 }
 
+// Columns c0 .. of key head j, from sequence `first` on.
+struct Columns {
+    int j, first, c0, columns;
+};
+__device__ __forceinline__ Columns unit_of(const AttnArgs &a, const Task &k, int unit) {
+    if (!k.units) return {k.j, k.first, k.c0, k.columns};
+    const int u = k.j + min(unit, k.units - 1), j = u / a.head_groups, c0 = (u - j * a.head_groups) * 16;
+    return {j, k.first, c0, min(16, a.group - c0)};
+}
 // A column's query as it was laid out; past the columns that of the last.
-template <int DP, typename E> __device__ __forceinline__ const E *query_of(const AttnArgs &a, const Task &k, const E *laid, int c) {
+template <int DP, typename E> __device__ __forceinline__ const E *query_of(const AttnArgs &a, const Columns &k, const E *laid, int c) {
     const int at = k.c0 + min(c, k.columns - 1), s = at / a.group;
     return laid + ((int64_t)(k.first + s) * a.heads + k.j * a.group + at - s * a.group) * DP;
 }
 
-// N sixteens of columns over a task's tokens.  finish(column, d, output, reference, sum) takes what comes of
-// them, joined over the waves.
+// N sixteens of columns over a task's tokens, or 1 << bundle units of 16, each by a part of the waves.
+// finish(unit, column, d, output, reference, sum) takes what comes of them, joined over the waves.
 // `laid`: queries as lay_queries leaves them, or none.
 template <typename E, int DP, bool FULL, int N, int WAVES, typename F>
-__device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, N, WAVES> &sh, const Task &k, const E *laid, F finish) {
+__device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, N, WAVES> &sh, const Task &k, int bundle, const E *laid, F finish) {
     typedef Step<E, DP> St;
     constexpr int TOK = St::TOK, TT = TOK / 4, NT = TOK / 16, VW = St::VW, NV = St::NV, THREADS = 64 * WAVES;
     const int D = a.c.head_dim, wave = uni(threadIdx.x / 64);
     int lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));   // what goes by the lane is worked out again for each task, not held in registers
     const int r = lane % 16, quad = lane / 16;
-    const E *keys = (const E *)a.keys + k.j * a.c.head_stride, *values = (const E *)a.values + k.j * a.c.head_stride;
+    const int each = WAVES >> bundle, unit = wave / each, first = wave - unit * each;   // waves of a unit
+    const Columns mine = unit_of(a, k, unit);
+    const int j = uni(mine.j);
+    const E *keys = (const E *)a.keys + j * a.c.head_stride, *values = (const E *)a.values + j * a.c.head_stride;
     const Scale scale(a.scale);
 
     St st;
@@ -412,7 +437,7 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
             sh.place[t] = place_in(a, k, base + t);
         if (base == k.from && laid) {   // queries come while the places do
 #pragma unroll
-            for (int c = 0; c < N; ++c) St::load_q(q[c], query_of<DP>(a, k, laid, c * 16 + r), quad);
+            for (int c = 0; c < N; ++c) St::load_q(q[c], query_of<DP>(a, mine, laid, c * 16 + r), quad);
         } else if (base == k.from)
             stage_queries<E, 16 * N, DP, THREADS>(a, k, [&](int c, int d, E v) { sh.q[c][d] = v; });
         __syncthreads();
@@ -485,14 +510,14 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
             }
             st.template outputs<N>(s, acc);
         };
-        int s0 = wave * TOK;
-        if (s0 < padded) {
+        int s0 = first * TOK;
+        if (s0 < padded && (unit == 0 || unit < k.units)) {
             load_k(s0);
             load_v(s0);
             for (;;) {
 #pragma unroll
                 for (int c = 0; c < N; ++c) st.template scores<FULL>(q[c], s[c], D);
-                const int next = s0 + WAVES * TOK;
+                const int next = s0 + each * TOK;
                 if (next >= padded) break;
                 load_k(next);
                 softmax();
@@ -509,7 +534,7 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
         l[c] += __shfl_xor(l[c], 16);
         l[c] += __shfl_xor(l[c], 32);
         if (quad == 0) sh.m[wave][c * 16 + r] = m[c], sh.l[wave][c * 16 + r] = l[c];
-        if (c * 16 + r < k.columns)
+        if (c * 16 + r < mine.columns)
 #pragma unroll
             for (int h = 0; h < NV; ++h)
 #pragma unroll
@@ -520,19 +545,18 @@ __device__ __forceinline__ void columns_narrow(const AttnArgs &a, Narrow<E, DP, 
                             (f32x4){acc[c][h][v][i], acc[c][h][v + 1][i], acc[c][h][v + 2][i], acc[c][h][v + 3][i]};
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < k.columns * DP; i += THREADS) {
-        const int c = i / DP, d = i % DP;
-        if (d >= D) continue;
-        float top = sh.m[0][c], sum = 0.f, o = 0.f;
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh.m[w][c]);
+    const int columns = k.units ? k.units * 16 : k.columns;
+    for (int i = threadIdx.x; i < columns * DP; i += THREADS) {
+        const int of = k.units ? i / (16 * DP) : 0, c = i / DP - of * 16, d = i % DP;
+        if (d >= D || c >= unit_of(a, k, of).columns) continue;
+        float top = -INFINITY, sum = 0.f, o = 0.f;
+        for (int w = of * each; w < (of + 1) * each; ++w) top = fmaxf(top, sh.m[w][c]);
         const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
+        for (int w = of * each; w < (of + 1) * each; ++w) {
             const float f = __builtin_amdgcn_exp2f(sh.m[w][c] - ref);
             sum += sh.l[w][c] * f, o += sh.o[w][c][d] * f;
         }
-        finish(c, d, o, top, sum);
+        finish(of, c, d, o, top, sum);
     }
     __syncthreads();   // the next task writes these arrays
 }
@@ -631,7 +655,7 @@ __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, co
     for (int n = 0; n < 2; ++n) {
         const int c = c_wave + n * 16 + r;
 #pragma unroll
-        for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)(query_of<DP>(a, k, laid, c) + i * 32 + quad * 8);
+        for (int i = 0; i < NC; ++i) q[n][i] = *(const u32x4 *)(query_of<DP>(a, {k.j, k.first, k.c0, k.columns}, laid, c) + i * 32 + quad * 8);
         m[n] = -INFINITY, ref[n] = l[n] = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[n][d] = (f32x4){0, 0, 0, 0};
@@ -825,7 +849,7 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
     __shared__ Shared<E, DP> sh;
     const AttnArgs &a = p.a;
     const Space space = space_of(a.workspace, z, a.batch, a.c.head_dim);
-    const int tasks = uni(space.head->tasks), shared = uni(space.head->shared);
+    const int tasks = uni(space.head->tasks), shared = uni(space.head->shared), bundle = uni(space.head->bundle);
     const E *laid = (const E *)space.q;
     int slot = blockIdx.x;   // of the task; later ones have their own number's
     for (;;) {
@@ -833,21 +857,21 @@ __global__ __launch_bounds__(64 * kTaskWaves<DP>, kTaskWaves<DP> / 4) void k_pre
         Task k;
         k.j = uni(at->j), k.first = uni(at->first), k.c0 = uni(at->c0), k.columns = uni(at->columns), k.from = uni(at->from);
         k.to = uni(at->to), k.row = uni(at->row), k.lead = uni(at->lead), k.shared = uni(at->shared), k.begin = uni(at->begin);
-        k.cut = uni(at->cut), k.skip = uni(at->skip), k.number = uni(at->number);
+        k.cut = uni(at->cut), k.skip = uni(at->skip), k.number = uni(at->number), k.units = uni(at->units);
         if (k.number < 0) return;
         if (tasks > kGrid && threadIdx.x == 0) sh.next = atomicAdd(&space.head->next, 1);
         const bool common = k.number < shared;
         const Parts parts = common ? space.shared : space.own;
         const int64_t number = common ? k.number : k.number - shared;
-        auto finish = [&](int c, int d, float o, float m, float l) {
-            const int64_t i = parts.at(number, c);
+        auto finish = [&](int unit, int c, int d, float o, float m, float l) {
+            const int64_t i = parts.at(common ? number : (number << bundle) + unit, c);
             parts.o[i * a.c.head_dim + d] = o;
             if (d == 0) parts.m[i] = m, parts.l[i] = l;
         };
-        if (k.columns <= 16) {
-            columns_narrow<E, DP, FULL, 1, kTaskWaves<DP>>(a, sh.one, k, laid, finish);
+        if (k.columns <= 16) {   // or units
+            columns_narrow<E, DP, FULL, 1, kTaskWaves<DP>>(a, sh.one, k, k.units ? bundle : 0, laid, finish);
         } else if (k.columns <= 32 || !Shared<E, DP>::WIDE) {
-            columns_narrow<E, DP, FULL, 2, kTaskWaves<DP>>(a, sh.two, k, laid, finish);
+            columns_narrow<E, DP, FULL, 2, kTaskWaves<DP>>(a, sh.two, k, 0, laid, finish);
         } else if constexpr (Shared<E, DP>::WIDE) {
             const void *zero = space.head->zero;
             if (k.columns <= 64)
@@ -877,12 +901,13 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
     const Space space = space_of(a.workspace, z, a.batch, D);
     const Member me = space.member[b];
     const int column = me.place * a.group + hh, block = column / block_columns;
-    const int n = me.pieces + me.own_pieces;
+    const int n = me.pieces + me.own_pieces, unit = j * a.head_groups + hh / 16, bundle = space.head->bundle;
     auto at = [&](int k, Parts *parts) {
         const bool common = k < me.pieces;
         *parts = common ? space.shared : space.own;
         return common ? space.shared.at(me.task + (int64_t)(j * me.pieces + k) * me.blocks + block, column - block * block_columns)
-                      : space.own.at(me.own_task + (int64_t)(j * a.head_groups + hh / 16) * me.own_pieces + k - me.pieces, hh % 16);
+                      : space.own.at(((me.own_task + (int64_t)(unit >> bundle) * me.own_pieces + k - me.pieces) << bundle)
+                                         + (unit & ((1 << bundle) - 1)), hh % 16);
     };
     auto finite = [](float top) { return top == -INFINITY ? 0.f : top; };   // what is taken off: -Inf - -Inf is none
     float top = -INFINITY, sum = 0.f;
@@ -933,7 +958,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
     Task k;
     k.row = uni(row_of(a, b)), k.j = u / a.head_groups, k.first = b, k.c0 = (u - k.j * a.head_groups) * 16;
     k.columns = min(16, a.group - k.c0);
-    k.begin = k.from = 0, k.to = uni(len_of(a, k.row)), k.cut = INT32_MAX, k.skip = 0, k.shared = 0, k.lead = -1;
+    k.units = 0, k.begin = k.from = 0, k.to = uni(len_of(a, k.row)), k.cut = INT32_MAX, k.skip = 0, k.shared = 0, k.lead = -1;
     if (a.window && k.to > a.window) k.begin = k.to - a.window, k.to = a.window;
     for (int g0 = 0; g0 < p.groups; g0 += 64) {
         const int g = g0 + lane;
@@ -953,7 +978,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
         }
         return;
     }
-    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, (const E *)nullptr, [&](int c, int d, float o, float m, float l) {
+    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, 0, (const E *)nullptr, [&](int, int c, int d, float o, float m, float l) {
         const int h = k.j * a.group + k.c0 + c;
         ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
         if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;
@@ -962,7 +987,10 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
 
 // Sequences of few tokens take one kernel, in which each reads what it shares by itself.
 constexpr int64_t kShort = 1024;
-bool is_short(int64_t tokens) { return tokens <= kShort; }
+bool is_short(const CacheArgs &c, int batch, int heads, int64_t tokens) {
+    const int64_t units = (int64_t)batch * c.kv_heads * ((heads / c.kv_heads + 15) / 16);
+    return tokens <= (units >= 128 ? 2 : 1) * kShort;
+}
 
 template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, bool few, hipStream_t st) {
     const AttnArgs &a = p.a;
@@ -992,7 +1020,7 @@ template <typename E> hipError_t run(const PrefixArgs &p, bool few, hipStream_t 
 
 // A window may make a call short: the workspace goes by the table alone.
 int64_t prefix_workspace(const CacheArgs &c, int batch, int heads, int groups, int width) {
-    if (is_short((int64_t)width * c.page_size)) return 0;
+    if (is_short(c, batch, heads, (int64_t)width * c.page_size)) return 0;
     return space_of(nullptr, sizes_of(c, batch, heads, groups), batch, c.head_dim).bytes;
 }
 
@@ -1002,7 +1030,8 @@ hipError_t launch_prefix(const PrefixArgs &args, hipStream_t st) {
     a.head_groups = (a.group + 15) / 16, a.shares = 0;
     int64_t tokens = (int64_t)a.width * a.c.page_size;
     if (a.window) tokens = std::min<int64_t>(tokens, a.window);
-    return a.c.dtype == BSP_F32 ? run<float>(p, is_short(tokens), st) : run<uint16_t>(p, is_short(tokens), st);
+    const bool few = is_short(a.c, a.batch, a.heads, tokens);
+    return a.c.dtype == BSP_F32 ? run<float>(p, few, st) : run<uint16_t>(p, few, st);
 }
 
 }  // namespace bsp

@@ -22,7 +22,7 @@ def B():
 @pytest.fixture(autouse=True, params=["short", "long"])
 def table_width(request):
     """Tables that hold no more than the sequences need, and those that could hold long ones."""
-    Setup.least = 0 if request.param == "short" else 1100
+    Setup.least = 0 if request.param == "short" else 2100
     yield
     Setup.least = 0
 
@@ -286,6 +286,68 @@ def test_column_blocks(B, dim, dt):
     s = Setup(B, sizes, shared, [rng.integers(0, 150, m) for m in sizes], 1, 4, dim, 16, dt, "slots" if dim == 72 else "heads", seed=dim, holes=0.02)
     s.check(*s.run(dim ** -0.5), dim ** -0.5)
     s.check(*s.run(dim ** -0.5, feature_major=True, window=1500), dim ** -0.5, 1500)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("kv,heads,dim,members", [(3, 6, 64, 60), (8, 8, 64, 40), (5, 100, 40, 30), (6, 18, 128, 70), (8, 16, 136, 20)])
+def test_short_ends_of_many_sequences(B, kv, heads, dim, members, dt):
+    """Several key heads of a sequence's own tokens are worked on together, not always as many as there is room for."""
+    rng = np.random.default_rng(kv)
+    own = [rng.integers(0, 200, members), rng.integers(-50, 300, 3)]
+    s = Setup(B, [members, 3], [130, 60], own, kv, heads, dim, 16, dt, seed=kv, extra=2)
+    s.check(*s.run(dim ** -0.5), dim ** -0.5)
+
+
+@pytest.mark.parametrize("dt,page,order,batch,kv,heads,dim,longest", [
+    ("bf16", 64, "heads", 64, 8, 64, 128, 12000), ("bf16", 16, "slots", 40, 8, 32, 64, 9000), ("bf16", 7, "heads", 33, 4, 16, 96, 6000),
+    ("f32", 16, "heads", 24, 8, 32, 128, 4000), ("bf16", 64, "heads", 12, 4, 16, 256, 5000)])
+def test_as_attention_over_long_prefixes(B, dt, page, order, batch, kv, heads, dim, longest):
+    """Tasks over several tiles of tokens, against attention that shares nothing (which has tests of its own)."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(batch)
+    tdt = torch.bfloat16 if dt == "bf16" else torch.float32
+    groups = 3
+    starts = [0, batch // 2, batch // 2 + 1, batch]
+    whole = [longest // page, longest // (3 * page), longest // (2 * page)]   # shared pages
+    own = torch.randint(0, 40, (batch,), generator=torch.Generator().manual_seed(1)).tolist()
+    rows, used = [], 0
+    for g in range(groups):
+        first = list(range(used, used + whole[g]))
+        used += whole[g]
+        for b in range(starts[g], starts[g + 1]):
+            n = M.ceil(own[b], page)
+            rows.append(first + list(range(used, used + n)))
+            used += n
+    lens = [whole[g] * page + own[b] for g in range(groups) for b in range(starts[g], starts[g + 1])]
+    width = max(map(len, rows)) + 1
+    ids = torch.randperm(used + 1, generator=gen, device="cuda").to(torch.int32)
+    table = torch.full((batch, width), -1, dtype=torch.int32, device="cuda")
+    for b, r in enumerate(rows):
+        table[b, :len(r)] = ids[torch.tensor(r, device="cuda", dtype=torch.long)]
+    inner = (kv, page) if order == "heads" else (page, kv)
+    data = [torch.randn(used + 1, *inner, dim, generator=gen, device="cuda").to(tdt) for _ in range(2)]
+    cache = B.CacheShape.of(data[0], B.HEAD_MAJOR if order == "heads" else B.SLOT_MAJOR)
+    q = torch.randn(batch, heads, dim, generator=gen, device="cuda").to(tdt)
+
+    def ints(a):
+        return torch.tensor(a, dtype=torch.int32, device="cuda")
+    y, z = torch.empty_like(q), torch.empty_like(q)
+    lse, lse2 = (torch.empty(batch, heads, device="cuda") for _ in range(2))
+    ws = torch.full((B.bsp_attention_prefix_workspace(cache, batch, heads, groups, width) + 16,), 0xff, dtype=torch.uint8, device="cuda")
+    ws2 = torch.empty(B.bsp_attention_workspace(cache, batch, heads, width) + 16, dtype=torch.uint8, device="cuda")
+    for window in (0, longest - 100):
+        for scale in (dim ** -0.5, 0.5):
+            B.bsp_attention_prefix(cache, q, *data, table, ints(lens), ints(starts), ints([n * page for n in whole]), y, scale, window,
+                                   None, None, lse, ws)
+            B.bsp_attention(cache, q, *data, table, ints(lens), z, scale, window, None, lse2, ws2)
+            torch.cuda.synchronize()
+            # Each within its bounds of the same values: the output's rounding; scores of up to some 4 sqrt(dim) units, whose 2 (dim + 4)
+            # roundings the exponential passes on; and the sums' own, over up to 12000 tokens.
+            u = 2.0 ** -8 if dt == "bf16" else S.U24
+            score = 2 * (dim + 4) * S.U24 * scale * dim
+            size = (2 * score + (2 * longest + 64) * S.U24 + (2.0 ** -15 if dt == "bf16" else 0)) * 5
+            assert ((y.double() - z.double()).abs() <= 2 * u * z.double().abs() + 2 * size).all()
+            assert ((lse.double() - lse2.double()).abs() <= 2 * (score + (longest + 64) * S.U24) + 8 * S.U24 * lse.double().abs()).all()
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
