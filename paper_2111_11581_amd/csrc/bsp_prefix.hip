@@ -68,7 +68,8 @@ struct Space {
     Parts shared, own;
     int64_t bytes;
 };
-// Of either kind there are as many tasks as units, which nothing cuts, and kRounds * kGrid more at most.
+// Of either kind there are as many tasks as units, which nothing cuts, and kRounds * kGrid more at most: a unit's pieces are
+// one more than its cost over the cost of all over kRounds * kGrid, rounded down.
 struct Sizes {
     int64_t shared_tasks, own_tasks, own_parts, query_bytes;
     int columns, own_columns;
@@ -145,10 +146,8 @@ template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wa
     return v;
 }
 
-// A workgroup, a thread for a group and for a sequence: as many waves as these need, since each wave makes every
-// scan and sum longer.  Bound by latency.
-// The other workgroups lay the queries out meanwhile, so that a task reads its operands as they lie: eight dimensions a
-// thread, along the sequences where these lie side by side.
+// Queries as a task's lanes read them, 16 bytes a thread, along the sequences where these lie side by side.  Staged by each
+// task instead, k_prefix takes 39 us for 32 sequences over 4096 tokens, and 31 so.
 template <typename E, int DP> __device__ __forceinline__ void lay_queries(const AttnArgs &a, E *to, int64_t i) {
     constexpr int VE = 16 / sizeof(E), N = DP / VE;
     const int rows = a.batch * a.heads;
@@ -166,6 +165,8 @@ template <typename E, int DP> __device__ __forceinline__ void lay_queries(const 
     *(u32x4 *)(to + ((int64_t)b * a.heads + h) * DP + d0) = *(const u32x4 *)v;
 }
 
+// Block 0 plans, a thread for a group and for a sequence: as many waves as these need, since each wave makes every
+// scan and sum longer.  The other blocks lay the queries out meanwhile.  Bound by latency: 8 us for 32 sequences.
 template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
     if (blockIdx.x > 0) {
         const Space space = space_of(p.a.workspace, z, p.a.batch, p.a.c.head_dim);
@@ -251,12 +252,14 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     __syncthreads();
     int64_t of_groups_all = 0, own_all = 0, own_step = 0;
     for (int w = 0; w < W; ++w) of_groups_all += s_sum[w][0], own_all += s_sum[w][1], own_step += s_sum[w][2];
-    const int64_t total = of_groups_all + own_all;
     // Where what sequences have of their own is much of the work, and short, its tasks are chains of latencies: several units go
     // in one, a part of the waves for each (32 sequences of 256 tokens after 4096 shared ones 44 -> 38 us, 64 of 16 tokens after
     // 3000 64 -> 54; of 2000 tokens after 1 83 -> 90, of 128 tokens after 32768 153 -> 164).
     const int bundle = own_all <= 2 * own_step && 2 * own_all >= of_groups_all ? z.bundle_log2 : 0;
     if (bundle) item[1].units = (item[1].units + (1 << bundle) - 1) >> bundle, item[1].cost <<= bundle;
+    // A last task of fewer units is taken for a whole one, here as in its pieces, whose number goes by this total.
+    const int64_t per_seq = (int64_t)a.c.kv_heads * a.head_groups;
+    const int64_t total = of_groups_all + own_all / per_seq * ((per_seq + (1 << bundle) - 1) >> bundle << bundle);
     // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks in all, in
     // rounds of the card, at the cost of the largest.
     auto pieces_of = [&](const Item &i, int64_t most) {

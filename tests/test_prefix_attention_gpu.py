@@ -470,3 +470,19 @@ def test_an_offset_past_32_bits(B):
     back = {int(p): i for i, p in enumerate(to)}
     s.table = np.array([[back.get(int(e), -1) for e in row] for row in s.table])
     s.check(y, lse, 0.088)
+
+
+def test_units_that_do_not_fill_their_tasks(B):
+    """Nine key heads go eight to a task, and most tasks in two pieces: no more than the workspace has room for."""
+    import torch
+    n = 257
+    s = Setup(B, [1] * n, [1] * (n - 1) + [3200], [[200]] * n, 9, 9, 8, 16, seed=11)
+    need = B.bsp_attention_prefix_workspace(s.cache, n, 9, n, s.width)
+    ws = torch.full((need + 4096,), 0xff, dtype=torch.uint8, device="cuda")
+    q, y = torch.from_numpy(s.q).to(s.tdt).cuda(), torch.full(s.q.shape, float("nan"), dtype=s.tdt, device="cuda")
+    out = torch.empty(n, 9, device="cuda")
+    B.bsp_attention_prefix(s.cache, q, *s.data, s.ints(s.table), s.ints(s.lens), s.ints(s.starts), s.ints(s.shared), y, 0.35, 0, None, None,
+                           out, ws[:need])
+    torch.cuda.synchronize()
+    s.check(y, out, 0.35)
+    assert bool((ws[need:] == 0xff).all())
