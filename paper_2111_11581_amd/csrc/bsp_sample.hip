@@ -5,11 +5,14 @@
 // counting and by adding up whole numbers, which has no order that could show: tokens fall into bins by
 // their logit's distance from the largest, and the bin in which a cut falls is cut further by the bits of
 // its keys.
-//  * Rows of up to 32768 tokens stay in the LDS of a workgroup (k_sample_row).
+//  * Rows of up to 32768 tokens stay in the LDS of a workgroup (k_sample_row), where each step waits for the one
+//    before: one row of 4000 tokens takes 7.4 us without a cut and 19.6 with three, 64 rows 23.4, 64 rows of 30000 41.
 //  * Of longer ones k_sample_scan finds the largest logits, k_sample_bins fills the bins of each chunk, and in
 //    k_sample_pick a workgroup a row finds cuts and token; it reads again the tokens of the bins where the cuts
 //    are, and one chunk.
-//  * Rows whose elements lie apart are laid out by k_sample_scan.
+//  * Rows whose elements lie apart are laid out by k_sample_lay.
+// 64 rows of 131072 tokens, three cuts, 33.5 MB: 20 us laid out (67 MB), 25 for the bins (fp64 weights of 8.4 million
+// tokens; 19 without cuts), 28 for cuts and tokens (a chain of latencies, the more the more cuts: 13 without).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -25,10 +28,16 @@ constexpr double kOne = 8796093022208.0;   // 2^43: what a weight of 1 counts; 2
 constexpr int kBins = 512, kSpan = 32;    // bins, and the distance that they cover: e^-32 is below 2^-44
 constexpr int kScan = 2048, kLay = 256;    // tokens whose largest logit k_sample_scan and k_sample_lay find
 constexpr int kChunk = 8192;               // tokens whose bins k_sample_bins fills
-constexpr int kRow = 32768;                // tokens that a workgroup holds in LDS
-constexpr int kQuick = 128;                // tokens of a bin that are compared with each other
+// Tokens that a workgroup holds in LDS.  Chunks would give more workgroups to few rows, but in three kernels: 12000 tokens
+// 26.2 us and in chunks 36.7, 16 rows of them 29.0 and 39.5, 30000 tokens 34.5 and 37.8, 64 rows of them 40.9 and 43.7.
+constexpr int kRow = 32768;
+// Tokens of a bin that are compared with each other, two a thread for a count of 128 * 128; 32 take the same time at
+// every size tried.
+constexpr int kQuick = 128;
 constexpr int kList = 4096;                // tokens of a bin that k_sample_pick holds in LDS
-constexpr int kFirst = 512;                // tokens of a chunk's first bins that k_sample_bins lists
+// Tokens of a chunk's first bins that k_sample_bins lists: enough for most cuts, which are among the likeliest tokens
+// (64 rows of 131072 tokens 73.1 us, with 512 76.1).
+constexpr int kFirst = 256;
 
 // Logits as numbers that are in the same order; NaN and -Inf, which are never taken, are 0.
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -757,7 +766,10 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
 }
 
 template <typename E, bool ALONG> hipError_t run_row(const SampleArgs &a, hipStream_t st) {
-    if (a.vocab <= 4096) k_sample_row<E, ALONG, 256, 4096><<<a.batch, 256, 0, st>>>(a);
+    // As many threads as keep each busy: 4000 tokens take 19.6 us with 512 and 23.8 with 256 threads, 1000 tokens 9.7 with
+    // 256 and 11.8 with 128 (and three cuts of 200 tokens 14.1 and 13.8); 8000 tokens 23.9 with 512 and 24.9 with 1024.
+    if (a.vocab <= 1024) k_sample_row<E, ALONG, 256, 1024><<<a.batch, 256, 0, st>>>(a);
+    else if (a.vocab <= 8192) k_sample_row<E, ALONG, 512, 8192><<<a.batch, 512, 0, st>>>(a);
     else k_sample_row<E, ALONG, 1024, kRow><<<a.batch, 1024, 0, st>>>(a);
     return hipGetLastError();
 }
@@ -768,7 +780,9 @@ template <typename E> hipError_t run_long(const SampleArgs &a, const Space &sp, 
     return hipGetLastError();
 }
 
-// Rows whose elements lie apart are read as they lie up to so many tokens: each element is a line of its own.
+// Rows whose elements lie apart are read as they lie up to so many tokens, each element a line of its own: 16 rows of 4000
+// tokens 27.7 us and laid out first 33.4, 64 rows 28.2 and 33.9; 64 rows of 8000 34.7 laid out and 35.5, of 30000 51
+// and 71.
 constexpr int kApart = 4096;
 
 template <typename E> hipError_t run(SampleArgs a, hipStream_t st) {
