@@ -53,16 +53,25 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
 
 typedef __attribute__((ext_vector_type(4))) uint16_t u16x4;
 
+// What a row is sampled with, read before anything waits.
+struct Setting {
+    float t, top_p, min_p, u;
+    int top_k;
+    __device__ __forceinline__ Setting(const SampleArgs &a, int b) {
+        t = a.temperature ? a.temperature[b] : 1.f, top_k = a.top_k ? a.top_k[b] : 0;
+        top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f, u = a.u[b];
+    }
+};
+
 struct Row {
     uint32_t top_key;
-    float top;           // the largest logit
+    float top, t;        // the largest logit, the temperature
     double steps;        // 64 / (temperature ln 2)
     float bins;          // of a distance of 1
     bool greedy;
     const double *powers;   // 2^(i / 64)
 
-    __device__ __forceinline__ Row(const SampleArgs &a, int b, uint32_t key, const double *p) : top_key(key), powers(p) {
-        const float t = a.temperature ? a.temperature[b] : 1.f;
+    __device__ __forceinline__ Row(float temperature, uint32_t key, const double *p) : top_key(key), t(temperature), powers(p) {
         greedy = !(t > 0.f);
         top = logit_of(key), steps = 92.332482616893656877 / t, bins = (float)((double)(kBins / kSpan) / t);
     }
@@ -209,6 +218,17 @@ template <typename P> __device__ __forceinline__ uint32_t first_key(uint32_t lo,
     return hi;
 }
 
+// The first key whose weight is at least min_p: beside where its logarithm says, or else wherever it is.
+__device__ __forceinline__ uint32_t least_key(const Row &row, float min_p) {
+    auto holds = [&](uint32_t k) { return row.reaches(k, min_p); };
+    const uint32_t guess = min(key_of((float)((double)row.top + log((double)min_p) * (double)row.t)), row.top_key);
+    const uint32_t lo = guess > kLeast + 32 ? guess - 32 : kLeast;
+    const uint64_t hit = __ballot(holds(min(lo + threadIdx.x % 64, row.top_key)));
+    const int first = hit ? __ffsll((unsigned long long)hit) - 1 : 64;
+    if (first == 0 && lo > kLeast) return first_key(kLeast, lo, holds);
+    return first < 64 ? min(lo + first, row.top_key) : first_key(lo + 64, row.top_key, holds);
+}
+
 // What is kept of a row: tokens whose key is above, and of those that have it the ones up to an index.
 struct Kept {
     uint32_t key, index;
@@ -275,34 +295,31 @@ __device__ __forceinline__ void cut_bin(Scratch<THREADS> &s, const Row &row, Fou
 // The cuts of a row of `live` tokens, whose bins hold their numbers; fill_mass(kept) adds their mass for what is kept, and
 // returns all of it.
 template <int THREADS, typename R, typename T, typename M>
-__device__ __forceinline__ Kept cut(const SampleArgs &a, int b, Scratch<THREADS> &s, const Row &row, uint64_t live, R prepare, T each_token,
+__device__ __forceinline__ Kept cut(const Setting &set, Scratch<THREADS> &s, const Row &row, uint64_t live, R prepare, T each_token,
                                     M fill_mass) {
-    const int top_k = a.top_k ? a.top_k[b] : 0;
-    const float top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
-    const bool by_k = top_k > 0 && (uint64_t)top_k < live, by_p = top_p < 1.f;
+    const bool by_k = set.top_k > 0 && (uint64_t)set.top_k < live, by_p = set.top_p < 1.f;
     Kept kept = {kLeast, 0xffffffffu};
     Found in;
     if (by_k) {
-        in = locate(s, 0, false, (uint64_t)top_k);
-        cut_bin(s, row, &in, false, top_k - in.count_before, prepare, each_token, &kept);
+        in = locate(s, 0, false, (uint64_t)set.top_k);
+        cut_bin(s, row, &in, false, set.top_k - in.count_before, prepare, each_token, &kept);
     }
     if (by_p) {
         const uint64_t all = fill_mass(kept, by_k, in);
-        const uint64_t target = max((uint64_t)1, (uint64_t)ceil(fmax((double)top_p, 0.0) * (double)all));
+        const uint64_t target = max((uint64_t)1, (uint64_t)ceil(fmax((double)set.top_p, 0.0) * (double)all));
         in = locate(s, 0, true, target);   // at most the bin of the first cut, of which not all is kept
         cut_bin(s, row, &in, true, target - in.mass_before, prepare, each_token, &kept);
     }
-    if (min_p > 0.f) {
-        const uint32_t least = first_key(kLeast, row.top_key, [&](uint32_t k) { return row.reaches(k, min_p); });
+    if (set.min_p > 0.f) {
+        const uint32_t least = least_key(row, set.min_p);
         if (least > kept.key) kept = {least, 0xffffffffu};
     }
     return kept;
 }
 
 // Where among a sum the token is.
-__device__ __forceinline__ uint64_t place_of(const SampleArgs &a, int b, uint64_t total) {
-    const float u = fminf(fmaxf(a.u[b], 0.f), 0x1.fffffep-1f);
-    return (uint64_t)((double)u * (double)total);   // the sum has to be more
+__device__ __forceinline__ uint64_t place_of(float u, uint64_t total) {
+    return (uint64_t)((double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f) * (double)total);   // the sum has to be more
 }
 __device__ __forceinline__ void put(const SampleArgs &a, int b, int token, uint64_t mass, uint64_t total) {
     a.tokens[b] = token;
@@ -348,6 +365,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
     __shared__ uint64_t s_sum[MOST / (4 * THREADS) * WAVES];
     const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
     const Source<E, ALONG> src(a.logits, b, a.row_stride, a.token_stride, a.vocab);
+    const Setting set(a, b);
     const int fours = (a.vocab + 3) / 4, rounds = (fours + THREADS - 1) / THREADS;
     uint32_t top = 0;
 #pragma unroll 4
@@ -363,7 +381,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
         if (t == 0) put(a, b, -1, 0, 0);
         return;
     }
-    const Row row(a, b, top, s.powers);
+    const Row row(set.t, top, s.powers);
     auto each_token = [&](auto f) {   // of the thread's own
 #pragma unroll 1
         for (int i = t; i < fours; i += THREADS) {
@@ -381,7 +399,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
     }
     Kept kept = {kLeast, 0xffffffffu};
     if (a.top_k || a.top_p || a.min_p) {
-        const bool by_count = a.top_k && a.top_k[b] > 0;
+        const bool by_count = set.top_k > 0;
         clear(s, 0);
         __syncthreads();
         uint64_t live = 0, all = 0;
@@ -394,7 +412,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
             __syncthreads();
             live = s.found[0];
         }
-        kept = cut(a, b, s, row, live, [](int, uint64_t) {}, each_token, [&](const Kept &k0, bool, const Found &) {
+        kept = cut(set, s, row, live, [](int, uint64_t) {}, each_token, [&](const Kept &k0, bool, const Found &) {
             if (by_count) clear(s, 0);   // bins of what is kept alone
             __syncthreads();
             uint64_t all = 0, none = 0;
@@ -427,7 +445,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
     uint64_t total = 0;
     for (int i = lane; i < sums; i += 64) total += s_sum[i];
     for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-    const uint64_t target = place_of(a, b, total);
+    const uint64_t target = place_of(set.u, total);
     uint64_t before = 0;
     int at = 0;
     for (int i0 = 0; i0 < sums; i0 += 64) {
@@ -555,6 +573,7 @@ template <typename E> __global__ __launch_bounds__(512) void k_sample_bins(Sampl
     __shared__ Scratch<T> s;
     const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
     const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    const Setting set(a, b);
     uint32_t key[Q][4];
 #pragma unroll
     for (int q = 0; q < Q; ++q) src.four(c * kChunk + 4 * (q * T + t), key[q]);
@@ -562,7 +581,7 @@ template <typename E> __global__ __launch_bounds__(512) void k_sample_bins(Sampl
     clear(s, 0);
     if (t == 0) s.listed = 0;
     const uint32_t top = top_of<T>(sp, b, s.key);
-    const Row row(a, b, top, s.powers);
+    const Row row(set.t, top, s.powers);
     if (top == 0 || row.greedy) return;
     __syncthreads();
 #pragma unroll
@@ -610,13 +629,30 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     __shared__ uint64_t s_chunk[MOST];
     const int b = blockIdx.x, t = threadIdx.x, lane = t % 64, wave = t / 64;
     const Source<E, true> src(a.logits, b, a.row_stride, 1, a.vocab);
+    const Setting set(a, b);
+    const bool cut_at_all = a.top_k || a.top_p || a.min_p;
+    const uint32_t *counts = sp.count + (int64_t)b * sp.chunks * kBins;
+    const uint64_t *masses = sp.mass + (int64_t)b * sp.chunks * kBins;
+    auto read_list = [&](int c, uint2 (&v)[kFirst / 64]) {   // past its end whatever is there
+#pragma unroll
+        for (int i = 0; i < kFirst / 64; ++i) v[i] = sp.token[((int64_t)b * sp.chunks + c) * kFirst + 64 * i + lane];
+    };
+    static_assert(WAVES * kFirst <= kList, "");
+    bool held = cut_at_all && sp.chunks <= WAVES;   // all lists in LDS, read before anything waits
+    if (held && wave < sp.chunks) {
+        uint2 v[kFirst / 64];
+        read_list(wave, v);
+#pragma unroll
+        for (int i = 0; i < kFirst / 64; ++i)
+            s_key[wave * kFirst + 64 * i + lane] = v[i].x, s_index[wave * kFirst + 64 * i + lane] = (int)v[i].y;
+    }
     start(s);
     const uint32_t top = top_of<T>(sp, b, s.key);
     if (top == 0) {
         if (t == 0) put(a, b, -1, 0, 0);
         return;
     }
-    const Row row(a, b, top, s.powers);
+    const Row row(set.t, top, s.powers);
     if (row.greedy) {   // in the first stretch that has it
         uint32_t from_end = 0;
         for (int i = t; i < sp.scans; i += T)
@@ -629,15 +665,17 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
         if (t == 0) put(a, b, first + sp.scan - from_end, 1, 1);
         return;
     }
-    const uint32_t *counts = sp.count + (int64_t)b * sp.chunks * kBins;
-    const uint64_t *masses = sp.mass + (int64_t)b * sp.chunks * kBins;
     uint64_t live = 0, all = 0;
+    static_assert(T == 2 * kBins, "");
     if (t < kBins) {
 #pragma unroll 8
-        for (int c = 0; c < sp.chunks; ++c) live += counts[c * kBins + t], all += masses[c * kBins + t];
-        s.count[0][t] = (uint32_t)live, s.mass[0][t] = all;
+        for (int c = 0; c < sp.chunks; ++c) live += counts[c * kBins + t];
+        s.count[0][t] = (uint32_t)live;
+    } else {
+#pragma unroll 8
+        for (int c = 0; c < sp.chunks; ++c) all += masses[c * kBins + t - kBins];
+        s.mass[0][t - kBins] = all;
     }
-    const bool cut_at_all = a.top_k || a.top_p || a.min_p;
     if (cut_at_all) {   // the first bins whose tokens all chunks list
         for (int c = t; c < sp.chunks; c += T) s_listed_of[c] = sp.listed[(int64_t)b * sp.chunks + c];
         if (t == 0) s_bins = kBins;
@@ -675,6 +713,7 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
         bin = next;
         from = bin < s_bins ? kListed : count <= kList ? kGathered : kReadAgain;
         if (from != kGathered) return;
+        held = false;
         __syncthreads();
         if (t == 0) s_listed = 0;
         __syncthreads();
@@ -689,11 +728,13 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     auto each_token = [&](auto f) {
         if (from == kListed) {
             for (int c = wave; c < sp.chunks; c += WAVES) {
-                const uint2 *list = sp.token + ((int64_t)b * sp.chunks + c) * kFirst;
                 const int n = s_listed_of[c].y;
+                if (held) {
+                    for (int i = lane; i < n; i += 64) f(s_key[c * kFirst + i], s_index[c * kFirst + i]);
+                    continue;
+                }
                 uint2 v[kFirst / 64];
-#pragma unroll
-                for (int i = 0; i < kFirst / 64; ++i) v[i] = list[64 * i + lane];   // of the last ones, what is there
+                read_list(c, v);
 #pragma unroll
                 for (int i = 0; i < kFirst / 64; ++i)
                     if (64 * i + lane < n) f(v[i].x, (int)v[i].y);
@@ -704,7 +745,7 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
             stream([&](uint32_t k, int i, int) { if (k) f(k, i); });
         }
     };
-    const Kept kept = cut(a, b, s, row, live, prepare, each_token,
+    const Kept kept = cut(set, s, row, live, prepare, each_token,
                           [&](const Kept &, bool by_k, const Found &in) { return by_k ? in.mass_before : all; });
 
     // What is kept of each chunk: whole bins, and of the one where the cut is the tokens that are kept.
@@ -714,7 +755,12 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     __syncthreads();
     for (int c = wave; c < sp.chunks; c += WAVES) {
         uint64_t m = 0;
-        for (int i = lane; i < last; i += 64) m += masses[c * kBins + i];
+        for (int i0 = 0; i0 < last; i0 += 256)
+#pragma unroll
+            for (int i = i0 + lane; i < i0 + 256; i += 64) {
+                const uint64_t v = masses[c * kBins + i];
+                m += i < last ? v : 0;
+            }
         for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
         if (lane == 0) s_chunk[c] = m;
     }
@@ -743,7 +789,7 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
     }
     uint64_t total = 0;
     for (int c = 0; c < sp.chunks; ++c) total += s_chunk[c];
-    const uint64_t target = place_of(a, b, total);
+    const uint64_t target = place_of(set.u, total);
     uint64_t before = 0;
     int c = 0;
     for (; c < sp.chunks - 1 && before + s_chunk[c] <= target; ++c) before += s_chunk[c];
