@@ -28,4 +28,41 @@ template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) { re
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
+// Scans over the wave's 64 lanes, all of which are there; 0 adds nothing to `join`.  By moves within and between rows of
+// 16 lanes: a shuffle through LDS takes some ten times as long.
+template <int CONTROL, int ROWS, typename T> __device__ __forceinline__ T moved(T v) {
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = moved<CONTROL, ROWS>((uint32_t)u), hi = moved<CONTROL, ROWS>((uint32_t)(u >> 32));
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    } else {
+        return (T)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, ROWS, 0xf, false);
+    }
+}
+template <typename T, typename F> __device__ __forceinline__ T wave_scan(T v, F join) {
+    v = join(v, moved<0x111, 0xf>(v));   // from 1, 2, 4 and 8 lanes below, within a row
+    v = join(v, moved<0x112, 0xf>(v));
+    v = join(v, moved<0x114, 0xf>(v));
+    v = join(v, moved<0x118, 0xf>(v));
+    v = join(v, moved<0x142, 0xa>(v));   // the last lane of the row below, for rows 1 and 3
+    v = join(v, moved<0x143, 0xc>(v));   // lane 31, for rows 2 and 3
+    return v;
+}
+// Of one lane, for all.
+template <typename T> __device__ __forceinline__ T of_lane(T v, int lane) {
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        return __builtin_bit_cast(T, (uint64_t)of_lane((uint32_t)(u >> 32), lane) << 32 | of_lane((uint32_t)u, lane));
+    } else {
+        return (T)__builtin_amdgcn_readlane((int)v, lane);
+    }
+}
+template <typename T, typename F> __device__ __forceinline__ T wave_all(T v, F join) { return of_lane(wave_scan(v, join), 63); }
+struct Sum {
+    template <typename T> __device__ __forceinline__ T operator()(T x, T y) const { return x + y; }
+};
+struct Largest {
+    template <typename T> __device__ __forceinline__ T operator()(T x, T y) const { return x > y ? x : y; }
+};
+
 }  // namespace bsp

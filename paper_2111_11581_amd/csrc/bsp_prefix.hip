@@ -132,13 +132,10 @@ __device__ __forceinline__ int cost_of(bool f32, int columns, int blocks) {
     return max((read + blocks - 1) / blocks, compute);
 }
 
-// Inclusive scan of one value a thread over the workgroup.
+// Inclusive scan of one value a thread over the workgroup; 0 adds nothing.
 template <typename T, typename F> __device__ __forceinline__ T scan(T v, T *s_wave, F join) {
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
-    for (int d = 1; d < 64; d *= 2) {
-        const T o = __shfl_up(v, d);
-        if (lane >= d) v = join(v, o);
-    }
+    v = wave_scan(v, join);
     __syncthreads();
     if (lane == 63) s_wave[w] = v;
     __syncthreads();
@@ -193,7 +190,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     if (G) {
         // bounds of groups in order and within the batch, whatever starts holds
         const int mine = t <= G ? bound(t) : 0, last = G == T && t == 0 ? bound(G) : 0;
-        const int lo = scan(mine, s_wave, [](int x, int y) { return max(x, y); });
+        const int lo = scan(mine, s_wave, Largest());
         if (t <= G) s_lo[t] = lo;
         s_from[t] = s_to[t] = 0;
         __syncthreads();
@@ -245,7 +242,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         i.all = (int64_t)i.units * i.steps * i.cost;
     }
     auto total_of = [&](int64_t v, int which) {
-        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+        v = wave_all(v, Sum());
         if (t % 64 == 0) s_sum[t / 64][which] = v;
     };
     total_of(item[0].all, 0), total_of(item[1].all, 1), total_of((int64_t)item[1].units * item[1].cost, 2);
@@ -273,10 +270,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         const int n = pieces_of(item[0], most_of[r]);
         tasks[r] = (int64_t)n * item[0].units, longest[r] = n ? (int64_t)((item[0].steps + n - 1) / n) * item[0].cost : 0;
     }
-    for (int d = 1; d < 64; d *= 2)
-        for (int r = 0; r < kRounds; ++r) {
-            tasks[r] += __shfl_xor(tasks[r], d), longest[r] = max(longest[r], (int64_t)__shfl_xor(longest[r], d));
-        }
+    for (int r = 0; r < kRounds; ++r) tasks[r] = wave_all(tasks[r], Sum()), longest[r] = wave_all(longest[r], Largest());
     __syncthreads();   // the total has been read
     if (t % 64 == 0) s_sum[t / 64][0] = tasks[0], s_sum[t / 64][1] = tasks[1], s_sum[t / 64][2] = longest[0], s_sum[t / 64][3] = longest[1];
     __syncthreads();
@@ -290,7 +284,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     // numbers of tasks: those of groups, then those of sequences, both in one scan
     const int n0 = pieces_of(item[0], most), n1 = pieces_of(item[1], most);
     const int64_t count = (int64_t)(n0 * item[0].units) << 32 | (uint32_t)(n1 * item[1].units);
-    const int64_t upto = scan(count, &s_sum[0][0], [](int64_t x, int64_t y) { return x + y; });
+    const int64_t upto = scan(count, &s_sum[0][0], Sum());
     if (t == T - 1) s_all = upto;
     __syncthreads();
     const int of_groups = (int)(s_all >> 32), before = of_groups + (int)(uint32_t)s_all;

@@ -115,10 +115,7 @@ template <int THREADS> struct Scratch {
 // Inclusive scans of two values over the workgroup.
 template <int THREADS> __device__ __forceinline__ void scan(uint64_t *x, uint64_t *y, uint64_t (*s_part)[THREADS / 64]) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t ox = __shfl_up(*x, d), oy = __shfl_up(*y, d);
-        if (lane >= d) *x += ox, *y += oy;
-    }
+    *x = wave_scan(*x, Sum()), *y = wave_scan(*y, Sum());
     __syncthreads();
     if (lane == 63) s_part[0][wave] = *x, s_part[1][wave] = *y;
     __syncthreads();
@@ -128,7 +125,7 @@ template <int THREADS> __device__ __forceinline__ void scan(uint64_t *x, uint64_
 }
 // Largest over the workgroup, for all.
 template <int THREADS> __device__ __forceinline__ uint32_t largest(uint32_t v, uint32_t *s_part) {
-    for (int d = 1; d < 64; d *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    v = wave_all(v, Largest());
     __syncthreads();
     if (threadIdx.x % 64 == 0) s_part[threadIdx.x / 64] = v;
     __syncthreads();
@@ -435,8 +432,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
         uint64_t m = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) m += mass(k[e], 4 * (q * THREADS + t) + e);
-        if (__any(m != 0))
-            for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+        if (__any(m != 0)) m = wave_all(m, Sum());
         if (lane == 0) s_sum[q * WAVES + wave] = m;
     }
     __syncthreads();
@@ -444,24 +440,20 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
     const int sums = rounds * WAVES;
     uint64_t total = 0;
     for (int i = lane; i < sums; i += 64) total += s_sum[i];
-    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    total = wave_all(total, Sum());
     const uint64_t target = place_of(set.u, total);
     uint64_t before = 0;
     int at = 0;
     for (int i0 = 0; i0 < sums; i0 += 64) {
         const uint64_t m = i0 + lane < sums ? s_sum[i0 + lane] : 0;
-        uint64_t upto = m;
-        for (int d = 1; d < 64; d *= 2) {
-            const uint64_t o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        const uint64_t upto = wave_scan(m, Sum());
         const uint64_t hit = __ballot(before + upto > target);
         if (hit) {
             const int first = __ffsll((unsigned long long)hit) - 1;
-            at = i0 + first, before += __shfl(upto - m, first);
+            at = i0 + first, before += of_lane(upto - m, first);
             break;
         }
-        before += __shfl(upto, 63);
+        before += of_lane(upto, 63);
     }
     if (at % WAVES != wave) return;
     const int i = at / WAVES * THREADS + t;
@@ -470,10 +462,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_row(SampleArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) upto += m[e] = mass(k[e], 4 * i + e);
     const uint64_t mine = upto;
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
+    upto = wave_scan(upto, Sum());
     upto += before - mine;   // before the lane's
     if (upto > target || upto + mine <= target) return;
 #pragma unroll
@@ -552,8 +541,7 @@ template <typename E> __global__ __launch_bounds__(256) void k_sample_lay(Sample
     for (int r = 0; r < ROWS; ++r) {
         const uint32_t k = s_key[r][t];
         if (r < rows && i0 + t < a.vocab) sp.keys[(int64_t)(b0 + r) * sp.row + i0 + t] = k;
-        uint32_t top = k;
-        for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        const uint32_t top = wave_all(k, Largest());
         if (lane == 0) s_top[r][wave] = top;
     }
     __syncthreads();
@@ -761,7 +749,7 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
                 const uint64_t v = masses[c * kBins + i];
                 m += i < last ? v : 0;
             }
-        for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+        m = wave_all(m, Sum());
         if (lane == 0) s_chunk[c] = m;
     }
     __syncthreads();
@@ -781,7 +769,7 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
                     for (int e = 0; e < 4; ++e)
                         if (kept.has(key[e], i + e) && row.bin(key[e]) == last) m += row.mass(key[e]);
                 }
-                for (int d = 1; d < 64; d *= 2) m += __shfl_xor(m, d);
+                m = wave_all(m, Sum());
                 if (lane == 0) s_chunk[c] += m;   // the wave's own
             }
         }
