@@ -130,6 +130,8 @@ def sample(model: Decoder, prompts, new, samples: int, temperature: float = 1.0,
     prompt [samples][new[i]]), the log probabilities that they were drawn with (the same) and the cache."""
     _check(model, prompts, new, samples, "sample")
     n = len(prompts)
+    if n * samples > 1024:
+        raise ValueError("sample draws up to 1024 continuations, which attention over shared prefixes takes at a time")
     pages = sum(-(-len(p) // page_size) + samples * (-(-t // page_size) + 2) for p, t in zip(prompts, new))
     cache = model.cache(n * (1 + samples), pages, page_size)
     gen = torch.Generator(device="cuda").manual_seed(seed)

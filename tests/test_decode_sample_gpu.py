@@ -170,6 +170,11 @@ def test_refusals(D):
             D.sample(model, prompts, new, samples)
 
 
+def test_more_continuations_than_a_call_takes(D):
+    with pytest.raises(ValueError, match="1024"):
+        D.sample(small(D, "bf16"), [[1], [2, 3]], [2, 2], 513)
+
+
 def test_command(D, capsys):
     D.main(["--prompts", "2", "--samples", "3", "--tokens", "4", "--dtype", "f32", "--layers", "1", "--top-k", "20", "--temperature", "0.7"])
     assert "0 pages in use" in capsys.readouterr().out
