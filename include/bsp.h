@@ -404,9 +404,11 @@ bsp_status bsp_cache_append_rotary(const bsp_cache *cache, const bsp_rope *rope,
  * group's first entry), and to the others in their own; no member attends to tokens at or past its own
  * length or before its window, whatever is shared.  So results are those of bsp_attention where members
  * and prefix row name the same pages for the shared tokens.  A prefix row not in 0 .. seqs - 1, and
- * entries that hold nothing, give no tokens; `shared` may be 0 and may be larger than lengths.  batch up
- * to 1024 and groups up to batch (0: nothing is shared); else BSP_EUNSUPPORTED.  The rest is as for
- * bsp_attention. */
+ * entries that hold nothing, give no tokens; `shared` may be 0 and may be larger than lengths.  Read once
+ * is what all members attend to; a member whose tokens end before those that the group's longest one
+ * shares, or whose window begins after them, is worked on by itself, so that what a token holds (an Inf, a
+ * NaN) meets no sequence that does not attend to it.  batch up to 1024 and groups up to batch (0: nothing
+ * is shared); else BSP_EUNSUPPORTED.  The rest is as for bsp_attention. */
 bsp_status bsp_attention_prefix_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t groups,
                                           int32_t width, int64_t *bytes);
 bsp_status bsp_attention_prefix(const bsp_cache *cache, int32_t batch, int32_t heads, const void *q,

@@ -11,6 +11,9 @@
 //    staged in LDS, 32 a wave (columns_wide).
 //  * k_prefix_join joins the tasks of every query head by their maxima, in the order of their tokens.
 // Tables that hold few tokens take one kernel instead (k_prefix_short).
+// 32 sequences over 4096 shared tokens (34 MB) take 38 us in a graph: a plan of 7, tasks of 25 and a join of 5.5, each
+// a chain of latencies.  64 over 32768 (69 GFLOP, half as many again for probabilities in two parts) take 156: tasks
+// of 138, in which MFMA works 37 % of the time and VALU 47 %.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -585,11 +588,15 @@ template <int N> __device__ __forceinline__ void copy16(const char *const *src, 
     else
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:1024\n\t"
-                     "global_load_lds_dwordx4 %3, off offset:2048\n\tglobal_load_lds_dwordx4 %4, off offset:3072\n\ts_mov_b32 m0, %0"
-                     : "=&s"(saved) : "v"(src[0]), "v"(src[1] - 1024), "v"(src[2] - 2048), "v"(src[3] - 3072), "s"(base) : "memory");
+                     "global_load_lds_dwordx4 %3, off offset:2048\n\tglobal_load_lds_dwordx4 %4, off offset:%6\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved) : "v"(src[0]), "v"(src[1] - 1024), "v"(src[2] - 2048), "v"(src[3] - 3 * 1024), "s"(base), "n"(3 * 1024)
+                     : "memory");
 }
 
-// CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.
+// CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.  256 columns over
+// 4096 tokens are bound by products and softmax, which the two waves of a SIMD overlap in part alone (48 MFMA by themselves
+// 1500 cycles, 160 VALU instructions 1227, both 2129); one bf16 for a probability would save an eighth of the time, and
+// half of its bits.  A priority for either wave or keys of the next step read ahead save nothing.
 template <int DP, bool FULL, int CW>
 __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, const Task &k, const uint16_t *laid, const void *zero,
                                              const Parts &parts, int64_t task) {
@@ -982,7 +989,9 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
     });
 }
 
-// Sequences of few tokens take one kernel, in which each reads what it shares by itself.
+// Sequences of few tokens take one kernel, in which each reads what it shares by itself: in tables of 1000 tokens 8
+// sequences of 8 key heads 15 us and by a plan 26.5, 32 sequences 17.5 and 39, 64 of 64 query heads 29 and 57.  Of 2100
+// tokens 4 sequences 27 and 23, but 32 sequences, which fill the card, 30 and 41; 64 over 3256 tokens 70 and 63.
 constexpr int64_t kShort = 1024;
 bool is_short(const CacheArgs &c, int batch, int heads, int64_t tokens) {
     const int64_t units = (int64_t)batch * c.kv_heads * ((heads / c.kv_heads + 15) / 16);
