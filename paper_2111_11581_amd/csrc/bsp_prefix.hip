@@ -260,8 +260,11 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     // A last task of fewer units is taken for a whole one, here as in its pieces, whose number goes by this total.
     const int64_t per_seq = (int64_t)a.c.kv_heads * a.head_groups;
     const int64_t total = of_groups_all + own_all / per_seq * ((per_seq + (1 << bundle) - 1) >> bundle << bundle);
-    // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks in all, in
-    // rounds of the card, at the cost of the largest.
+    // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks of groups in all,
+    // in rounds of the card, at the cost of the largest.  Two also where what sequences have of their own is a third of
+    // the work, whose tasks differ more than the model knows: 60 sequences of up to 4000 own tokens 138 and 117 us, 64 of
+    // 1000 after 16000 shared ones 146 and 125, but of 600 after 32768 169 and 190, of 100 in 3 groups of 8000 85 and
+    // 98.  Three or four tasks are not better.
     auto pieces_of = [&](const Item &i, int64_t most) {
         // in fp64, which holds these whole numbers, as a division of 64 bits takes a hundred instructions
         return i.units ? max(1, min(i.steps, (int)min(ceil((double)i.steps * i.cost / (double)most), 1e9))) : 0;
@@ -282,7 +285,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         int64_t n = 0, l = 0;
         for (int w = 0; w < W; ++w) n += s_sum[w][r], l = max(l, s_sum[w][2 + r]);
         const int64_t time = max((n + kGrid - 1) / kGrid * (l + kTaskCost), total / kGrid + kTaskCost * (r + 1));
-        if (time < best) best = time, most = most_of[r];
+        if (time < best || 2 * own_all >= of_groups_all) best = time, most = most_of[r];
     }
     // numbers of tasks: those of groups, then those of sequences, both in one scan
     const int n0 = pieces_of(item[0], most), n1 = pieces_of(item[1], most);
@@ -954,9 +957,9 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
 }
 
 // A workgroup for up to 16 query heads of a key head of a sequence.
-template <typename E, int DP, bool FULL>
-__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short(PrefixArgs p) {
-    __shared__ Narrow<E, DP, 1, kWaves> sh;
+template <typename E, int DP, bool FULL, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_prefix_short(PrefixArgs p) {
+    __shared__ Narrow<E, DP, 1, WAVES> sh;
     const AttnArgs &a = p.a;
     const int per_seq = a.c.kv_heads * a.head_groups, b = blockIdx.x / per_seq, u = blockIdx.x - b * per_seq, lane = threadIdx.x % 64;
     Task k;
@@ -975,14 +978,14 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_prefix_short
         break;
     }
     if (k.from >= k.to) {   // no tokens
-        for (int i = threadIdx.x; i < k.columns * a.c.head_dim; i += 64 * kWaves) {
+        for (int i = threadIdx.x; i < k.columns * a.c.head_dim; i += 64 * WAVES) {
             const int c = i / a.c.head_dim, h = k.j * a.group + k.c0 + c, d = i - c * a.c.head_dim;
             ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = (E)0;
             if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = -INFINITY;
         }
         return;
     }
-    columns_narrow<E, DP, FULL, 1, kWaves>(a, sh, k, 0, (const E *)nullptr, [&](int, int c, int d, float o, float m, float l) {
+    columns_narrow<E, DP, FULL, 1, WAVES>(a, sh, k, 0, (const E *)nullptr, [&](int, int c, int d, float o, float m, float l) {
         const int h = k.j * a.group + k.c0 + c;
         ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
         if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;
@@ -1001,7 +1004,12 @@ bool is_short(const CacheArgs &c, int batch, int heads, int64_t tokens) {
 template <typename E, int DP, bool FULL> hipError_t run(const PrefixArgs &p, bool few, hipStream_t st) {
     const AttnArgs &a = p.a;
     if (few) {
-        k_prefix_short<E, DP, FULL><<<a.batch * a.c.kv_heads * a.head_groups, 64 * kWaves, 0, st>>>(p);
+        // Eight waves where each has a CU for itself, unless a wave's registers ask for a SIMD: 132 workgroups of fp32 30.9 ->
+        // 26.5 us, 128 and 256 of bf16 2 to 3 % less; but 512 workgroups 26.9 -> 30.5, 1600 of 90 tokens 24 -> 36.
+        const int units = a.batch * a.c.kv_heads * a.head_groups;
+        constexpr int MORE = DP == 256 ? kWaves : 2 * kWaves;
+        if (units <= kGrid) k_prefix_short<E, DP, FULL, MORE><<<units, 64 * MORE, 0, st>>>(p);
+        else k_prefix_short<E, DP, FULL, kWaves><<<units, 64 * kWaves, 0, st>>>(p);
         return hipGetLastError();
     }
     const Sizes z = sizes_of(a.c, a.batch, a.heads, p.groups);

@@ -486,3 +486,11 @@ def test_units_that_do_not_fill_their_tasks(B):
     torch.cuda.synchronize()
     s.check(y, out, 0.35)
     assert bool((ws[need:] == 0xff).all())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+def test_more_workgroups_than_fill_the_card(B, dim, dt):
+    rng = np.random.default_rng(dim)
+    s = Setup(B, [100, 30], [50, 33], [rng.integers(-20, 20, 100), rng.integers(0, 9, 30)], 2, 6, dim, 16, dt, seed=dim)
+    s.check(*s.run(dim ** -0.5), dim ** -0.5)
