@@ -129,7 +129,7 @@ struct Scale {
 // What 128 tokens cost a CU, in units of 1800 cycles: reading keys and values of 128 dimensions from memory takes
 // 4 of these for bf16 and 8 for fp32 (less each where several column blocks read the same), the products 1 for
 // every 64 columns of bf16 and 5 for 32 of fp32.  A task by itself is worth kTaskCost.
-constexpr int kTaskCost = 8;
+constexpr int kTaskCost = 8, kLeastTask = 16;   // the latter: the least that a task is cut to
 __device__ __forceinline__ int cost_of(bool f32, int columns, int blocks) {
     const int read = f32 ? 8 : 4, compute = f32 ? 5 * ((columns + 31) / 32) : (columns + 63) / 64;
     return max((read + blocks - 1) / blocks, compute);
@@ -180,7 +180,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     __shared__ struct {
         int row, lead, shared, begin, cut, skip, len;
     } s_own[kMost];
-    __shared__ int64_t s_sum[MOST][4], s_all;
+    __shared__ int64_t s_sum[MOST][5], s_all;
     const AttnArgs &a = p.a;
     const int t = threadIdx.x, G = p.groups, B = a.batch;
     const Space space = space_of(a.workspace, z, B, a.c.head_dim);
@@ -256,10 +256,11 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     // in one, a part of the waves for each (32 sequences of 256 tokens after 4096 shared ones 44 -> 38 us, 64 of 16 tokens after
     // 3000 64 -> 54; of 2000 tokens after 1 83 -> 90, of 128 tokens after 32768 153 -> 164).
     const int bundle = own_all <= 2 * own_step && 2 * own_all >= of_groups_all ? z.bundle_log2 : 0;
-    if (bundle) item[1].units = (item[1].units + (1 << bundle) - 1) >> bundle, item[1].cost <<= bundle;
-    // A last task of fewer units is taken for a whole one, here as in its pieces, whose number goes by this total.
-    const int64_t per_seq = (int64_t)a.c.kv_heads * a.head_groups;
-    const int64_t total = of_groups_all + own_all / per_seq * ((per_seq + (1 << bundle) - 1) >> bundle << bundle);
+    // The units of a task are worked on side by side: one step of eight takes some 8 us, of one 4.
+    const int64_t per_seq = (int64_t)a.c.kv_heads * a.head_groups, bundles = (per_seq + (1 << bundle) - 1) >> bundle;
+    if (bundle) item[1].units = item[1].units ? (int)bundles : 0, item[1].cost *= 2;
+    // Of the tasks as they are, since it bounds the number of pieces.
+    const int64_t total = of_groups_all + (bundle ? own_all / per_seq * bundles * 2 : own_all);
     // One task for a workgroup, or two of half the cost where these fill the card more evenly: the tasks of groups in all,
     // in rounds of the card, at the cost of the largest.  Two also where what sequences have of their own is a third of
     // the work, whose tasks differ more than the model knows: 60 sequences of up to 4000 own tokens 138 and 117 us, 64 of
@@ -270,15 +271,29 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         return i.units ? max(1, min(i.steps, (int)min(ceil((double)i.steps * i.cost / (double)most), 1e9))) : 0;
     };
     static_assert(kRounds == 2, "");
-    int64_t most_of[kRounds], tasks[kRounds], longest[kRounds];
+    int64_t most_of[kRounds], tasks[kRounds], longest[kRounds], few = 0, few_most[2];
     for (int r = 0; r < kRounds; ++r) {
-        most_of[r] = max((int64_t)(2 * kTaskCost), (int64_t)ceil((double)total / (kGrid * (r + 1))));
+        most_of[r] = max((int64_t)kLeastTask, (int64_t)ceil((double)total / (kGrid * (r + 1))));
         const int n = pieces_of(item[0], most_of[r]);
         tasks[r] = (int64_t)n * item[0].units, longest[r] = n ? (int64_t)((item[0].steps + n - 1) / n) * item[0].cost : 0;
     }
     for (int r = 0; r < kRounds; ++r) tasks[r] = wave_all(tasks[r], Sum()), longest[r] = wave_all(longest[r], Largest());
+    // Where even two tasks a workgroup would be small, smaller ones than otherwise, if there is a workgroup for each (32
+    // sequences over 4096 shared tokens 36.3 -> 34.4 us, 64 of 8 in 4 groups of 3000 44.4 -> 38.3; with more tasks than
+    // workgroups 64 of 64 heads over 3000 53.8 -> 68.5).
+    const bool small = total < kGrid * kRounds * kLeastTask;
+    if (small) {
+        for (int r = 0; r < 2; ++r) {
+            few_most[r] = max((int64_t)(kLeastTask * (r + 2) / 4), (int64_t)ceil((double)total / (kGrid * kRounds)));
+            for (int k = 0; k < 2; ++k) few += (int64_t)pieces_of(item[k], few_most[r]) * item[k].units << 32 * r;
+        }
+        few = wave_all(few, Sum());
+    }
     __syncthreads();   // the total has been read
-    if (t % 64 == 0) s_sum[t / 64][0] = tasks[0], s_sum[t / 64][1] = tasks[1], s_sum[t / 64][2] = longest[0], s_sum[t / 64][3] = longest[1];
+    if (t % 64 == 0) {
+        int64_t *of = s_sum[t / 64];
+        of[0] = tasks[0], of[1] = tasks[1], of[2] = longest[0], of[3] = longest[1], of[4] = few;
+    }
     __syncthreads();
     int64_t best = INT64_MAX, most = 1;
     for (int r = 0; r < kRounds; ++r) {
@@ -286,6 +301,12 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         for (int w = 0; w < W; ++w) n += s_sum[w][r], l = max(l, s_sum[w][2 + r]);
         const int64_t time = max((n + kGrid - 1) / kGrid * (l + kTaskCost), total / kGrid + kTaskCost * (r + 1));
         if (time < best || 2 * own_all >= of_groups_all) best = time, most = most_of[r];
+    }
+    if (small) {
+        int64_t n = 0;
+        for (int w = 0; w < W; ++w) n += s_sum[w][4];
+        if (n >> 32 <= kGrid) most = few_most[1];
+        if ((uint32_t)n <= kGrid) most = few_most[0];
     }
     // numbers of tasks: those of groups, then those of sequences, both in one scan
     const int n0 = pieces_of(item[0], most), n1 = pieces_of(item[1], most);
