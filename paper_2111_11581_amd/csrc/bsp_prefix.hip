@@ -11,8 +11,8 @@
 //    staged in LDS, 32 a wave (columns_wide).
 //  * k_prefix_join joins the tasks of every query head by their maxima, in the order of their tokens.
 // Tables that hold few tokens take one kernel instead (k_prefix_short).
-// 32 sequences over 4096 shared tokens (34 MB) take 38 us in a graph: a plan of 7, tasks of 25 and a join of 5.5, each
-// a chain of latencies.  64 over 32768 (69 GFLOP, half as many again for probabilities in two parts) take 156: tasks
+// 32 sequences over 4096 shared tokens (34 MB) take 34 us in a graph: a plan of 8, tasks of 20 and a join of 6, each
+// a chain of latencies.  64 over 32768 (69 GFLOP, half as many again for probabilities in two parts) take 155: tasks
 // of 138, in which MFMA works 37 % of the time and VALU 47 %.
 #include <hip/hip_runtime.h>
 

@@ -6,13 +6,14 @@
 // their logit's distance from the largest, and the bin in which a cut falls is cut further by the bits of
 // its keys.
 //  * Rows of up to 32768 tokens stay in the LDS of a workgroup (k_sample_row), where each step waits for the one
-//    before: one row of 4000 tokens takes 7.4 us without a cut and 19.6 with three, 64 rows 23.4, 64 rows of 30000 41.
+//    before: one row of 4000 tokens takes 7.4 us without a cut and 16.6 with three, 64 rows 20.3, 64 rows of 30000 36.5.
 //  * Of longer ones k_sample_scan finds the largest logits, k_sample_bins fills the bins of each chunk, and in
 //    k_sample_pick a workgroup a row finds cuts and token; it reads again the tokens of the bins where the cuts
 //    are, and one chunk.
 //  * Rows whose elements lie apart are laid out by k_sample_lay.
-// 64 rows of 131072 tokens, three cuts, 33.5 MB: 20 us laid out (67 MB), 25 for the bins (fp64 weights of 8.4 million
-// tokens; 19 without cuts), 28 for cuts and tokens (a chain of latencies, the more the more cuts: 13 without).
+// 64 rows of 131072 tokens, three cuts, 33.5 MB, 64 us in a graph: 16 laid out (67 MB, 4.2 TB/s), 25 for the bins (19
+// without cuts; neither weights nor atomics bound them, but four workgroups a CU that wait in step), 25 for cuts and
+// tokens (a chain of latencies, the more the more cuts).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
