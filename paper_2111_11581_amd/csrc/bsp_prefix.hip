@@ -1014,8 +1014,9 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_prefix_short(
 }
 
 // Sequences of few tokens take one kernel, in which each reads what it shares by itself: in tables of 1000 tokens 8
-// sequences of 8 key heads 15 us and by a plan 26.5, 32 sequences 17.5 and 39, 64 of 64 query heads 29 and 57.  Of 2100
-// tokens 4 sequences 27 and 23, but 32 sequences, which fill the card, 30 and 41; 64 over 3256 tokens 70 and 63.
+// sequences of 8 key heads 14.7 us and by a plan 25.4, 32 sequences 16.4 and 30, 64 of 64 query heads 28 and 43.  Of 2100
+// tokens 4 sequences 27 and 25, but 32 sequences, which fill the card, 29 and 32, 64 with nothing shared 61 and 73; of
+// 3256 tokens 32 sequences 41 and 33.
 constexpr int64_t kShort = 1024;
 bool is_short(const CacheArgs &c, int batch, int heads, int64_t tokens) {
     const int64_t units = (int64_t)batch * c.kv_heads * ((heads / c.kv_heads + 15) / 16);

@@ -30,14 +30,14 @@ constexpr int kBins = 512, kSpan = 32;    // bins, and the distance that they co
 constexpr int kScan = 2048, kLay = 256;    // tokens whose largest logit k_sample_scan and k_sample_lay find
 constexpr int kChunk = 8192;               // tokens whose bins k_sample_bins fills
 // Tokens that a workgroup holds in LDS.  Chunks would give more workgroups to few rows, but in three kernels: 12000 tokens
-// 26.2 us and in chunks 36.7, 16 rows of them 29.0 and 39.5, 30000 tokens 34.5 and 37.8, 64 rows of them 40.9 and 43.7.
+// 21.9 us and in chunks 30.9, 16 rows of them 24.5 and 33.5, 30000 tokens 30.3 and 32.2, 64 rows of them 36 and 45.
 constexpr int kRow = 32768;
 // Tokens of a bin that are compared with each other, two a thread for a count of 128 * 128; 32 take the same time at
 // every size tried.
 constexpr int kQuick = 128;
 constexpr int kList = 4096;                // tokens of a bin that k_sample_pick holds in LDS
 // Tokens of a chunk's first bins that k_sample_bins lists: enough for most cuts, which are among the likeliest tokens
-// (64 rows of 131072 tokens 73.1 us, with 512 76.1).
+// (64 rows of 131072 tokens 64.0 us, with 512 67.5).
 constexpr int kFirst = 256;
 
 // Logits as numbers that are in the same order; NaN and -Inf, which are never taken, are 0.
@@ -47,7 +47,7 @@ __device__ __forceinline__ uint32_t key_of(float l) {
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ uint32_t key_of(uint16_t l) { return key_of(bf16_to_f32(l)); }
-__device__ __forceinline__ uint32_t key_of(uint32_t key) { return key; }   // laid out by k_sample_scan
+__device__ __forceinline__ uint32_t key_of(uint32_t key) { return key; }   // laid out by k_sample_lay
 __device__ __forceinline__ float logit_of(uint32_t key) {
     return key == 0 ? -INFINITY : __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
 }
@@ -801,8 +801,8 @@ template <typename E> __global__ __launch_bounds__(1024) void k_sample_pick(Samp
 }
 
 template <typename E, bool ALONG> hipError_t run_row(const SampleArgs &a, hipStream_t st) {
-    // As many threads as keep each busy: 4000 tokens take 19.6 us with 512 and 23.8 with 256 threads, 1000 tokens 9.7 with
-    // 256 and 11.8 with 128 (and three cuts of 200 tokens 14.1 and 13.8); 8000 tokens 23.9 with 512 and 24.9 with 1024.
+    // As many threads as keep each busy: 1000 tokens take 8.4 us with 256 threads and 8.7 with 512 (and with 128 a fifth
+    // more than with 256), 4000 tokens 20.8 with 256, 16.6 with 512 and 17.8 with 1024, 8000 tokens 20.9 and 20.6.
     if (a.vocab <= 1024) k_sample_row<E, ALONG, 256, 1024><<<a.batch, 256, 0, st>>>(a);
     else if (a.vocab <= 8192) k_sample_row<E, ALONG, 512, 8192><<<a.batch, 512, 0, st>>>(a);
     else k_sample_row<E, ALONG, 1024, kRow><<<a.batch, 1024, 0, st>>>(a);
@@ -816,8 +816,8 @@ template <typename E> hipError_t run_long(const SampleArgs &a, const Space &sp, 
 }
 
 // Rows whose elements lie apart are read as they lie up to so many tokens, each element a line of its own: 16 rows of 4000
-// tokens 27.7 us and laid out first 33.4, 64 rows 28.2 and 33.9; 64 rows of 8000 34.7 laid out and 35.5, of 30000 51
-// and 71.
+// tokens 19.6 us and laid out first 23.3, 64 rows 20.5 and 24.2; 64 rows of 8000 29.3 laid out and 31.5, of 30000 45
+// and 66.
 constexpr int kApart = 4096;
 
 template <typename E> hipError_t run(SampleArgs a, hipStream_t st) {
