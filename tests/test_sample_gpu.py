@@ -203,3 +203,19 @@ def test_streams_and_graphs(B):
             torch.cuda.synchronize()
             for b in range(n):
                 assert int(tokens[b]) == S.sample(l[b], r[b], top_p=float(np.float32(0.9)))[0]
+
+
+@pytest.mark.parametrize("vocab", [1000, 9000, 40000])
+def test_where_min_p_cuts(B, vocab):
+    """Logits of every spread around the cut: some next to it, all of them far above or below, across zero, one float apart."""
+    rng = np.random.default_rng(vocab)
+    for t in (1e-6, 0.7, 30.0, 1e5, 1e30, 2.0 ** -140):
+        for scale in (1e-3, 1.0, 40.0, 1e6):
+            p = np.array([1e-42, 1e-20, 1e-3, 0.5, 1 - 2.0 ** -23, 1.5], np.float32)
+            l = (rng.standard_normal((6, vocab)) * scale).astype(np.float32)
+            l[:, :64] = l.max(1, keepdims=True) + (np.log(p.astype(np.float64)) * t).clip(-1e30, 0)[:, None].astype(np.float32)
+            for i in range(64):   # a run of neighbours across the cut
+                for _ in range(2):
+                    l[:, i:64] = np.nextafter(l[:, i:64], np.float32(-np.inf if i % 2 else np.inf))
+            check(B, l, rng.random(6), temperature=[t] * 6, min_p=p)
+            check(B, l, rng.random(6), temperature=[t] * 6, min_p=p, top_k=[40] * 6, top_p=[0.9] * 6)
