@@ -29,7 +29,7 @@ template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) { re
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
 // Scans over the wave's 64 lanes, all of which are there; 0 adds nothing to `join`.  By moves within and between rows of
-// 16 lanes: a shuffle through LDS takes some ten times as long.
+// 16 lanes; with shuffles, which go through LDS, the sampling of 64 rows of 131072 tokens takes 72.1 us instead of 64.4.
 template <int CONTROL, int ROWS, typename T> __device__ __forceinline__ T moved(T v) {
     if constexpr (sizeof(T) == 8) {
         const uint64_t u = __builtin_bit_cast(uint64_t, v);

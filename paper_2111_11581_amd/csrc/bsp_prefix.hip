@@ -256,7 +256,8 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
     // in one, a part of the waves for each (32 sequences of 256 tokens after 4096 shared ones 44 -> 38 us, 64 of 16 tokens after
     // 3000 64 -> 54; of 2000 tokens after 1 83 -> 90, of 128 tokens after 32768 153 -> 164).
     const int bundle = own_all <= 2 * own_step && 2 * own_all >= of_groups_all ? z.bundle_log2 : 0;
-    // The units of a task are worked on side by side: one step of eight takes some 8 us, of one 4.
+    // The units of a task are worked on side by side: a step of eight takes some 9 us, of 128 columns
+    // of a group 5.
     const int64_t per_seq = (int64_t)a.c.kv_heads * a.head_groups, bundles = (per_seq + (1 << bundle) - 1) >> bundle;
     if (bundle) item[1].units = item[1].units ? (int)bundles : 0, item[1].cost *= 2;
     // Of the tasks as they are, since it bounds the number of pieces.
