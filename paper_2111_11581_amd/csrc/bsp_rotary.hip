@@ -198,11 +198,14 @@ template <typename E, bool BESIDE> __global__ __launch_bounds__(256) void k_rota
     int first, second;
     bool turned;
     if (BESIDE) {
-        first = 2 * lane, second = first + 1, turned = first < rotated;   // of an odd number of rotated ones the last has a 1
+        first = 2 * lane, second = first + 1, turned = first < rotated;
     } else {
         turned = 2 * lane < rotated;
         first = turned ? lane : 2 * lane, second = turned ? lane + rotated / 2 : first + 1;
     }
+    // Of an odd number of rotated vectors the last one's neighbour is passed on: its bits, as its values times 1 and
+    // 0 would let an Inf or a NaN reach the other dimension of a pair.
+    const bool passed = BESIDE && turned && second >= rotated;
     const bool in = i < a.n, has[2] = {in && first < vectors, in && second < vectors};
     const int d[2] = {min(first, vectors - 1) * VE, min(second, vectors - 1) * VE};
     int64_t place = -1;
@@ -268,6 +271,7 @@ template <typename E, bool BESIDE> __global__ __launch_bounds__(256) void k_rota
                 if (turned) {
 #pragma unroll
                     for (int j = 0; j < VE; ++j) {
+                        if (2 * j / VE == 1 && passed) continue;
                         float *p = BESIDE ? &x[2 * j / VE][2 * j % VE] : &x[0][j], *o = BESIDE ? p + 1 : &x[1][j];
                         const float y = *p * c[j] - *o * sn[j];
                         *o = *o * c[j] + *p * sn[j], *p = y;
@@ -277,6 +281,7 @@ template <typename E, bool BESIDE> __global__ __launch_bounds__(256) void k_rota
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
+                        if (s == 1 && passed && !norm) continue;
                         if constexpr (sizeof(E) == 4) v[k][s][j] = __float_as_uint(x[s][j]);
                         else v[k][s][j] = pack_bf16(x[s][2 * j], x[s][2 * j + 1]);
                     }
