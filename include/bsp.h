@@ -333,7 +333,8 @@ bsp_status bsp_cache_append(const bsp_cache *cache, int32_t n, const void *k, co
  * No such token (len 0, no page, row not in 0 .. seqs - 1): y = 0 and lse = -Inf.  lens above width *
  * page_size read as that.  Nothing else of the cache is used: what other slots hold, NaN too,
  * does not reach y.  Scores, sums and the softmax are in fp32; for BSP_BF16, probabilities keep
- * 16 bits where they multiply the values.
+ * 16 bits where they multiply the values.  A value of Inf makes its y Inf, however small p is (of both
+ * signs, or beside a NaN: NaN); scores that are NaN or +Inf make all of y NaN.
  * workspace: bsp_attention_workspace bytes, 16-byte aligned, whose content does not matter; calls
  * that may overlap need one each.  Async. */
 bsp_status bsp_attention_workspace(const bsp_cache *cache, int32_t batch, int32_t heads, int32_t width, int64_t *bytes);

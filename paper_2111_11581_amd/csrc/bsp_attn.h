@@ -26,6 +26,30 @@ template <bool ONCE, typename T> __device__ __forceinline__ T fetch(const T *p) 
     else return *p;
 }
 
+// An output that is NaN where its probabilities are none has met an Inf: that times the second part of a bf16
+// probability, which may be 0 or negative, or times one that fp32 holds as 0, is not what the probability itself gives.
+// Which it is is told by the values: the Inf that is among those at place(0 .. n - 1), or NaN where both are, or a NaN.
+// For the last step of an output alone, since the sums of parts would be NaN again.
+template <typename E, typename P> __device__ __forceinline__ float of_values(const E *values, int n, P place) {
+    constexpr int AHEAD = 8;
+    float inf = 0.f;
+    for (int i = 0; i < n; i += AHEAD) {
+        int64_t at[AHEAD];
+        float v[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) at[k] = place(min(i + k, n - 1));
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) v[k] = to_f32(values[max(at[k], (int64_t)0)]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (at[k] < 0 || fabsf(v[k]) < INFINITY) continue;
+            if (v[k] != v[k] || v[k] == -inf) return NAN;
+            inf = v[k];
+        }
+    }
+    return inf == 0.f ? NAN : inf;
+}
+
 // What a wave loads and multiplies in one step, for head_dim up to DP: tokens of one key head, with N times 16
 // query heads.
 template <typename E, int DP> struct Step;

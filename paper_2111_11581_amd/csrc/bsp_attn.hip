@@ -365,10 +365,11 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
         const float ref = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += s_l[w][h] * __builtin_amdgcn_exp2f(s_m[w][h] - ref);
-        const float o = s_o[0][h][d] + s_o[1][h][d];
+        float o = s_o[0][h][d] + s_o[1][h][d];
         const int64_t bh = (int64_t)b * a.heads + h0 + h;
         if (whole_unit) {
             E *y = (E *)a.y + b * a.ys.seq + (h0 + h) * a.ys.head + d * a.ys.dim;
+            if (o != o && sum == sum) o = of_values(values + d, to - from, [&](int i) { return place_of(a.c, a.table, sp.row, a.seqs, a.width, from + i); });
             *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);
             if (d == 0 && a.lse) a.lse[bh] = (ref + log2f(sum)) * kLn2;
         } else {
@@ -437,6 +438,12 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     float o = 0.f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
+    if (o != o && sum == sum) {
+        const int row = row_of(a, b);
+        const Span sp = span_of(a, row, len_of(a, row));
+        o = of_values((const E *)a.values + h / a.group * a.c.head_stride + dim, sp.len - sp.first,
+                      [&](int i) { return place_of(a.c, a.table, row, a.seqs, a.width, sp.first + i); });
+    }
     E *y = (E *)a.y + b * a.ys.seq + h * a.ys.head + dim * a.ys.dim;
     *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);
     if (dim == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;

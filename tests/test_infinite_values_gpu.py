@@ -1,0 +1,97 @@
+"""Attention over values of Inf: what it answers is what the definition does, Inf, or NaN where both are attended to or
+a NaN is."""
+
+import numpy as np
+import pytest
+
+from tests import decode_model as M
+from tests.test_paged_attention_gpu import B, Setup   # noqa: F401 (B is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def spoil(s, at, rng):
+    """Values (by `at(b)`: pages and slots that sequence b attends to) of Inf in dimension 0 of one token, -Inf in 1,
+    both in 2, NaN in 3, Inf in 4 of several tokens, in 5 of the last one and in 6 of the first."""
+    inf = np.inf
+    for b in range(s.n if hasattr(s, "n") else len(s.lens)):
+        tokens = at(b)
+        if not tokens:
+            continue
+
+        def put(dim, value, *which):
+            for i in which:
+                s.values[tokens[i][0], tokens[i][1], :, dim] = value
+        n = len(tokens)
+        one, two = int(rng.integers(0, n)), int(rng.integers(0, n))
+        put(0, inf, one), put(1, -inf, two), put(2, inf, one), put(3, np.nan, two), put(5, inf, n - 1), put(6, -inf, 0)
+        if one != two:
+            put(2, -inf, two)
+        put(4, inf, *rng.integers(0, n, 5))
+
+
+def same(got, ref, bound):
+    """Alike where ref is not finite, and within the bound where it is."""
+    odd = ~np.isfinite(ref)
+    assert np.array_equal(got[odd], ref[odd], equal_nan=True), (got[odd], ref[odd])
+    assert (np.abs(got[~odd] - ref[~odd]) <= bound[~odd]).all()
+    return odd
+
+
+def check(s, y, lse, scale, window=0):
+    """As Setup.check, with the bounds of finite values."""
+    y, lse, spoiled = y.double().cpu().numpy(), lse.double().cpu().numpy(), 0
+    for i, n in enumerate(s.lens):
+        for h in range(s.heads):
+            j = h // (s.heads // s.kv)
+            with np.errstate(invalid="ignore"):
+                ref, l, size, _, qk = M.attention(s.q[i, h], s.keys[:, :, j], s.values[:, :, j], s.table[i], s.page, n, window, scale)
+                small = 2 * 2 * (s.dim + 4) * M.U24 * qk + (2 * n + 64) * M.U24
+                p, u = (2.0 ** -8, 2.0 ** -8) if s.dt == "bf16" else (0.0, M.U24)
+                spoiled += same(y[i, h], ref, u * np.abs(ref) + (1 + u) * (p + small) * size).sum()
+            assert lse[i, h] == l if l == -np.inf else abs(lse[i, h] - l) <= 2 * (s.dim + 4) * M.U24 * qk + (n + 64) * M.U24 + 4 * M.U24 * abs(l)
+    assert spoiled > 0
+
+
+def tokens_of(s, b, window=0):
+    n = s.lens[b]
+    at = [(s.table[b, t // s.page], t % s.page) for t in range(max(0, n - window) if window else 0, n)]
+    return [(p, t) for p, t in at if p >= 0]
+
+
+@pytest.mark.parametrize("order", ["heads", "slots"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 40, 64, 96, 128, 136, 256])
+@pytest.mark.parametrize("lens", [[0, 1, 2, 31, 33, 129], [1, 3000, 0, 700, 1500]])
+def test_attention(B, lens, dim, dt, order):
+    s = Setup(B, lens, 2, 6, dim, 16, dt, order, seed=dim)
+    spoil(s, lambda b: tokens_of(s, b), np.random.default_rng(dim))
+    s.dvalues = s.plane(s.values, 0)
+    check(s, *s.run(dim ** -0.5), dim ** -0.5)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attention_windows_and_holes(B, dt):
+    """Nothing of what lies before the window, past the end or in no page."""
+    for lens, window in (([40, 100, 7], 30), ([2500, 1300, 20], 1100)):
+        s = Setup(B, lens, 2, 4, 64, 7, dt, "heads", seed=window, holes=0.1)
+        spoil(s, lambda b: tokens_of(s, b, window), np.random.default_rng(window))
+        s.dvalues = s.plane(s.values, 0)
+        check(s, *s.run(0.125, window), 0.125, window)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [60, 2000])
+def test_attention_of_probabilities_that_are_almost_nothing(B, dt, n):
+    """A value of Inf whose probability is 2^-200 or so: below what fp32 holds, but above 0."""
+    s = Setup(B, [n, n], 1, 2, 64, 16, dt, "heads", seed=n)
+    s.q[:] = 1.0
+    s.keys[np.isfinite(s.keys)] = 0.0
+    page, slot = s.table[0, 5 // 16], 5 % 16
+    s.keys[page, slot] = -2.0      # a score of -128, times 1.125: e^-144
+    s.values[page, slot, :, :4] = np.inf
+    s.values[page, slot, :, 4] = -np.inf
+    s.dkeys, s.dvalues = s.plane(s.keys, 0), s.plane(s.values, 0)
+    y, lse = s.run(1.125)
+    check(s, y, lse, 1.125)
+    assert np.isinf(y[0, :, :5].float().cpu().numpy()).all() and y[1].isfinite().all()
