@@ -439,10 +439,11 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
     if (o != o && sum == sum) {
-        const int row = row_of(a, b);
-        const Span sp = span_of(a, row, len_of(a, row));
-        o = of_values((const E *)a.values + h / a.group * a.c.head_stride + dim, sp.len - sp.first,
-                      [&](int i) { return place_of(a.c, a.table, row, a.seqs, a.width, sp.first + i); });
+        const AttnArgs &args = argument_again<AttnArgs>();
+        const int row = row_of(args, b);
+        const Span sp = span_of(args, row, len_of(args, row));
+        o = of_values((const E *)args.values + h / args.group * args.c.head_stride + dim, sp.len - sp.first,
+                      [&](int i) { return place_of(args.c, args.table, row, args.seqs, args.width, sp.first + i); });
     }
     E *y = (E *)a.y + b * a.ys.seq + h * a.ys.head + dim * a.ys.dim;
     *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);

@@ -974,6 +974,17 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
     float o = 0.f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
+    if (o != o && sum == sum) {   // what the sequence attends to, in a row
+        const PrefixArgs &again = argument_again<PrefixArgs>();
+        const AttnArgs &args = again.a;
+        Task k;
+        k.row = row_of(args, b), k.to = len_of(args, k.row), k.begin = args.window && k.to > args.window ? k.to - args.window : 0;
+        k.to -= k.begin, k.cut = INT32_MAX, k.skip = k.shared = 0, k.lead = -1;
+        for (int g = 0; g < again.groups; ++g)
+            if (const int lo = again.starts[g]; lo >= 0 && lo <= b && b < again.starts[g + 1])
+                k.shared = again.shared[g], k.lead = again.prefix_rows ? again.prefix_rows[g] : row_of(args, lo);
+        o = of_values((const E *)args.values + j * args.c.head_stride + dim, k.to, [&](int i) { return place_in(args, k, i); });
+    }
     ((E *)a.y)[b * a.ys.seq + h * a.ys.head + dim * a.ys.dim] = from_f32<E>(sum == 0.f ? 0.f : o / sum);
     if (dim == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;
 }
@@ -1008,6 +1019,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_prefix_short(
         return;
     }
     columns_narrow<E, DP, FULL, 1, WAVES>(a, sh, k, 0, (const E *)nullptr, [&](int, int c, int d, float o, float m, float l) {
+        if (o != o && l == l)
+            o = of_values((const E *)a.values + k.j * a.c.head_stride + d, k.to, [&](int i) { return place_in(a, k, i); });
         const int h = k.j * a.group + k.c0 + c;
         ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
         if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;

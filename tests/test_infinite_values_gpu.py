@@ -5,6 +5,8 @@ import numpy as np
 import pytest
 
 from tests import decode_model as M
+from tests import sampling_model as S
+from tests import test_prefix_attention_gpu as P
 from tests.test_paged_attention_gpu import B, Setup   # noqa: F401 (B is a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -95,3 +97,63 @@ def test_attention_of_probabilities_that_are_almost_nothing(B, dt, n):
     y, lse = s.run(1.125)
     check(s, y, lse, 1.125)
     assert np.isinf(y[0, :, :5].float().cpu().numpy()).all() and y[1].isfinite().all()
+
+
+# ---- sequences that share their first tokens ----
+
+def check_prefix(s, y, lse, scale, window=0):
+    y, lse, spoiled = y.double().cpu().numpy(), lse.double().cpu().numpy(), 0
+    group = s.heads // s.kv
+    for b in range(s.n):
+        at = s.tokens(b, window)
+        if not at:
+            assert (y[b] == 0).all() and (lse[b] == -np.inf).all()
+            continue
+        p, t = np.array(at).T
+        for j in range(s.kv):
+            h = slice(j * group, (j + 1) * group)
+            with np.errstate(invalid="ignore"):
+                ref, l, size, qk = S.attention(s.q[b, h], s.keys[p, t, j], s.values[p, t, j], scale)
+                score = 2 * (s.dim + 4) * S.U24 * qk[:, None]
+                u, cut = (2.0 ** -8, 2.0 ** -15) if s.dt == "bf16" else (S.U24, 0.0)
+                spoiled += same(y[b, h], ref, u * np.abs(ref) + (1 + u) * (cut + 2 * score + (2 * len(at) + 64) * S.U24) * size).sum()
+            assert (np.abs(lse[b, h] - l) <= score[:, 0] + (len(at) + 64) * S.U24 + 4 * S.U24 * np.abs(l)).all()
+    assert spoiled > 0
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 64, 96, 128, 256])
+@pytest.mark.parametrize("sizes,shared,longest,window,least", [
+    ([1, 3, 0, 2], [33, 100, 5, 64], 40, 0, 0), ([3, 4], [60, 90], 50, 70, 0),              # short tables
+    ([1, 3, 0, 2], [33, 100, 5, 64], 40, 0, 2100), ([3, 9], [2200, 300], 300, 0, 0),        # by a plan
+    ([10, 33, 70], [1500, 900, 2300], 200, 0, 2100), ([30, 5], [3000, 2900], 300, 2500, 0)])
+def test_prefix(B, sizes, shared, longest, window, least, dim, dt):
+    rng = np.random.default_rng(dim + longest)
+    P.Setup.least = least
+    try:
+        s = P.Setup(B, sizes, shared, [rng.integers(-20, longest, m) for m in sizes], 1, 3, dim, 16, dt, seed=dim, extra=1, holes=0.03)
+    finally:
+        P.Setup.least = 0
+    few = rng.permutation(s.n)[:3]   # what most members share stays finite but for a few dimensions
+    spoil(s, lambda b: s.tokens(b, window)[-40:] if b in few else [], rng)
+    for b in few[:1]:
+        for t in s.tokens(b, window)[:3]:
+            s.values[t][:, 7] = np.inf
+    s.data = [s.plane(a) for a in (s.keys, s.values)]
+    check_prefix(s, *s.run(dim ** -0.5, window), dim ** -0.5, window)
+    check_prefix(s, *s.run(dim ** -0.5, window, feature_major=True), dim ** -0.5, window)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("least", [0, 2100])
+def test_prefix_of_other_rows(B, least, dt):
+    """Shared tokens in the pages of a sequence of their own, which alone has the Inf."""
+    P.Setup.least = least
+    try:
+        s = P.Setup(B, [3, 2], [60, 90], [[5, 9, 1], [30, 7]], 2, 4, 64, 16, dt, seed=3, prefix_rows=True)
+    finally:
+        P.Setup.least = 0
+    for t, dim, value in ((3, 0, np.inf), (59, 1, -np.inf), (20, 2, np.nan)):
+        s.values[s.table[s.prefix_rows[0], t // 16], t % 16, :, dim] = value
+    s.data = [s.plane(a) for a in (s.keys, s.values)]
+    check_prefix(s, *s.run(0.125), 0.125)
