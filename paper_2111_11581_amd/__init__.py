@@ -370,6 +370,14 @@ def _ints(name: str, t, n: int):
         raise ValueError(f"{name} must be int32")
 
 
+def _floats(name: str, t, n: int):
+    """A contiguous device array of at least n float32."""
+    if t is None or t.dtype is not _float_types()[F32]:
+        _dev(name, t, 4 * n)
+        raise ValueError(f"{name} must be float32, not {t.dtype}")
+    _dev(name, t, 4 * n)
+
+
 def _on_device(**arrays):
     for name, t in arrays.items():
         if not t.is_cuda:
@@ -652,7 +660,7 @@ def bsp_rotary(dt: int, rope: Rope, freqs, x, pos, y, norm=None, eps: float = 1e
     _freqs(freqs, rope.dims)
     _ints("pos", pos, n)
     if norm is not None:
-        _dev("norm", norm, 4 * dim, F32)
+        _floats("norm", norm, dim)
     st = lib().bsp_rotary(dt, rope, _p(freqs), n, heads, dim, x.data_ptr(), xs, pos.data_ptr(), _p(norm), eps, y.data_ptr(), ys,
                           _stream(stream))
     if st:
@@ -670,9 +678,9 @@ def bsp_cache_append_rotary(cache: CacheShape, rope: Rope, freqs, q, k, v, q_out
         _on_device(q=q, k=k, v=v, q_out=q_out, keys=keys, values=values)
     _freqs(freqs, rope.dims)
     if q_norm is not None:
-        _dev("q_norm", q_norm, 4 * cache.head_dim, F32)
+        _floats("q_norm", q_norm, cache.head_dim)
     if k_norm is not None:
-        _dev("k_norm", k_norm, 4 * cache.head_dim, F32)
+        _floats("k_norm", k_norm, cache.head_dim)
     seqs, width = _table(table)
     _ints("pos", pos, n)
     if rows is not None:
@@ -717,7 +725,7 @@ def bsp_attention_prefix(cache: CacheShape, q, keys, values, table, lens, starts
     if prefix_rows is not None:
         _ints("prefix_rows", prefix_rows, groups)
     if lse is not None:
-        _dev("lse", lse, batch * heads * 4, F32)
+        _floats("lse", lse, batch * heads)
     need = _prefix_workspace(key, batch, heads, groups, width)
     if need:
         _dev("workspace", workspace, need)
@@ -746,18 +754,18 @@ def bsp_sample(dt: int, logits, u, tokens, temperature=None, top_k=None, top_p=N
     batch, vocab = logits.shape
     if not logits.is_cuda:
         _on_device(logits=logits)
-    _dev("u", u, 4 * batch, F32)
+    _floats("u", u, batch)
     _ints("tokens", tokens, batch)
     if temperature is not None:
-        _dev("temperature", temperature, 4 * batch, F32)
+        _floats("temperature", temperature, batch)
     if top_k is not None:
         _ints("top_k", top_k, batch)
     if top_p is not None:
-        _dev("top_p", top_p, 4 * batch, F32)
+        _floats("top_p", top_p, batch)
     if min_p is not None:
-        _dev("min_p", min_p, 4 * batch, F32)
+        _floats("min_p", min_p, batch)
     if logp is not None:
-        _dev("logp", logp, 4 * batch, F32)
+        _floats("logp", logp, batch)
     need = _sample_workspace(batch, vocab)
     if need:
         _dev("workspace", workspace, need)
