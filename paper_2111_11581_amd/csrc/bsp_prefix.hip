@@ -195,7 +195,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         const int mine = t <= G ? bound(t) : 0, last = G == T && t == 0 ? bound(G) : 0;
         const int lo = scan(mine, s_wave, Largest());
         if (t <= G) s_lo[t] = lo;
-        s_from[t] = s_to[t] = 0;
+        s_from[t] = -1, s_to[t] = 0;   // no member is worked on with others
         __syncthreads();
         if (G == T && t == 0) s_lo[G] = max(last, s_lo[G - 1]);
         __syncthreads();
@@ -218,7 +218,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         const bool together = group >= 0 && begin < s_to[group] && len >= s_to[group];
         if (together) atomicMax(&s_from[group], begin);
         __syncthreads();
-        if (together && s_from[group] < s_to[group]) core_from = s_from[group], core_to = s_to[group];
+        if (together) core_from = s_from[group], core_to = s_to[group];   // begin < s_to of each, so of the largest
     }
     s_own[t].begin = begin, s_own[t].cut = core_to ? core_from - begin : INT32_MAX, s_own[t].skip = core_to - core_from;
     s_own[t].row = row, s_own[t].lead = lead, s_own[t].shared = common, s_own[t].len = len - begin - (core_to - core_from);
@@ -234,7 +234,7 @@ template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_
         if (k == 0 && t < G) {
             const int columns = (s_lo[t + 1] - s_lo[t]) * a.group;
             blocks = (columns + block_columns - 1) / block_columns;
-            i.steps = (max(0, s_to[t] - s_from[t]) + kStep - 1) / kStep;
+            i.steps = s_from[t] < 0 ? 0 : (s_to[t] - s_from[t] + kStep - 1) / kStep;
             i.units = i.steps ? blocks * a.c.kv_heads : 0;
             if (i.units) i.cost = cost_of(f32, min(columns, block_columns), blocks);
         } else if (k == 1 && t < B) {
