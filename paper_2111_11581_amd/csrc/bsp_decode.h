@@ -110,7 +110,7 @@ int64_t prefix_workspace(const CacheArgs &c, int batch, int heads, int groups, i
 hipError_t launch_prefix(const PrefixArgs &p, hipStream_t st);
 
 // ---- sampling ----
-constexpr int kMostVocab = 1 << 20;   // so many weights of 2^43 add up to 2^63
+constexpr int kMostVocab = 1 << 20;   // so many weights of 2^43 add up to 2^63, which unsigned sums hold
 struct SampleArgs {
     int dtype, batch, vocab;
     const void *logits;

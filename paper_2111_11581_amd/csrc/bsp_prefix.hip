@@ -12,8 +12,9 @@
 //  * k_prefix_join joins the tasks of every query head by their maxima, in the order of their tokens.
 // Tables that hold few tokens take one kernel instead (k_prefix_short).
 // 32 sequences over 4096 shared tokens (34 MB) take 34 us in a graph: a plan of 8, tasks of 20 and a join of 6, each
-// a chain of latencies.  64 over 32768 (69 GFLOP, half as many again for probabilities in two parts) take 155: tasks
-// of 138, in which MFMA works 37 % of the time and VALU 47 %.
+// a chain of latencies.  64 over 32768 (69 GFLOP, half as many again for probabilities in two parts) take 149: tasks
+// of 138, in which MFMA works 37 % of the time and VALU 47 %.  Without tokens of their own, which are 512 short tasks after
+// the shared ones, 16 less, whether they are 1 or 128 for a sequence.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -166,7 +167,8 @@ template <typename E, int DP> __device__ __forceinline__ void lay_queries(const 
 }
 
 // Block 0 plans, a thread for a group and for a sequence: as many waves as these need, since each wave makes every
-// scan and sum longer.  The other blocks lay the queries out meanwhile.  Bound by latency: 8 us for 32 sequences.
+// scan and sum longer, but four at least.  The other blocks lay the queries out meanwhile.  Bound by latency: 8 us for
+// 32 sequences.
 template <typename E, int DP> __global__ __launch_bounds__(kMost) void k_prefix_plan(PrefixArgs p, Sizes z, int block_columns) {
     if (blockIdx.x > 0) {
         const Space space = space_of(p.a.workspace, z, p.a.batch, p.a.c.head_dim);
@@ -618,10 +620,12 @@ template <int N> __device__ __forceinline__ void copy16(const char *const *src, 
                      : "memory");
 }
 
-// CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.  256 columns over
-// 4096 tokens are bound by products and softmax, which the two waves of a SIMD overlap in part alone (48 MFMA by themselves
-// 1500 cycles, 160 VALU instructions 1227, both 2129); one bf16 for a probability would save an eighth of the time, and
-// half of its bits.  A priority for either wave or keys of the next step read ahead save nothing.
+// CW: waves that share the columns, 32 each; the 8 / CW sets of these share the tokens of a stage.  Of 256 columns over 32
+// tokens the two waves of a SIMD take 2129 cycles (48 MFMA by themselves 1500, 160 VALU instructions 1227), 153 thousand
+// for the 18 stages of a task of 64 sequences over 32768 tokens, which takes some 220 thousand: the others, in which
+// stages begin and end and wait for each other, have not been accounted for one by one.  One bf16 for a probability
+// would save an eighth of the time, and half of its bits.  A priority for either wave or keys of the next step read ahead
+// save nothing.
 template <int DP, bool FULL, int CW>
 __device__ __forceinline__ void columns_wide(const AttnArgs &a, Wide<DP> &sh, const Task &k, const uint16_t *laid, const void *zero,
                                              const Parts &parts, int64_t task) {

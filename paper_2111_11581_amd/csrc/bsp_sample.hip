@@ -25,14 +25,14 @@ namespace bsp {
 
 namespace {
 
-constexpr double kOne = 8796093022208.0;   // 2^43: what a weight of 1 counts; 2^20 of them stay below 2^63
+constexpr double kOne = 8796093022208.0;   // 2^43: what a weight of 1 counts; 2^20 of them add up to 2^63, which unsigned sums hold
 constexpr int kBins = 512, kSpan = 32;    // bins, and the distance that they cover: e^-32 is below 2^-44
 constexpr int kScan = 2048, kLay = 256;    // tokens whose largest logit k_sample_scan and k_sample_lay find
 constexpr int kChunk = 8192;               // tokens whose bins k_sample_bins fills
 // Tokens that a workgroup holds in LDS.  Chunks would give more workgroups to few rows, but in three kernels: 12000 tokens
 // 21.9 us and in chunks 30.9, 16 rows of them 24.5 and 33.5, 30000 tokens 30.3 and 32.2, 64 rows of them 36 and 45.
 constexpr int kRow = 32768;
-// Tokens of a bin that are compared with each other, two a thread for a count of 128 * 128; 32 take the same time at
+// Tokens of a bin that are compared with each other, a thread a token, each with all others; 32 take the same time at
 // every size tried.
 constexpr int kQuick = 128;
 constexpr int kList = 4096;                // tokens of a bin that k_sample_pick holds in LDS
