@@ -356,6 +356,8 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
                     }
         __syncthreads();
     }
+    int kinds = 0;
+    static_assert(64 * kWaves % DP == 0, "");
     for (int i = threadIdx.x; i < heads * DP; i += 64 * kWaves) {
         const int h = i / DP, d = i % DP;
         if (d >= D) continue;
@@ -369,7 +371,14 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void k_attn(AttnArg
         const int64_t bh = (int64_t)b * a.heads + h0 + h;
         if (whole_unit) {
             E *y = (E *)a.y + b * a.ys.seq + (h0 + h) * a.ys.head + d * a.ys.dim;
-            if (o != o && sum == sum) o = of_values(values + d, to - from, [&](int i) { return place_of(a.c, a.table, sp.row, a.seqs, a.width, from + i); });
+            if (__builtin_expect(o != o && sum == sum, 0)) {   // d is the same for all of a thread's outputs
+                const AttnArgs &args = argument_again<AttnArgs>();
+                if (!kinds)
+                    kinds_of<1, 4>((const E *)args.values + j * args.c.head_stride + d, to - from, 0, 1,
+                                   [&](int t) { return place_of(args.c, args.table, sp.row, args.seqs, args.width, from + t); },
+                                   [&](int, int found) { return kinds |= found; });
+                o = told_by(kinds);
+            }
             *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);
             if (d == 0 && a.lse) a.lse[bh] = (ref + log2f(sum)) * kLn2;
         } else {
@@ -391,6 +400,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     constexpr int kAhead = 8, GROUPS = 256 / LANES;
     __shared__ float s_m[kMostShares + 2], s_top[4], s_sum[4];
     __shared__ f32x4 s_o[GROUPS][LANES];
+    __shared__ int s_nan, s_kinds[4 * LANES];
     const int h = blockIdx.x % a.heads, b = blockIdx.x / a.heads, t = threadIdx.x, D = a.c.head_dim;
     const int u = h / a.group * a.head_groups + h % a.group / 16;
     const int64_t unit = (int64_t)b * (a.c.kv_heads * a.head_groups) + u;
@@ -419,6 +429,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     sum *= __builtin_amdgcn_exp2f(top - finite(all));
     for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
     if (t % 64 == 0) s_top[t / 64] = all, s_sum[t / 64] = sum;
+    if (t < 4 * LANES) s_kinds[t] = 0;
+    if (t == 0) s_nan = 0;
     __syncthreads();
     top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     const float ref = finite(top);
@@ -432,19 +444,26 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 #pragma unroll 8
     for (int p = g + GROUPS * kAhead; p < n; p += GROUPS) v += out(p) * __builtin_amdgcn_exp2f(s_m[p] - ref);
     s_o[g][t % LANES] = v;
+    if (any_nan(v)) s_nan = 1;
     __syncthreads();
+    if (__builtin_expect(s_nan && sum == sum, 0)) {
+        const AttnArgs &args = argument_again<AttnArgs>();
+        const int row = row_of(args, b), lane = t % LANES;
+        const Span sp = span_of(args, row, len_of(args, row));
+        kinds_of<4, 4>((const E *)args.values + h / args.group * args.c.head_stride + min(d, D - 4), sp.len - sp.first, g, GROUPS,
+                       [&](int i) { return place_of(args.c, args.table, row, args.seqs, args.width, sp.first + i); },
+                       [&](int e, int found) {
+                           if (found) atomicOr(&s_kinds[4 * lane + e], found);
+                           return *(volatile int *)&s_kinds[4 * lane + e];
+                       });
+        __syncthreads();
+    }
     const int dim = from + t;
     if (t >= 4 * LANES || dim >= D) return;
     float o = 0.f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
-    if (o != o && sum == sum) {
-        const AttnArgs &args = argument_again<AttnArgs>();
-        const int row = row_of(args, b);
-        const Span sp = span_of(args, row, len_of(args, row));
-        o = of_values((const E *)args.values + h / args.group * args.c.head_stride + dim, sp.len - sp.first,
-                      [&](int i) { return place_of(args.c, args.table, row, args.seqs, args.width, sp.first + i); });
-    }
+    if (o != o && sum == sum) o = told_by(s_kinds[t]);
     E *y = (E *)a.y + b * a.ys.seq + h * a.ys.head + dim * a.ys.dim;
     *y = from_f32<E>(sum == 0.f ? 0.f : o / sum);
     if (dim == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;

@@ -928,6 +928,7 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
     constexpr int LANES = 32, GROUPS = 256 / LANES;
     __shared__ float s_f[kMostJoined], s_top[4], s_sum[4];
     __shared__ f32x4 s_o[GROUPS][LANES];
+    __shared__ int s_nan, s_kinds[4 * LANES];
     const AttnArgs &a = p.a;
     const int h = blockIdx.x % a.heads, b = blockIdx.x / a.heads, t = threadIdx.x, D = a.c.head_dim;
     const int j = h / a.group, hh = h - j * a.group;
@@ -957,6 +958,8 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
     sum *= __builtin_amdgcn_exp2f(top - finite(all));
     for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
     if (t % 64 == 0) s_top[t / 64] = all, s_sum[t / 64] = sum;
+    if (t < 4 * LANES) s_kinds[t] = 0;
+    if (t == 0) s_nan = 0;
     __syncthreads();
     top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     const float ref = finite(top);
@@ -972,23 +975,32 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs p, Sizes z, int 
         v += *(const f32x4 *)(parts.o + i * D + min(d, D - 4)) * __builtin_amdgcn_exp2f(m - ref);
     }
     s_o[t / LANES][t % LANES] = v;
+    if (any_nan(v)) s_nan = 1;
     __syncthreads();
-    const int dim = from + t;
-    if (t >= 4 * LANES || dim >= D) return;
-    float o = 0.f;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
-    if (o != o && sum == sum) {   // what the sequence attends to, in a row
+    if (__builtin_expect(s_nan && sum == sum, 0)) {   // over what the sequence attends to, in a row
         const PrefixArgs &again = argument_again<PrefixArgs>();
         const AttnArgs &args = again.a;
+        const int lane = t % LANES;
         Task k;
         k.row = row_of(args, b), k.to = len_of(args, k.row), k.begin = args.window && k.to > args.window ? k.to - args.window : 0;
         k.to -= k.begin, k.cut = INT32_MAX, k.skip = k.shared = 0, k.lead = -1;
         for (int g = 0; g < again.groups; ++g)
             if (const int lo = again.starts[g]; lo >= 0 && lo <= b && b < again.starts[g + 1])
                 k.shared = again.shared[g], k.lead = again.prefix_rows ? again.prefix_rows[g] : row_of(args, lo);
-        o = of_values((const E *)args.values + j * args.c.head_stride + dim, k.to, [&](int i) { return place_in(args, k, i); });
+        kinds_of<4, 4>((const E *)args.values + j * args.c.head_stride + min(d, D - 4), k.to, t / LANES, GROUPS,
+                       [&](int i) { return place_in(args, k, i); },
+                       [&](int e, int found) {
+                           if (found) atomicOr(&s_kinds[4 * lane + e], found);
+                           return *(volatile int *)&s_kinds[4 * lane + e];
+                       });
+        __syncthreads();
     }
+    const int dim = from + t;
+    if (t >= 4 * LANES || dim >= D) return;
+    float o = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) o += ((const float *)s_o[i])[t];
+    if (o != o && sum == sum) o = told_by(s_kinds[t]);
     ((E *)a.y)[b * a.ys.seq + h * a.ys.head + dim * a.ys.dim] = from_f32<E>(sum == 0.f ? 0.f : o / sum);
     if (dim == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = (ref + log2f(sum)) * kLn2;
 }
@@ -1022,9 +1034,15 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_prefix_short(
         }
         return;
     }
+    int kinds = 0;
+    static_assert(64 * WAVES % DP == 0, "");
     columns_narrow<E, DP, FULL, 1, WAVES>(a, sh, k, 0, (const E *)nullptr, [&](int, int c, int d, float o, float m, float l) {
-        if (o != o && l == l)
-            o = of_values((const E *)a.values + k.j * a.c.head_stride + d, k.to, [&](int i) { return place_in(a, k, i); });
+        if (__builtin_expect(o != o && l == l, 0)) {   // d is the same for all of a thread's outputs
+            if (!kinds)
+                kinds_of<1, 8>((const E *)a.values + k.j * a.c.head_stride + d, k.to, 0, 1, [&](int i) { return place_in(a, k, i); },
+                               [&](int, int found) { return kinds |= found; });
+            o = told_by(kinds);
+        }
         const int h = k.j * a.group + k.c0 + c;
         ((E *)a.y)[b * a.ys.seq + h * a.ys.head + d * a.ys.dim] = from_f32<E>(l == 0.f ? 0.f : o / l);
         if (d == 0 && a.lse) a.lse[(int64_t)b * a.heads + h] = ((m == -INFINITY ? 0.f : m) + log2f(l)) * kLn2;
