@@ -157,3 +157,43 @@ def test_prefix_of_other_rows(B, least, dt):
         s.values[s.table[s.prefix_rows[0], t // 16], t % 16, :, dim] = value
     s.data = [s.plane(a) for a in (s.keys, s.values)]
     check_prefix(s, *s.run(0.125), 0.125)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("least", [0, 2100])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_keys(B, value, least, dt):
+    """A score of NaN or Inf makes all of y NaN, one of -Inf is of no weight."""
+    import torch
+    P.Setup.least = least
+    try:
+        s = P.Setup(B, [3, 2], [60, 90], [[5, 9, 1], [30, 7]], 2, 4, 64, 16, dt, seed=4)
+    finally:
+        P.Setup.least = 0
+    s.keys[s.table[0, 1], 3, :, 5] = value   # token 19 of the first group
+    s.keys[s.table[3, 0], 0, :, 9] = value
+    s.data = [s.plane(a) for a in (s.keys, s.values)]
+    y, lse = s.run(0.125)
+    z, lse2 = torch.empty_like(y), torch.empty_like(lse)
+    ws = torch.empty(max(16, B.bsp_attention_workspace(s.cache, s.n, s.heads, s.width)), dtype=torch.uint8, device="cuda")
+    B.bsp_attention(s.cache, torch.from_numpy(s.q).to(s.tdt).cuda(), *s.data, s.ints(s.table), s.ints(s.lens), z, 0.125, 0, None, lse2, ws)
+    torch.cuda.synchronize()
+    odd = 0
+    for b in range(s.n):
+        p, t = np.array(s.tokens(b, 0)).T
+        for h in range(s.heads):
+            k, v = s.keys[p, t, h // 2].astype(np.float64), s.values[p, t, h // 2]
+            score = k @ s.q[b, h].astype(np.float64)
+            spoiled = bool((np.isnan(score) | (score == np.inf)).any())
+            odd += spoiled
+            on = score > -np.inf
+            for got in (y, z):
+                got = got[b, h].double().cpu().numpy()
+                if spoiled:
+                    assert np.isnan(got).all()
+                    continue
+                ref, _, size, qk = S.attention(s.q[b, h][None], k[on], v[on], 0.125)
+                score_error = 2 * (s.dim + 4) * S.U24 * qk[0]
+                u, cut = (2.0 ** -8, 2.0 ** -15) if dt == "bf16" else (S.U24, 0.0)
+                assert (np.abs(got - ref[0]) <= u * np.abs(ref[0]) + (1 + u) * (cut + 2 * score_error + (2 * len(p) + 64) * S.U24) * size[0]).all()
+    assert odd > 0 and (odd == s.n * s.heads) == np.isnan(value)
